@@ -57,6 +57,11 @@ extern "C" {
 
 #define TPLA_MAX_G 8 /* largest supported number of latent slices */
 
+#define TPLA_MAX_DRAFTS 64 /* most drafted tokens per sequence: one bit each in a mask word */
+
+#define TPLA_ROTARY_INTERLEAVED 0 /* pair j = columns 2 j, 2 j + 1                      */
+#define TPLA_ROTARY_HALF 1        /* pair j = columns j, j + rot_dim / 2                */
+
 typedef struct tpla_shape {
   int32_t B;           /* sequences in the decode batch                              */
   int32_t H;           /* query heads handled here                                   */
@@ -405,6 +410,114 @@ int tpla_stream_read(const void* buf, size_t bytes, void* sink, void* stream);
 int tpla_validate_block_table(const tpla_shape_t* shape, const int32_t* block_table,
                               int32_t max_pages_per_seq, const int32_t* seq_lens,
                               int64_t n_pool_pages, int forbid_shared);
+
+/*
+ * ---- Speculative decode: several drafted tokens per sequence and step ----
+ * Drafts are written to the cache behind the committed tokens (tpla_extend_sequences gives pages, slots and positions,
+ * tpla_apply_rotary turns queries and keys, tpla_append_token_sliced with B T rows writes), attended to in one pass
+ * (tpla_decode_shards_tree), and the accepted ones are moved together (tpla_commit_drafts).  Nothing here needs the host
+ * between two steps; every call can be captured into a graph.
+ */
+
+/*
+ * Pages, slots and positions of new tokens from the request lengths, on the GPU.  Sequence b holds seq_lens[b] tokens in
+ * pages_held[b] pages (the first entries of its block_table row) and gets add_lens[b] more:
+ *     want_b = min(ceil((seq_lens[b] + add_lens[b]) / page_tokens), max_pages_per_seq)
+ *     need_b = max(0, want_b - pages_held[b]),   first_b = sum of need over the sequences before b
+ *     block_table[b, pages_held[b] + k] = free_pages[first_b + k]   for k < need_b while first_b + k < n_free
+ *     pages_held_out[b] = pages_held[b] + pages given to b
+ * New token i of b is token t = seq_lens[b] + i of its sequence: slot block_table[b, t / page_tokens] * page_tokens +
+ * t % page_tokens, or -1 where that page is not held (no free page, or beyond the row), and position t, or with depths
+ * seq_lens[b] + depths[b, i] (drafts of a tree: siblings share a position).  row_tokens = 0: tokens are packed, those of b
+ * at cu_tokens[b] .. cu_tokens[b + 1] - 1; n_tokens is the room in slots and positions, entries behind the last token get
+ * slot -1 and position 0.  row_tokens > 0: token i of b is at b * row_tokens + i, add_lens is clipped to row_tokens, the
+ * rest of a row gets slot -1 and position 0, n_tokens = B * row_tokens.  cu_tokens int32 [B + 1] is the prefix sum of
+ * add_lens either way, clipped to n_tokens.  counts int32 [2]: pages taken from the front of free_pages, pages that were
+ * missing.  Negative lengths count as 0, lengths beyond the row as the row's.  pages_held_out may be pages_held.  All
+ * pointers but counts' meaning above are int32 DEVICE arrays; depths [B, row_tokens] or NULL; free_pages may be NULL with
+ * n_free = 0.  Only shape->B and page_tokens are read (the shape is checked whole).
+ */
+int tpla_extend_sequences(const tpla_shape_t* shape, const int32_t* seq_lens, const int32_t* add_lens, int32_t row_tokens,
+                          const int32_t* depths, const int32_t* free_pages, int32_t n_free, const int32_t* pages_held,
+                          int32_t* pages_held_out, int32_t* block_table, int32_t max_pages_per_seq, int32_t* cu_tokens,
+                          int32_t* slots, int32_t* positions, int64_t n_tokens, int32_t* counts, void* stream);
+
+/*
+ * Frequencies of tpla_apply_rotary, on the HOST: freq double [rot_dim / 2], radians per position,
+ *     f_j = base^(-2 j / rot_dim).
+ * factor > 1 stretches them for contexts that many times as long.  original_positions = 0: every f_j / factor.  Otherwise by
+ * how often a pair turns over the original_positions the model was trained on: pairs that turn at least beta_fast times stay,
+ * those that turn at most beta_slow times are divided by factor, between them linearly in j, the ends of that ramp rounded
+ * outwards to whole pairs.  (The factor on sine and cosine that goes with it is tpla_apply_rotary's amplitude.)
+ */
+int tpla_rotary_frequencies(int32_t rot_dim, double base, double factor, int32_t original_positions, double beta_fast,
+                            double beta_slow, double* freq);
+
+/*
+ * Rotary positions of queries and keys.  Row t of q (H heads of d_r columns) and of k (d_r columns, shared by the heads) is
+ * turned by the angles a_j = positions[t] * freq[j]:
+ *     (x, y) -> amplitude * (x cos a_j - y sin a_j, x sin a_j + y cos a_j)
+ * for the rot_dim / 2 pairs of `layout`; columns rot_dim .. d_r - 1 are copied.  inverse = 1 turns by -a_j: the transpose,
+ * hence the gradient with respect to the input.  Angles are formed in double, sine and cosine and the products in float, one
+ * rounding on the way out.  q, k, q_out, k_out in shape->dtype with strides in elements (innermost dense), so that they may be
+ * columns of a wider projection; pointers and strides in whole 16 bytes (TPLA_ERR_ALIGN).  An output may be its input, with
+ * the same strides; no other overlap.  q with q_out, or k with k_out, may be NULL.  freq double [rot_dim / 2] and positions
+ * int32 [T] on the device; rot_dim even, 2 .. d_r.  Only H, d_r and dtype of shape are read (the shape is checked whole).
+ */
+int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse, int32_t rot_dim, const double* freq,
+                      float amplitude, const int32_t* positions, int64_t T, const void* q, int64_t q_token_stride,
+                      int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                      const void* k, int64_t k_token_stride, void* k_out, int64_t k_out_token_stride, void* stream);
+
+/*
+ * tpla_decode_shard(s) for T drafted tokens per sequence, 1 <= T <= TPLA_MAX_DRAFTS.  seq_lens[b] counts the committed
+ * tokens; draft j of b (j < draft_lens[b]; draft_lens NULL: T for all) is token seq_lens[b] + j, already in the cache.
+ * Draft t attends to every committed token and to draft j where bit j of tree_mask[b, t] is set; its own bit is not
+ * implied.  For draft t of sequence b and head h, over the tokens it sees:
+ *     s_k = sm_scale * (q_lat_i[b,t,h] . row_k[:d_c/g] + q_pe[b,t,h] . row_k[d_c/g:])
+ *     o_lat_i[b,t,h,:] = sum_k softmax(s)_k row_k[:d_c/g]       lse_i[b,t,h] = log sum_k exp(s_k)
+ * A row that sees nothing, and rows t >= draft_lens[b], get o = 0, lse = -inf.  What a draft's row holds (infinities and NaN
+ * too) does not reach rows that do not see it; bits at or beyond draft_lens[b] are ignored; slots at or beyond seq_lens[b] +
+ * draft_lens[b] are never read.  Lengths out of range are clipped as in tpla_decode_shard (drafts beyond the block-table row
+ * are not seen).  q_lat [g,B,T,H,d_c/g], q_pe [B,T,H,d_r] in shape->dtype: the layout of tpla_absorb_query, and o_lat float
+ * [g,B,T,H,d_c/g] that of tpla_combine_shards, called with B T rows.  tree_mask uint64 [B,T] and draft_lens int32 [B] on the
+ * device; lse float [g,B,T,H] or NULL.  The other arguments as in tpla_decode_shards; any page size.  Bit-reproducible for
+ * fixed arguments.  bf16 with d_r = 64 and d_c/g of 64, 128, 256 or 512 runs on the matrix cores, with the softmax weights
+ * rounded to bf16 for the product with the values as in tpla_decode_shards; everything else in float
+ * (TPLA_ERR_UNSUPPORTED beyond d_c/g = 1024 or d_c/g + d_r = 1984).
+ */
+size_t tpla_workspace_bytes_tree(const tpla_shape_t* shape, int32_t T, int32_t max_pages_per_seq);
+int tpla_decode_shard_tree(const tpla_shape_t* shape, int32_t T, const void* q_lat_i, const void* q_pe, const void* shard_pool,
+                           const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                           const int32_t* draft_lens, const uint64_t* tree_mask, void* workspace, size_t workspace_bytes,
+                           float* o_lat_i, float* lse_i, void* stream);
+int tpla_decode_shards_tree(const tpla_shape_t* shape, int32_t T, const void* q_lat, const void* q_pe,
+                            const void* const* shard_pools, const int32_t* block_table, int32_t max_pages_per_seq,
+                            const int32_t* seq_lens, const int32_t* draft_lens, const uint64_t* tree_mask, void* workspace,
+                            size_t workspace_bytes, float* o_lat, float* lse, void* stream);
+
+/*
+ * tpla_decode_shards_tree, then tpla_combine_shards_to over the B T rows: o [B, T, H, d_v] float (o_dtype = TPLA_F32) or
+ * bfloat16 (TPLA_BF16).  o_lat is required and written.  Every argument check runs before the first launch.
+ */
+int tpla_decode_shards_tree_combine(const tpla_shape_t* shape, int32_t T, const void* q_lat, const void* q_pe,
+                                    const void* const* shard_pools, const int32_t* block_table, int32_t max_pages_per_seq,
+                                    const int32_t* seq_lens, const int32_t* draft_lens, const uint64_t* tree_mask,
+                                    void* workspace, size_t workspace_bytes, const void* W_UV_t, void* o, int32_t o_dtype,
+                                    float* o_lat, float* lse, void* stream);
+
+/*
+ * The accepted drafts of every sequence behind its committed tokens: for k < n_accepted[b], in all g pools,
+ *     row of token seq_lens[b] + k  =  row of token seq_lens[b] + accepted[b, k]   (as it was before the call)
+ * and new_lens[b] = seq_lens[b] + n_accepted[b].  accepted int32 [B, T]: indices into the drafts, ascending (a path of a
+ * tree whose parents come before their children); n_accepted int32 [B], clipped to [0, T] and to the block-table row.
+ * Entries outside [0, T) are clipped; an order that is not ascending gives wrong rows, never an access outside the pages
+ * listed.  new_lens may be seq_lens.  No two sequences may share the pages that hold their drafts.  Rows are copied bit for
+ * bit.  d_n, d_v, H of shape are not used.
+ */
+int tpla_commit_drafts(const tpla_shape_t* shape, int32_t T, const int32_t* accepted, const int32_t* n_accepted,
+                       const int32_t* seq_lens, const int32_t* block_table, int32_t max_pages_per_seq,
+                       void* const* shard_pools, int32_t* new_lens, void* stream);
 
 #ifdef __cplusplus
 }

@@ -15,4 +15,7 @@ from .binding import (  # noqa: F401
     tpla_decode_shards_combine, tpla_validate_block_table, tpla_decode_shards_combine_static,
     tpla_combine_shards_to, tpla_decode_shards_combine_to, tpla_output_projection_to,
     tpla_attention_block_workspace_bytes, tpla_decode_shards_project,
+    TPLA_MAX_DRAFTS, TPLA_ROTARY_HALF, TPLA_ROTARY_INTERLEAVED,
+    tpla_extend_sequences, tpla_rotary_frequencies, tpla_apply_rotary, tpla_workspace_bytes_tree, tpla_decode_shard_tree,
+    tpla_decode_shards_tree, tpla_decode_shards_tree_combine, tpla_commit_drafts,
 )

@@ -16,6 +16,8 @@ _LIB_PATH = os.environ.get("TPLA_LIBRARY") or os.path.join(_PKG, "lib", "libtpla
 TPLA_F32, TPLA_BF16 = 0, 1
 TPLA_U_IDENTITY, TPLA_U_HADAMARD, TPLA_U_DENSE = 0, 1, 2
 TPLA_MAX_G = 8
+TPLA_MAX_DRAFTS = 64
+TPLA_ROTARY_INTERLEAVED, TPLA_ROTARY_HALF = 0, 1
 
 EXPORTS = (
     "tpla_last_error", "tpla_version", "tpla_transform_latent", "tpla_transform_latent_paged",
@@ -27,6 +29,8 @@ EXPORTS = (
     "tpla_decode_shards_combine", "tpla_validate_block_table", "tpla_decode_shards_combine_static",
     "tpla_combine_shards_to", "tpla_decode_shards_combine_to", "tpla_output_projection_to",
     "tpla_attention_block_workspace_bytes", "tpla_decode_shards_project",
+    "tpla_extend_sequences", "tpla_rotary_frequencies", "tpla_apply_rotary", "tpla_workspace_bytes_tree",
+    "tpla_decode_shard_tree", "tpla_decode_shards_tree", "tpla_decode_shards_tree_combine", "tpla_commit_drafts",
 )
 
 
@@ -129,6 +133,23 @@ def load_library():
     lib.tpla_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
     lib.tpla_validate_block_table.restype = ctypes.c_int
     lib.tpla_validate_block_table.argtypes = [shp, vp, i32, vp, i64, ctypes.c_int]
+    lib.tpla_extend_sequences.restype = ctypes.c_int
+    lib.tpla_extend_sequences.argtypes = [shp, vp, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, i64, vp, vp]
+    lib.tpla_rotary_frequencies.restype = ctypes.c_int
+    lib.tpla_rotary_frequencies.argtypes = [i32, ctypes.c_double, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, vp]
+    lib.tpla_apply_rotary.restype = ctypes.c_int
+    lib.tpla_apply_rotary.argtypes = [shp, i32, i32, i32, vp, ctypes.c_float, vp, i64, vp, i64, i64, vp, i64, i64, vp, i64, vp, i64, vp]
+    lib.tpla_workspace_bytes_tree.restype = ctypes.c_size_t
+    lib.tpla_workspace_bytes_tree.argtypes = [shp, i32, i32]
+    lib.tpla_decode_shard_tree.restype = ctypes.c_int
+    lib.tpla_decode_shard_tree.argtypes = [shp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, ctypes.c_size_t, vp, vp, vp]
+    lib.tpla_decode_shards_tree.restype = ctypes.c_int
+    lib.tpla_decode_shards_tree.argtypes = [shp, i32, vp, vp, ctypes.POINTER(vp), vp, i32, vp, vp, vp, vp, ctypes.c_size_t, vp, vp, vp]
+    lib.tpla_decode_shards_tree_combine.restype = ctypes.c_int
+    lib.tpla_decode_shards_tree_combine.argtypes = [shp, i32, vp, vp, ctypes.POINTER(vp), vp, i32, vp, vp, vp, vp, ctypes.c_size_t,
+                                                    vp, vp, i32, vp, vp, vp]
+    lib.tpla_commit_drafts.restype = ctypes.c_int
+    lib.tpla_commit_drafts.argtypes = [shp, i32, vp, vp, vp, vp, i32, ctypes.POINTER(vp), vp, vp]
     lib.tpla_pca_basis.restype = ctypes.c_int
     lib.tpla_pca_basis.argtypes = [i32, i32, i64, vp, vp, vp, vp, vp]
     _lib = lib
@@ -336,6 +357,79 @@ def tpla_latent_moments(shape, mla_pool, page_ids, page_fill, n_pages, workspace
     _check(load_library().tpla_latent_moments(
         ctypes.byref(shape), _ptr(mla_pool), _ptr(page_ids), _ptr(page_fill), n_pages, _ptr(workspace),
         workspace_bytes, _ptr(sum_out), _ptr(gram_out), _stream(stream)))
+
+
+def tpla_extend_sequences(shape, seq_lens, add_lens, row_tokens, depths, free_pages, n_free, pages_held, pages_held_out,
+                          block_table, max_pages_per_seq, cu_tokens, slots, positions, n_tokens, counts, stream=None):
+    _check(load_library().tpla_extend_sequences(
+        ctypes.byref(shape), _ptr(seq_lens), _ptr(add_lens), row_tokens, _ptr(depths), _ptr(free_pages), n_free,
+        _ptr(pages_held), _ptr(pages_held_out), _ptr(block_table), max_pages_per_seq, _ptr(cu_tokens), _ptr(slots),
+        _ptr(positions), n_tokens, _ptr(counts), _stream(stream)))
+
+
+def tpla_rotary_frequencies(rot_dim, base=10000.0, factor=1.0, original_positions=0, beta_fast=32.0, beta_slow=1.0):
+    """Host call.  float64 numpy array [rot_dim / 2]: radians per position of every pair."""
+    import numpy as np
+    freq = np.empty(max(1, rot_dim // 2), dtype=np.float64)
+    _check(load_library().tpla_rotary_frequencies(rot_dim, base, factor, original_positions, beta_fast, beta_slow,
+                                                  freq.ctypes.data))
+    return freq
+
+
+def _view(x, dims):
+    """Address and the strides (in elements) of a tensor whose innermost dimension is dense."""
+    if x is None:
+        return (None,) + (0,) * (dims - 1)
+    if x.dim() != dims or (x.shape[-1] > 1 and x.stride(-1) != 1):
+        raise ValueError("libtpla needs a tensor of %d dimensions, the innermost one dense" % dims)
+    return (x.data_ptr(),) + x.stride()[:-1]
+
+
+def tpla_apply_rotary(shape, layout, inverse, rot_dim, freq, amplitude, positions, T, q, q_out, k, k_out, stream=None):
+    """q, q_out [T, H, d_r] and k, k_out [T, d_r] may be views (a part of a wider projection): their strides, which the C
+    call takes after each pointer, are read off the tensors.  q (with q_out) or k (with k_out) may be None."""
+    for x, y, want in ((q, q_out, (T, shape.H, shape.d_r)), (k, k_out, (T, shape.d_r))):
+        for z in (x, y):
+            if z is not None and tuple(z.shape) != want:
+                raise ValueError("libtpla needs a tensor of shape %r, got %r" % (want, tuple(z.shape)))
+    _check(load_library().tpla_apply_rotary(
+        ctypes.byref(shape), layout, inverse, rot_dim, _ptr(freq), amplitude, _ptr(positions), T, *_view(q, 3), *_view(q_out, 3),
+        *_view(k, 2), *_view(k_out, 2), _stream(stream)))
+
+
+def tpla_workspace_bytes_tree(shape, T, max_pages_per_seq):
+    return int(load_library().tpla_workspace_bytes_tree(ctypes.byref(shape), T, max_pages_per_seq))
+
+
+def tpla_decode_shard_tree(shape, T, q_lat_i, q_pe, shard_pool, block_table, max_pages_per_seq, seq_lens, draft_lens, tree_mask,
+                           workspace, workspace_bytes, o_lat_i, lse_i, stream=None):
+    _check(load_library().tpla_decode_shard_tree(
+        ctypes.byref(shape), T, _ptr(q_lat_i), _ptr(q_pe), _ptr(shard_pool), _ptr(block_table), max_pages_per_seq,
+        _ptr(seq_lens), _ptr(draft_lens), _ptr(tree_mask), _ptr(workspace), workspace_bytes, _ptr(o_lat_i), _ptr(lse_i),
+        _stream(stream)))
+
+
+def tpla_decode_shards_tree(shape, T, q_lat, q_pe, shard_pools, block_table, max_pages_per_seq, seq_lens, draft_lens, tree_mask,
+                            workspace, workspace_bytes, o_lat, lse, stream=None):
+    _check(load_library().tpla_decode_shards_tree(
+        ctypes.byref(shape), T, _ptr(q_lat), _ptr(q_pe), _pool_array(shard_pools), _ptr(block_table), max_pages_per_seq,
+        _ptr(seq_lens), _ptr(draft_lens), _ptr(tree_mask), _ptr(workspace), workspace_bytes, _ptr(o_lat), _ptr(lse),
+        _stream(stream)))
+
+
+def tpla_decode_shards_tree_combine(shape, T, q_lat, q_pe, shard_pools, block_table, max_pages_per_seq, seq_lens, draft_lens,
+                                    tree_mask, workspace, workspace_bytes, W_UV_t, o, o_dtype, o_lat, lse, stream=None):
+    _check(load_library().tpla_decode_shards_tree_combine(
+        ctypes.byref(shape), T, _ptr(q_lat), _ptr(q_pe), _pool_array(shard_pools), _ptr(block_table), max_pages_per_seq,
+        _ptr(seq_lens), _ptr(draft_lens), _ptr(tree_mask), _ptr(workspace), workspace_bytes, _ptr(W_UV_t), _ptr(o), o_dtype,
+        _ptr(o_lat), _ptr(lse), _stream(stream)))
+
+
+def tpla_commit_drafts(shape, T, accepted, n_accepted, seq_lens, block_table, max_pages_per_seq, shard_pools, new_lens,
+                       stream=None):
+    _check(load_library().tpla_commit_drafts(
+        ctypes.byref(shape), T, _ptr(accepted), _ptr(n_accepted), _ptr(seq_lens), _ptr(block_table), max_pages_per_seq,
+        _pool_array(shard_pools), _ptr(new_lens), _stream(stream)))
 
 
 def tpla_pca_basis(d_c, g, n_rows, sum_host, gram_host):

@@ -71,9 +71,7 @@ static void profile_mark(hipStream_t st, bool start) {
   if (!start) ++g_prof.used;
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-static int check_dtype(const tpla_shape_t* sh) {
+int check_dtype(const tpla_shape_t* sh) {
   if (!sh) return fail(TPLA_ERR_NULL, "shape is NULL");
   if (sh->dtype != TPLA_F32 && sh->dtype != TPLA_BF16)
     return fail(TPLA_ERR_DTYPE, "dtype %d is neither TPLA_F32 nor TPLA_BF16", sh->dtype);
@@ -81,7 +79,7 @@ static int check_dtype(const tpla_shape_t* sh) {
 }
 
 // Full consistency check of the attention geometry.
-static int check_shape(const tpla_shape_t* sh) {
+int check_shape(const tpla_shape_t* sh) {
   int rc = check_dtype(sh);
   if (rc) return rc;
   if (sh->B < 1 || sh->H < 1 || sh->d_c < 1 || sh->g < 1 || sh->d_r < 1 || sh->d_n < 1 ||

@@ -279,6 +279,98 @@ int launch_prefill_attention(const tpla_shape_t& sh, const void* q_nope, const v
                              const void* k_pe, const void* W_UK, const void* W_UV, const int32_t* cu_seqlens,
                              int T, int max_seq_len, void* kv_workspace, float* o, hipStream_t st);
 
+// Argument checks shared by the entry points (api.hip).
+int check_dtype(const tpla_shape_t* sh);
+int check_shape(const tpla_shape_t* sh);
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Pages, slots and positions of new tokens; accepted drafts: see token_tables.hip.
+struct ExtendArgs {
+  const int32_t* seq_lens;
+  const int32_t* add_lens;
+  const int32_t* depths;       // [B, row_tokens] or nullptr
+  const int32_t* free_pages;
+  const int32_t* held;         // held_out may be the same array
+  int32_t* held_out;
+  int32_t* block_table;
+  int32_t* cu;                 // [B + 1]
+  int32_t* slots;
+  int32_t* positions;
+  int32_t* counts;             // pages taken, pages missing
+  int32_t B, page_tokens, max_pages, row_tokens, n_free, n_tokens;
+};
+int launch_extend_sequences(const ExtendArgs& a, hipStream_t st);
+struct CommitArgs {
+  ShardPools pools;
+  const int32_t* accepted;     // [B, T]
+  const int32_t* n_accepted;
+  const int32_t* seq_lens;     // new_lens may be the same array
+  const int32_t* block_table;
+  int32_t* new_lens;
+  int32_t T, n_shards, page_tokens, max_pages, row_bytes, B;
+};
+int launch_commit_drafts(const CommitArgs& a, hipStream_t st);
+
+// Rotary positions: see rotary.hip.  Strides in elements; q or k may be nullptr.
+struct RotaryArgs {
+  const double* freq;          // [rot / 2] radians per position
+  const int32_t* positions;
+  const void* q;
+  const void* k;
+  void* q_out;
+  void* k_out;
+  int64_t T, q_ts, q_hs, qo_ts, qo_hs, k_ts, ko_ts;
+  int32_t H, d_r, rot, layout, inverse;
+  float amplitude;
+  int32_t block_tokens, block_heads;     // filled in by the launcher
+};
+int launch_rotary(RotaryArgs a, int dtype, hipStream_t st);
+
+// Attention of drafted tokens: see tree.hip, tree_mfma.hip.  Row r = t H + h of a (slice, sequence) is head h of draft t.
+// Rows go in blocks of `block` of one (slice, sequence), an "item"; item index = (slice B + b) blocks + row block.
+struct TreePlan {
+  int32_t mfma;                // the matrix-core kernel; otherwise the general one
+  int32_t block, blocks;       // rows per item, items per (slice, sequence)
+  int32_t n_wg;                // mfma: workgroups; partial slots 2 n_wg
+  int32_t n_splits, split_tokens;   // general: splits of the longest sequence; slots items * n_splits
+};
+struct TreeArgs {
+  const void* q_lat;           // [n_shards, B, T, H, dl]
+  const void* q_pe;            // [B, T, H, d_r]
+  const void* pools[TPLA_MAX_G];
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const int32_t* draft_lens;   // or nullptr: T for every sequence
+  const unsigned long long* mask;   // [B, T]
+  float* part_acc;             // [slots, block, dl]
+  float* part_ml;              // [slots, block, 2]
+  int32_t* plan;               // mfma: per item (first workgroup, number of them, whether its part is the first's last segment)
+  float* o_lat;                // [n_shards, B, T, H, dl]
+  float* lse;                  // [n_shards, B, T, H] or nullptr
+  int32_t n_shards, B, T, H, dl, d_r, page_tokens, max_pages;
+  TreePlan p;
+  float scale_log2;
+};
+bool tree_mfma_supported(const tpla_shape_t& sh);
+void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p);
+int launch_tree_mfma(const TreeArgs& a, hipStream_t st);
+int launch_tree_generic(const TreeArgs& a, int dtype, hipStream_t st);
+int launch_tree_merge(const TreeArgs& a, hipStream_t st);
+// Committed and drafted tokens of a sequence as the kernels use them, clipped to what its block-table row can address.
+struct TreeLens {
+  int L, n, keys;              // committed, drafts (= rows / H), tokens whose rows may be read
+};
+__device__ __forceinline__ TreeLens tree_lens(const TreeArgs& a, int b) {
+  const long long cap = (long long)a.max_pages * a.page_tokens, L = a.seq_lens[b];
+  TreeLens r;
+  r.L = (int)(L < 0 ? 0 : (L > cap ? cap : L));
+  const int n = a.draft_lens ? a.draft_lens[b] : a.T;
+  r.n = n < 0 ? 0 : (n > a.T ? a.T : n);
+  const long long keys = (long long)r.L + r.n;
+  r.keys = (int)(keys > cap ? cap : keys);
+  return r;
+}
+
 int launch_stream_read(const void* buf, size_t bytes, void* sink, hipStream_t st);
 
 // PCA calibration: see pca.hip.

@@ -1,0 +1,173 @@
+"""tpla_extend_sequences and tpla_commit_drafts against plain host loops: whole numbers and moved rows, equal to the bit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_15881_amd as tp
+
+pytestmark = pytest.mark.gpu
+
+
+def shape(B, pt=64, g=2, dl=256, d_r=64, dtype=None):
+    return tp.TplaShape(B, 16, dl * g, g, d_r, 128, 128, pt, tp.TPLA_BF16 if dtype is None else dtype, 0.07)
+
+
+def extend_plain(pt, lens, adds, row_tokens, depths, free, held, table, n_tokens):
+    B, max_pages = table.shape
+    table, held = table.copy(), list(held)
+    cu, slots, pos = [0], np.full(n_tokens, -1, dtype=np.int64), np.zeros(n_tokens, dtype=np.int64)
+    first = taken = missing = 0
+    for b in range(B):
+        L, n = min(max(lens[b], 0), max_pages * pt), max(adds[b], 0)
+        n = min(n, row_tokens) if row_tokens else n
+        need = max(0, min(-(-(L + n) // pt), max_pages) - held[b])
+        for k in range(need):
+            if first + k < len(free):
+                table[b, held[b] + k] = free[first + k]
+        given = min(need, max(0, len(free) - first))
+        first, taken, missing, held[b] = first + need, taken + given, missing + need - given, held[b] + given
+        at0 = b * row_tokens if row_tokens else cu[-1]
+        for i in range(n):
+            if at0 + i >= n_tokens:
+                break
+            t = L + i
+            slots[at0 + i] = table[b, t // pt] * pt + t % pt if t // pt < held[b] else -1
+            pos[at0 + i] = L + (int(depths[b, i]) if depths is not None else i)
+        cu.append(min(cu[-1] + n, n_tokens))
+    return table, held, cu, slots, pos, [taken, missing]
+
+
+def extend(pt, lens, adds, row_tokens, depths, free, held, table, n_tokens, in_place=False, stream=None):
+    B, max_pages = table.shape
+    dev = lambda v: torch.tensor(np.asarray(v, dtype=np.int32)).cuda()  # noqa: E731
+    t = dict(lens=dev(lens), adds=dev(adds), free=dev(free) if len(free) else None, held=dev(held), table=dev(table),
+             depths=None if depths is None else dev(depths))
+    out = t["held"] if in_place else torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    cu, counts = torch.full((B + 1,), -7, dtype=torch.int32, device="cuda"), torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    slots, pos = torch.full((n_tokens + 4,), -7, dtype=torch.int32, device="cuda"), torch.full((n_tokens + 4,), -7, dtype=torch.int32, device="cuda")
+    tp.tpla_extend_sequences(shape(B, pt), t["lens"], t["adds"], row_tokens, t["depths"], t["free"], len(free), t["held"], out, t["table"],
+                             max_pages, cu, slots, pos, n_tokens, counts)
+    torch.cuda.synchronize()
+    assert (slots[n_tokens:] == -7).all() and (pos[n_tokens:] == -7).all()
+    if not in_place:
+        assert t["held"].tolist() == list(held)
+    return t["table"].cpu().numpy(), out.tolist(), cu.tolist(), slots[:n_tokens].cpu().numpy(), pos[:n_tokens].cpu().numpy(), counts.tolist()
+
+
+def assert_same(got, want):
+    for name, x, y in zip(("table", "held", "cu", "slots", "positions", "counts"), got, want):
+        assert np.array_equal(np.asarray(x, dtype=np.int64), np.asarray(y, dtype=np.int64)), name
+
+
+def problem(r, B, pt, max_len, max_add, max_pages=None, spare=5, extra_held=0):
+    lens = r.integers(0, max_len + 1, B).tolist()
+    adds = r.integers(0, max_add + 1, B).tolist()
+    max_pages = max_pages or max(-(-(a + b) // pt) for a, b in zip(lens, adds)) + 2
+    held = [min(max_pages, -(-a // pt) + (int(r.integers(0, extra_held + 1)) if extra_held else 0)) for a in lens]
+    n = sum(held) + sum(-(-(a + b) // pt) for a, b in zip(lens, adds)) + spare
+    ids = r.permutation(n)
+    table = np.full((B, max_pages), -1, dtype=np.int32)
+    k = 0
+    for b in range(B):
+        table[b, :held[b]] = ids[k:k + held[b]]
+        k += held[b]
+    return lens, adds, held, table, ids[k:].astype(np.int32)
+
+
+@pytest.mark.parametrize("B,pt,row_tokens,max_len,max_add,extra,in_place", [
+    (1, 64, 1, 0, 1, 0, False), (1, 64, 0, 5, 200, 0, False), (7, 16, 5, 100, 5, 2, True), (48, 64, 1, 3000, 1, 0, True),
+    (130, 1, 64, 60, 64, 0, False), (1025, 64, 3, 500, 3, 1, True), (2500, 32, 0, 90, 40, 0, False), (33, 64, 0, 10, 4000, 0, True),
+    (3, 7, 0, 1000, 30000, 0, False), (64, 128, 17, 2000, 17, 0, False),
+])
+def test_extend(B, pt, row_tokens, max_len, max_add, extra, in_place):
+    r = np.random.default_rng([B, pt, max_add])
+    lens, adds, held, table, free = problem(r, B, pt, max_len, max_add, extra_held=extra)
+    depths = r.integers(0, 9, (B, row_tokens)) if row_tokens and B % 2 else None
+    n = B * row_tokens if row_tokens else sum(adds)
+    args = (pt, lens, adds, row_tokens, depths, free, held, table, n)
+    assert_same(extend(*args, in_place=in_place), extend_plain(*args))
+
+
+def test_extend_room_for_more_and_for_fewer_tokens():
+    r = np.random.default_rng(3)
+    lens, adds, held, table, free = problem(r, 20, 64, 100, 300)
+    for n in (sum(adds) + 77, sum(adds) - 50, 1, 0, 20000):
+        args = (64, lens, adds, 0, None, free, held, table, n)
+        assert_same(extend(*args), extend_plain(*args))
+
+
+@pytest.mark.parametrize("n_free", [0, 1, 5, 11])
+def test_extend_runs_out_of_pages(n_free):
+    r = np.random.default_rng(4)
+    lens, adds, held, table, free = problem(r, 9, 16, 50, 60)
+    args = (16, lens, adds, 0, None, free[:n_free], held, table, sum(adds))
+    got = extend(*args)
+    assert_same(got, extend_plain(*args))
+    assert got[5][0] == n_free and got[5][1] > 0 and (got[3] == -1).any()
+
+
+def test_extend_beyond_the_row_and_out_of_range():
+    r = np.random.default_rng(5)
+    lens, adds, held, table, free = problem(r, 8, 16, 60, 100, max_pages=5)
+    lens[0], lens[1], adds[2], adds[3] = -4, 500, -9, 2000
+    held = [min(max(0, -(-min(max(v, 0), 80) // 16)), 5) for v in lens]
+    table = np.arange(40, dtype=np.int32).reshape(8, 5)
+    args = (16, lens, adds, 0, None, free, held, table, sum(max(a, 0) for a in adds))
+    assert_same(extend(*args), extend_plain(*args))
+
+
+@pytest.mark.parametrize("T,g,dl,pt,dtype", [(1, 1, 256, 64, "bf16"), (8, 2, 256, 64, "bf16"), (64, 4, 128, 16, "bf16"), (64, 1, 512, 1, "bf16"),
+                                            (13, 2, 72, 3, "f32"), (40, 8, 512, 64, "f32")])
+def test_commit(T, g, dl, pt, dtype):
+    B, d_r = 7, 64
+    r = np.random.default_rng([T, g, pt])
+    lens = [0, 1, pt, pt - 1, 5 * pt + 2, 130, 33][:B]
+    pages = [-(-(n + T) // pt) for n in lens]
+    mp, n_pool = max(pages), sum(pages) + 2
+    order, k = r.permutation(n_pool), 0
+    bt = np.full((B, mp), n_pool - 1, dtype=np.int32)
+    for b in range(B):
+        bt[b, :pages[b]] = order[k:k + pages[b]]
+        k += pages[b]
+    acc, n_acc = np.zeros((B, T), dtype=np.int32), []
+    for b in range(B):
+        n = [0, T, 1, T // 2, max(1, T - 1), T // 3, T][b]
+        acc[b, :n] = np.sort(r.choice(T, n, replace=False))
+        acc[b, n:] = r.integers(-5, 2 * T, T - n)              # behind the accepted ones: not looked at
+        n_acc.append(n)
+    st = torch.float32 if dtype == "f32" else torch.bfloat16
+    pools = [torch.from_numpy(r.standard_normal((n_pool, pt, dl + d_r)).astype(np.float32)).cuda().to(st) for _ in range(g)]
+    want = [p.cpu().clone() for p in pools]
+    at = lambda b, t: (int(bt[b, t // pt]), t % pt)  # noqa: E731
+    for w, p in zip(want, pools):
+        old = p.cpu()
+        for b in range(B):
+            for j in range(n_acc[b]):
+                w[at(b, lens[b] + j)] = old[at(b, lens[b] + int(acc[b, j]))]
+    s = shape(B, pt, g, dl, d_r, tp.TPLA_F32 if dtype == "f32" else tp.TPLA_BF16)
+    dev = lambda v: torch.tensor(np.asarray(v, dtype=np.int32)).cuda()  # noqa: E731
+    ln, new = dev(lens), torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    if T % 2:
+        new = ln                                               # in place
+    tp.tpla_commit_drafts(s, T, dev(acc), dev(n_acc), ln, dev(bt), mp, pools, new)
+    torch.cuda.synchronize()
+    for w, p in zip(want, pools):
+        assert torch.equal(w.view(torch.int32 if dtype == "f32" else torch.int16), p.cpu().view(torch.int32 if dtype == "f32" else torch.int16))
+    assert new.tolist() == [a + b for a, b in zip(lens, n_acc)]
+
+
+def test_commit_clips_what_is_out_of_range():
+    pt, T, B = 16, 4, 3
+    s = shape(B, pt, 1, 64)
+    pool = torch.randn((6, pt, 128), device="cuda").to(torch.bfloat16)
+    old = pool.clone()
+    bt = torch.arange(6, dtype=torch.int32, device="cuda").reshape(3, 2)
+    acc = torch.tensor([[1, 2, 3, 99], [-5, 3, 3, 3], [0, 1, 2, 3]], dtype=torch.int32, device="cuda")
+    n_acc = torch.tensor([4, -2, 9], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([30, 10, 31], dtype=torch.int32, device="cuda")      # 32 tokens a row
+    new = torch.zeros(3, dtype=torch.int32, device="cuda")
+    tp.tpla_commit_drafts(s, T, acc, n_acc, lens, bt, 2, [pool], new)
+    torch.cuda.synchronize()
+    assert new.tolist() == [32, 10, 32]
+    old[1, 14] = old[1, 15]                                    # draft 1 of sequence 0 is the last token its row holds
+    assert torch.equal(old, pool)

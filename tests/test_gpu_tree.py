@@ -1,0 +1,229 @@
+"""Attention of drafted tokens (tpla_decode_shard(s)_tree) against its 64-bit definition, at the sizes and masks where it can go
+wrong.  Every bound is derived from the roundings in draft_common.TreeProblem.expected."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_15881_amd as tp
+from paper_2508_15881_amd import workloads as wl
+from draft_common import TreeProblem, assert_close, chain_masks, out_buffers, run_all, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,dl,g,H,T,lens,drafts,pt", [
+    ("bf16", 256, 2, 16, 4, [130, 1, 64, 0, 1000], [4, 1, 3, 2, 4], 64),
+    ("bf16", 256, 2, 64, 3, [33, 500], [3, 2], 64),                  # 192 rows
+    ("bf16", 256, 1, 64, 8, [95, 96, 97], [8, 8, 8], 64),            # 512 rows, ends around a tile's edge
+    ("bf16", 256, 2, 5, 7, [31, 62, 640], [7, 1, 5], 16),            # 35 rows, pages that end inside a tile
+    ("bf16", 256, 1, 16, 64, [200, 3], [64, 61], 64),                # the most drafts
+    ("bf16", 256, 1, 16, 2, [700, 77], [2, 2], 1),                   # one token a page: ids in several chunks
+    ("bf16", 256, 1, 16, 2, [1500, 300], [2, 1], 3),
+    ("bf16", 256, 2, 1, 1, [1, 0, 2049], [1, 1, 1], 128),            # one row
+    ("bf16", 128, 4, 64, 4, [300, 65], [4, 4], 64),
+    ("bf16", 128, 4, 16, 2, [31, 0, 1025], [2, 2, 0], 32),
+    ("bf16", 64, 8, 16, 9, [257, 40], [9, 6], 64),
+    ("bf16", 64, 8, 64, 4, [100], [4], 64),
+    ("bf16", 512, 1, 16, 5, [129, 800], [5, 3], 64),
+    ("bf16", 512, 1, 64, 2, [64, 31], [2, 1], 16),
+    ("bf16", 72, 2, 6, 5, [70, 3], [5, 4], 16),                      # a width of the general kernel
+    ("f32", 32, 2, 4, 5, [128, 60, 0], [5, 3, 2], 64),
+    ("f32", 256, 2, 3, 6, [900, 1], [6, 6], 64),
+    ("f32", 1024, 1, 2, 3, [65], [3], 16),
+])
+def test_against_the_definition(dtype, dl, g, H, T, lens, drafts, pt):
+    d_r = 64 if dtype == "bf16" and dl in (64, 128, 256, 512) else 16
+    print("tree", dtype, dl, g, H, T, lens, drafts, pt, flush=True)
+    p = TreeProblem(lens, drafts, T, H=H, g=g, dl=dl, d_r=d_r, pt=pt, dtype=dtype, seed=dl + H + T)
+    assert_close(p, *run_all(p))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_empty_masks_and_drafts_that_do_not_exist(dtype):
+    lens, drafts, T = [0, 0, 70, 5], [3, 0, 4, 2], 4
+    masks = np.zeros((4, T), dtype=np.uint64)
+    masks[0] = [0, 2, 4, 0]                                  # draft 0 of an empty sequence sees nothing
+    masks[2] = [0, np.uint64(0xFFFFFFFFFFFFFFFF), 1, 8]      # bits beyond the drafts are ignored
+    masks[3] = [np.uint64(1) << np.uint64(63), 3, 3, 3]
+    p = TreeProblem(lens, drafts, T, masks=masks, dtype=dtype, seed=5)
+    o, lse = run_all(p)
+    assert_close(p, o, lse)
+    assert (o[:, 0, 0] == 0).all() and (lse[:, 0, 0] == -np.inf).all()
+    assert (o[:, 1] == 0).all() and (lse[:, 1] == -np.inf).all()
+    assert (o[:, 3, 2:] == 0).all() and (lse[:, 3, 2:] == -np.inf).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L", [0, 50, 64, 95])
+def test_what_a_masked_draft_holds_reaches_nobody_else(dtype, L):
+    T = 6
+    p = TreeProblem([L, 40], [T, T], T, masks=chain_masks(2, T), dtype=dtype, seed=7)
+    p.masks[0] = [1, 2, 5, 9, 17, 33]                        # draft 1 is seen by itself alone
+    clean = p.expected()
+    nan, inf = (np.float32("nan"), np.float32("inf")) if dtype == "f32" else (0x7FC0, 0x7F80)
+    page, off = p.row_of(0, L + 1)
+    for i in range(2):
+        p.pools[i][page, off, ::2] = nan
+        p.pools[i][page, off, 1::2] = inf
+    o, lse = run_all(p)
+    assert np.isnan(o[:, 0, 1]).all() and np.isnan(lse[:, 0, 1]).all()
+    o[:, 0, 1], lse[:, 0, 1] = clean[0][:, 0, 1], clean[1][:, 0, 1]
+    assert_close(p, o, lse, clean)
+
+
+def test_a_committed_row_that_is_not_a_number_is_seen_by_all_of_its_sequence():
+    p = TreeProblem([300, 40], [2, 2], 2, seed=8)
+    clean = p.expected()
+    page, off = p.row_of(0, 11)
+    p.pools[1][page, off, 3] = 0x7FC0
+    o, lse = run_all(p)
+    assert np.isnan(o[1, 0]).all() and np.isnan(lse[1, 0]).all()
+    o[1, 0], lse[1, 0] = clean[0][1, 0], clean[1][1, 0]
+    assert_close(p, o, lse, clean)
+
+
+def test_large_and_lowest_scores():
+    p = TreeProblem([200], [3], 3, seed=9)
+    p.q_lat = wl.to_storage(wl.as_f64(p.q_lat, "bf16") * 400.0, "bf16")    # a few tokens carry everything, the reference moves
+    assert_close(p, *run_all(p))
+
+
+def test_lengths_out_of_range_are_clipped():
+    T = 4
+    p = TreeProblem([120, 64], [4, 4], T, masks=chain_masks(2, T), seed=10)
+    d = p.device()
+    ref = p.expected()
+    d["drafts"] = torch.tensor([9, 4], dtype=torch.int32).cuda()         # more than T count as T
+    assert_close(p, *run_all(p, d), ref)
+    d["drafts"] = torch.tensor([-1, 4], dtype=torch.int32).cuda()
+    o, lse = run_all(p, d)
+    assert (o[:, 0] == 0).all() and (lse[:, 0] == -np.inf).all()
+    d["drafts"] = torch.tensor([4, 4], dtype=torch.int32).cuda()
+    d["lens"] = torch.tensor([-5, 64], dtype=torch.int32).cuda()         # fewer than none count as none
+    p.lens = [0, 64]
+    assert_close(p, *run_all(p, d))
+
+
+def test_drafts_beyond_the_table_row_are_not_seen():
+    T = 4
+    p = TreeProblem([124], [4], T, masks=chain_masks(1, T), seed=10)
+    assert p.max_pages * 64 == 128
+    d = p.device()
+    p.lens = [126]                                             # drafts 2 and 3 would be tokens 128 and 129
+    d["lens"] = torch.tensor([126], dtype=torch.int32).cuda()
+    assert_close(p, *run_all(p, d))
+    p.lens, p.drafts = [128], [4]
+    d["lens"] = torch.tensor([500], dtype=torch.int32).cuda()  # clipped to the row; no draft is seen
+    assert_close(p, *run_all(p, d))
+
+
+def test_no_draft_lengths_means_all():
+    p = TreeProblem([100, 7], [5, 5], 5, seed=11)
+    assert_close(p, *run_all(p, drafts=None))
+
+
+@pytest.mark.parametrize("H,T,lens", [(16, 2, [9000, 40, 3000]), (64, 4, [5003, 1200]), (64, 16, [700, 3000]), (16, 1, [20000])])
+def test_long_contexts_are_cut_and_joined(H, T, lens):
+    p = TreeProblem(lens, [T] * len(lens), T, H=H, g=1, seed=12)
+    assert_close(p, *run_all(p))
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    p = TreeProblem([3000, 77, 512], [6, 2, 5], 6, H=32, seed=13)
+    d = p.device()
+    a = run_all(p, d)
+    b = run_all(p, d)
+    o, lse = out_buffers(p)
+    ws, n = workspace(p)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        tp.tpla_decode_shards_tree(p.shape, p.T, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"], d["drafts"],
+                                   d["masks"], ws, n, o, lse)
+    side.synchronize()
+    for x, y, z in zip(a, b, (o, lse)):
+        assert np.array_equal(x, y) and np.array_equal(x, z.cpu().numpy().astype(np.float64))
+
+
+def test_one_slice_is_that_slice():
+    p = TreeProblem([400, 90], [5, 3], 5, H=64, g=4, dl=128, seed=14)
+    d = p.device()
+    ref = p.expected()
+    ws, n = workspace(p)
+    for i in range(4):
+        o, lse = out_buffers(p)
+        tp.tpla_decode_shard_tree(p.shape, p.T, d["q_lat"][i], d["q_pe"], d["pools"][i], d["bt"], p.max_pages, d["lens"], d["drafts"],
+                                  d["masks"], ws, n, o[i], lse[i])
+        torch.cuda.synchronize()
+        both = o.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+        for k in range(2):
+            both[k][[j for j in range(4) if j != i]] = ref[k][[j for j in range(4) if j != i]]
+        assert_close(p, *both, ref)
+
+
+def test_one_draft_that_sees_itself_is_the_decode_of_a_sequence_one_longer():
+    p = TreeProblem([640, 63], [1, 1], 1, H=64, masks=[[1], [1]], seed=15)
+    d = p.device()
+    o, lse = run_all(p, d)
+    o2, lse2 = out_buffers(p)
+    n = tp.tpla_workspace_bytes_all(p.shape, p.max_pages, 0)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    tp.tpla_decode_shards(p.shape, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"] + 1, 0, ws, n, o2, lse2)
+    torch.cuda.synchronize()
+    _, _, o_off, lse_off = p.expected()
+    assert (np.abs(o - o2.cpu().numpy()) <= 2 * o_off).all()          # both round their weights to bf16
+    # (the sum of the decode kernel is that of its rounded weights)
+    assert (np.abs(lse - lse2.cpu().numpy()) <= 2 * lse_off + 2.0 ** -8).all()
+
+
+def test_pools_beyond_32_bit_offsets():
+    """Pages behind 4 GiB and 2^31 elements; only the pages in use are written."""
+    p = TreeProblem([100, 30], [4, 4], 4, H=16, g=1, spare_pages=0, seed=16)
+    d = p.device()
+    used = p.pools[0].shape[0]
+    n_pool = 120000                                            # 64 x 320 elements each: 2.46e9 elements, 4.9 GB
+    big = torch.empty((n_pool, 64, 320), dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([n_pool - 1 - 7001 * k for k in range(used)])
+    assert int(ids.min()) >= 0
+    for k in range(used):
+        big[int(ids[k])] = d["pools"][0][k]
+    p.bt = ids.numpy().astype(np.int32)[np.minimum(p.bt, used - 1)]
+    d["pools"], d["bt"] = [big], torch.from_numpy(p.bt).cuda()
+    o, lse = out_buffers(p)
+    ws, n = workspace(p)
+    tp.tpla_decode_shards_tree(p.shape, p.T, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"], d["drafts"], d["masks"],
+                               ws, n, o, lse)
+    torch.cuda.synchronize()
+    back = {int(v): k for k, v in enumerate(ids)}
+    p.bt = np.vectorize(lambda v: back[int(v)])(p.bt).astype(np.int32)
+    assert_close(p, o.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64))
+
+
+def test_captured_into_a_graph():
+    p = TreeProblem([2100, 65], [4, 3], 4, H=64, seed=17)
+    q = TreeProblem([900, 33], [2, 4], 4, H=64, seed=18, max_pages=p.max_pages)
+    d, e = p.device(), q.device()
+    want_p, want_q = run_all(p, d), run_all(q, e)
+    o, lse = out_buffers(p)
+    ws, n = workspace(p)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tp.tpla_decode_shards_tree(p.shape, p.T, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"], d["drafts"],
+                                   d["masks"], ws, n, o, lse)
+    keep = {k: d[k].clone() for k in ("q_lat", "q_pe", "lens", "drafts", "masks")}
+    for it in range(4):
+        o.fill_(float("nan"))
+        if it % 2:                                             # same lengths' table, other queries, lengths and masks
+            d["lens"].copy_(keep["lens"] // 2)
+        else:
+            d["lens"].copy_(keep["lens"])
+        graph.replay()
+        torch.cuda.synchronize()
+        if it % 2 == 0:
+            assert np.array_equal(o.cpu().numpy(), want_p[0].astype(np.float32)) and np.array_equal(lse.cpu().numpy(), want_p[1].astype(np.float32))
+        else:
+            h = TreeProblem([2100, 65], [4, 3], 4, H=64, seed=17)
+            h.lens = [v // 2 for v in h.lens]
+            assert_close(h, o.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64))
+    again = run_all(q, e)
+    assert all(np.array_equal(x, y) for x, y in zip(again, want_q))
