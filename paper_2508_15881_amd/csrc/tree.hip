@@ -123,14 +123,30 @@ int launch_tree_generic(const TreeArgs& a, int dtype, hipStream_t st) {
   return check_launch("tree_generic_kernel");
 }
 
-// A wave per row: the references and sums of all its slots first, then their rows, in ascending order.  Rows of drafts that do
-// not exist get zeros and -inf here.  grid: (groups of 16 rows of a (slice, sequence), (slice, sequence)).
+// Merge: a workgroup takes 8 rows of one item, a wave two of them one after the other.  Per row the lanes hold the references and
+// weights of 64 slots at a time, and the slots' rows are added in ascending order, MERGE_LOADS on their way together (each is a round trip
+// to memory).  Rows of drafts that do not exist get zeros and -inf here.  grid: (groups of 8 rows of a (slice, sequence), (slice, sequence)).
+constexpr int MERGE_ROWS = 8, MERGE_LOADS = 8;
 __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a) {
-  const int v = blockIdx.y, b = v % a.B, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const TreeLens len = tree_lens(a, b);
-  const int all_rows = a.T * a.H, rows = len.n * a.H;
-  for (int e = 0; e < 4; ++e) {
-    const int r = blockIdx.x * 16 + 4 * e + wave;
+  const int v = blockIdx.y, b = v % a.B, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int all_rows = a.T * a.H, r0 = blockIdx.x * MERGE_ROWS;
+  const int item = v * a.p.blocks + r0 / a.p.block;             // whole groups of 8 lie in one
+  int first, next, step, n;
+  if (a.p.mfma) {
+    const int w0 = a.plan[3 * item];                            // (of an item without rows: whatever lies there, not used)
+    n = a.plan[3 * item + 1];
+    first = 2 * w0 + a.plan[3 * item + 2];
+    next = 2 * (w0 + 1);
+    step = 2;
+  } else {
+    first = item * a.p.n_splits;
+    next = first + 1;
+    step = 1;
+    n = a.p.n_splits;
+  }
+  const int rows = tree_lens(a, b).n * a.H;
+  for (int e = wave; e < MERGE_ROWS; e += 4) {
+    const int r = r0 + e;
     if (r >= all_rows) break;
     float* out = a.o_lat + ((size_t)v * all_rows + r) * a.dl;
     if (r >= rows) {
@@ -138,46 +154,39 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a) {
       if (a.lse && lane == 0) a.lse[(size_t)v * all_rows + r] = -INFINITY;
       continue;
     }
-    const int item = v * a.p.blocks + r / a.p.block;
-    int first, next, step, n;
-    if (a.p.mfma) {
-      const int w0 = a.plan[3 * item];
-      n = a.plan[3 * item + 1];
-      if (n == 1) continue;                         // written by the workgroup that had it whole
-      first = 2 * w0 + a.plan[3 * item + 2];
-      next = 2 * (w0 + 1);
-      step = 2;
-    } else {
-      first = item * a.p.n_splits;
-      next = first + 1;
-      step = 1;
-      n = a.p.n_splits;
-    }
-    auto slot = [&](int s) { return (size_t)(s == 0 ? first : next + (s - 1) * step) * a.p.block + r % a.p.block; };
-    float M = -INFINITY;
+    if (n == 1 && a.p.mfma) continue;                           // written by the workgroup that had it whole
+    const size_t local = r % a.p.block;
+    auto slot = [&](int s) { return (size_t)(s == 0 ? first : next + (s - 1) * step) * a.p.block + local; };
+    float M = -INFINITY, l = 0.f;
     for (int s0 = 0; s0 < n; s0 += 64) M = fmaxf(M, wave_max(s0 + lane < n ? a.part_ml[2 * slot(s0 + lane)] : -INFINITY));
     const float ref = M == -INFINITY ? 0.f : M;
-    float l = 0.f;
-    for (int s0 = 0; s0 < n; s0 += 64) {
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (s0 + lane < n) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot(s0 + lane));
-      l += wave_sum(ml.y * exp2f(ml.x - ref));
-    }
-    const float inv = l != 0.f ? 1.0f / l : 0.f;
-    for (int c = 4 * lane; c < a.dl; c += 256) {
+    for (int c0 = 0; c0 < a.dl; c0 += 256) {
+      const int c = min(c0 + 4 * lane, a.dl - 4);
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < n; ++s) {
-        const float w = exp2f(a.part_ml[2 * slot(s)] - ref);
-        x += *reinterpret_cast<const f32x4*>(a.part_acc + slot(s) * a.dl + c) * w;
+      for (int s0 = 0; s0 < n; s0 += 64) {
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (s0 + lane < n) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot(s0 + lane));
+        const float w = exp2f(ml.x - ref);
+        if (c0 == 0) l += wave_sum(ml.y * w);
+        const int here = min(64, n - s0);
+        for (int s = 0; s < here; s += MERGE_LOADS) {
+          f32x4 p[MERGE_LOADS];
+#pragma unroll
+          for (int k = 0; k < MERGE_LOADS; ++k) p[k] = *reinterpret_cast<const f32x4*>(a.part_acc + slot(s0 + min(s + k, here - 1)) * a.dl + c);
+#pragma unroll
+          for (int k = 0; k < MERGE_LOADS; ++k)
+            if (s + k < here) x += p[k] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s + k));
+        }
       }
-      *reinterpret_cast<f32x4*>(out + c) = x * inv;
+      const float inv = l != 0.f ? 1.0f / l : 0.f;
+      if (c0 + 4 * lane < a.dl) *reinterpret_cast<f32x4*>(out + c) = x * inv;
     }
     if (a.lse && lane == 0) a.lse[(size_t)v * all_rows + r] = merge_lse(M, l);
   }
 }
 
 int launch_tree_merge(const TreeArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((a.T * a.H + 15) / 16), (unsigned)(a.n_shards * a.B)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((a.T * a.H + MERGE_ROWS - 1) / MERGE_ROWS), (unsigned)(a.n_shards * a.B)), dim3(256), 0, st, a);
   return check_launch("tree_merge_kernel");
 }
 

@@ -11,6 +11,8 @@
 // an item that lies in one range is written at once, the others leave partial results for the merge (tree.hip).
 #include "lds_tile.h"
 
+#include <float.h>
+
 #include <algorithm>
 
 namespace tpla {
@@ -23,15 +25,42 @@ constexpr int TR_NW = 4;
 // first of them is read (the wait for the tile after the request covers them).
 constexpr int TR_IDS = 256, TR_ID_RING = 4 * TR_IDS;
 
-template <int DL>
+// QL: every second k-step, the first QL of them, of the queries lies in LDS and not in registers.
+template <int DL, int RB, int QL>
 struct TreeTile {
   static constexpr int RC = (DL + 64) / 8;             // 16-byte pieces per row
   static constexpr int BYTES = TR_TOK * RC * 16;
   static constexpr int CPT = TR_TOK * RC / 64 / TR_NW;  // direct-to-LDS loads per wave and tile
-  // Tiles in flight or in use; at most 8 (see TR_IDS).
-  static constexpr int NSTAGE = 150 * 1024 / BYTES < 8 ? 150 * 1024 / BYTES : 8;
-  static constexpr int LDS = NSTAGE * BYTES + TR_ID_RING * 4;
+  static constexpr int Q_BYTES = TR_NW * RB * QL * 1024;
+  static constexpr int FIT = (158 * 1024 - Q_BYTES - TR_ID_RING * 4) / BYTES;
+  static constexpr int NSTAGE = FIT < 8 ? FIT : 8;      // tiles in flight or in use; at most 8 (see TR_IDS)
+  static constexpr int IDS = NSTAGE * BYTES, Q = IDS + TR_ID_RING * 4, LDS = Q + Q_BYTES;
   static_assert(TR_TOK * RC % (64 * TR_NW) == 0, "every wave issues the same number of loads");
+  static_assert(NSTAGE >= 4, "a tile whose values are read, two whose scores are, and one on its way");
+};
+
+// LDS reads of the score product, in program order: K fragments x = 2 ks + tb, KRING of them ahead; the queries of an LDS
+// k-step at the first fragment of the k-step before; V fragments (two reads each) in place of the last KRING K fragments.
+// How many reads are younger than what fragment x needs when it is waited for (LDS answers in order).
+template <int KS, int QL, int RB, int KRING>
+struct ScoreReads {
+  static constexpr int NQ = 2 * KS;
+  static constexpr bool in_lds(int ks) { return ks < KS && (ks & 1) && ks / 2 < QL; }
+  static constexpr int in_regs(int ks) { return ks - (ks / 2 < QL ? ks / 2 : QL); }       // index among the k-steps in registers
+  static constexpr int q_reads(int x) { return x % 2 == 0 && in_lds(x / 2 + 1) ? RB : 0; }
+  static constexpr int tail_reads(int x, bool with_v) { return x + KRING < NQ ? 1 : (with_v ? 2 : 0); }
+  static constexpr int younger(int x, bool with_v) {
+    int issued = KRING, need = x < KRING ? x : -1;
+    for (int y = 0; y <= x; ++y) {
+      issued += q_reads(y);
+      if (x % 2 == 0 && in_lds(x / 2) && y == x - 2 && issued - 1 > need) need = issued - 1;   // the queries of this k-step
+      if (y < x) {
+        if (y + KRING == x && issued > need) need = issued;
+        issued += tail_reads(y, with_v);
+      }
+    }
+    return issued - need - 1;
+  }
 };
 
 __host__ __device__ __forceinline__ int tree_start(int n_wg, int units, int w) { return (int)((double)w * (double)units / (double)n_wg); }
@@ -51,32 +80,126 @@ __device__ __forceinline__ int tree_prefix(int v) {      // inclusive sum over t
   return v;
 }
 // Units (tiles) of sequence b: row blocks x tiles; none without drafts.
-__device__ __forceinline__ int tree_units(const TreeArgs& a, int b, int* tiles) {
-  if (b >= a.B) return *tiles = 0;
-  const TreeLens len = tree_lens(a, b);
-  *tiles = len.n > 0 ? max((len.keys + TR_TOK - 1) / TR_TOK, 1) : 0;
-  return *tiles * ((len.n * a.H + a.p.block - 1) / a.p.block);
+struct TreeUnits {
+  TreeLens len;
+  int tiles, units;
+};
+__device__ __forceinline__ TreeUnits tree_units(const TreeArgs& a, int b) {
+  TreeUnits r;
+  if (b >= a.B) {
+    r.len = TreeLens{0, 0, 0};
+    r.tiles = r.units = 0;
+    return r;
+  }
+  r.len = tree_lens(a, b);
+  r.tiles = r.len.n > 0 ? max((r.len.keys + TR_TOK - 1) / TR_TOK, 1) : 0;
+  r.units = r.tiles * ((r.len.n * a.H + a.p.block - 1) / a.p.block);
+  return r;
 }
 
-template <int DL, int RB>
+// ---- matrix instructions on registers of our choice ----
+// The output accumulators are the accumulation registers a0 .. themselves, quad N of them at a[4 N : 4 N + 3], and everything else
+// stays in the other 256.  Left to the compiler the accumulators exist twice (a branch may rescale them, and it copies them over for
+// every tile so that this branch finds them in ordinary registers): no room for 64 rows a wave.  So both products and what else touches
+// the accumulators are written out, with the wait states that the compiler then does not insert: 2 between an ordinary write and a
+// matrix instruction that reads it, 11 (here 18) between a matrix instruction and an ordinary one that reads its result.
+// acc_keep() stands at every step of the loop: nothing of the compiler's may live in these registers across it.  That it puts nothing
+// there in between either is checked on the assembly (tests/test_isa_tree_waits.py).
+#define TR_ACC_REGS \
+  "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", "a10", "a11", "a12", "a13", "a14", "a15", "a16", "a17", "a18", "a19", "a20", "a21", "a22", \
+  "a23", "a24", "a25", "a26", "a27", "a28", "a29", "a30", "a31", "a32", "a33", "a34", "a35", "a36", "a37", "a38", "a39", "a40", "a41", "a42", "a43", \
+  "a44", "a45", "a46", "a47", "a48", "a49", "a50", "a51", "a52", "a53", "a54", "a55", "a56", "a57", "a58", "a59", "a60", "a61", "a62", "a63", "a64", \
+  "a65", "a66", "a67", "a68", "a69", "a70", "a71", "a72", "a73", "a74", "a75", "a76", "a77", "a78", "a79", "a80", "a81", "a82", "a83", "a84", "a85", \
+  "a86", "a87", "a88", "a89", "a90", "a91", "a92", "a93", "a94", "a95", "a96", "a97", "a98", "a99", "a100", "a101", "a102", "a103", "a104", "a105", \
+  "a106", "a107", "a108", "a109", "a110", "a111", "a112", "a113", "a114", "a115", "a116", "a117", "a118", "a119", "a120", "a121", "a122", "a123", \
+  "a124", "a125", "a126", "a127", "a128", "a129", "a130", "a131", "a132", "a133", "a134", "a135", "a136", "a137", "a138", "a139", "a140", "a141", \
+  "a142", "a143", "a144", "a145", "a146", "a147", "a148", "a149", "a150", "a151", "a152", "a153", "a154", "a155", "a156", "a157", "a158", "a159", \
+  "a160", "a161", "a162", "a163", "a164", "a165", "a166", "a167", "a168", "a169", "a170", "a171", "a172", "a173", "a174", "a175", "a176", "a177", \
+  "a178", "a179", "a180", "a181", "a182", "a183", "a184", "a185", "a186", "a187", "a188", "a189", "a190", "a191", "a192", "a193", "a194", "a195", \
+  "a196", "a197", "a198", "a199", "a200", "a201", "a202", "a203", "a204", "a205", "a206", "a207", "a208", "a209", "a210", "a211", "a212", "a213", \
+  "a214", "a215", "a216", "a217", "a218", "a219", "a220", "a221", "a222", "a223", "a224", "a225", "a226", "a227", "a228", "a229", "a230", "a231", \
+  "a232", "a233", "a234", "a235", "a236", "a237", "a238", "a239", "a240", "a241", "a242", "a243", "a244", "a245", "a246", "a247", "a248", "a249", \
+  "a250", "a251", "a252", "a253", "a254", "a255"
+__device__ __forceinline__ void acc_keep() {
+#ifdef __HIP_DEVICE_COMPILE__                         // (the host's compiler does not know the names)
+  asm volatile("" : : : TR_ACC_REGS);
+#endif
+}
+__device__ __forceinline__ void mm_first(f32x4& s, const bf16x8& k, const bf16x8& q) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+}
+__device__ __forceinline__ void mm_score(f32x4& s, const bf16x8& k, const bf16x8& q) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+}
+template <int N>
+__device__ __forceinline__ void mm_out(const u32x4& v, const bf16x8& p) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 a[%2:%3], %0, %1, a[%2:%3]" : : "v"(v), "v"(p), "n"(4 * N), "n"(4 * N + 3));
+}
+__device__ __forceinline__ void mm_settle_write() { asm volatile("s_nop 1" ::: "memory"); }
+__device__ __forceinline__ void mm_settle_result() { asm volatile("s_nop 15\n\ts_nop 1" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void acc_zero() {
+  asm volatile("v_accvgpr_write_b32 a[%0], 0\n\tv_accvgpr_write_b32 a[%1], 0\n\tv_accvgpr_write_b32 a[%2], 0\n\tv_accvgpr_write_b32 a[%3], 0"
+               : : "n"(4 * N), "n"(4 * N + 1), "n"(4 * N + 2), "n"(4 * N + 3));
+}
+template <int A>
+__device__ __forceinline__ float acc_read_one() {
+  float x;
+  asm volatile("v_accvgpr_read_b32 %0, a[%1]" : "=v"(x) : "n"(A));
+  return x;
+}
+template <int N>
+__device__ __forceinline__ f32x4 acc_read() {
+  const float x = acc_read_one<4 * N>(), y = acc_read_one<4 * N + 1>(), z = acc_read_one<4 * N + 2>(), w = acc_read_one<4 * N + 3>();
+  return f32x4{x, y, z, w};
+}
+template <int A>
+__device__ __forceinline__ void acc_scale_one(float by) {
+  float t;
+  asm volatile("v_accvgpr_read_b32 %0, a[%2]\n\tv_mul_f32 %0, %0, %1\n\tv_accvgpr_write_b32 a[%2], %0" : "=&v"(t) : "v"(by), "n"(A));
+}
+template <int N>
+__device__ __forceinline__ void acc_scale(float by) {
+  acc_scale_one<4 * N>(by);
+  acc_scale_one<4 * N + 1>(by);
+  acc_scale_one<4 * N + 2>(by);
+  acc_scale_one<4 * N + 3>(by);
+}
+
+__device__ __forceinline__ unsigned lds_read_id(unsigned addr) {
+  unsigned id;
+  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(id) : "v"(addr) : "memory");
+  return id;
+}
+
+// The value, made known here: what is computed from it on a rare path is not computed ahead of the loop and kept.
+template <typename T>
+__device__ __forceinline__ T here(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+template <int DL, int RB, int QL>
 __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
-  using Tile = TreeTile<DL>;
+  using Tile = TreeTile<DL, RB, QL>;
   constexpr int RC = Tile::RC, CPT = Tile::CPT, NSTAGE = Tile::NSTAGE;
-  constexpr int KS = (DL + 64) / 32, DB = DL / 16;
-  constexpr int KRING = 8, VRING = 4;
+  constexpr int KS = (DL + 64) / 32, DB = DL / 16, NQ = 2 * KS;
+  constexpr int RING = 4;                              // K and V fragments on their way
+  constexpr int PAIRS = RB * 4;                        // pairs of weights per lane and tile
+  using Reads = ScoreReads<KS, QL, RB, RING>;
   extern __shared__ u32x4 smem[];
-  const unsigned lds_base = lds_at(reinterpret_cast<const char*>(smem));
-  const unsigned lds_ids = lds_base + NSTAGE * Tile::BYTES;
+  char* const lds = reinterpret_cast<char*>(smem);
+  const unsigned lds_base = lds_at(lds);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, q4 = lane >> 4;
 
   // ---- this workgroup's range of units ----
-  int per_slice = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int tiles;
-    per_slice += __builtin_amdgcn_readlane(tree_prefix(tree_units(a, b0 + lane, &tiles)), 63);
-  }
+  // (the first 64 sequences stay in the lanes: a search among them loads nothing)
+  const TreeUnits front = tree_units(a, lane);
+  const int front_incl = tree_prefix(front.units);
+  int per_slice = __builtin_amdgcn_readlane(front_incl, 63);
+  for (int b0 = 64; b0 < a.B; b0 += 64) per_slice += __builtin_amdgcn_readlane(tree_prefix(tree_units(a, b0 + lane).units), 63);
   const int units = per_slice * a.n_shards;
   const int n_wg = max(1, min(a.p.n_wg, units / a.p.split_tokens));     // no shorter ranges than pay
   const int w = n_wg % 8 == 0 ? (blockIdx.x & 7) * (n_wg >> 3) + (blockIdx.x >> 3) : blockIdx.x;
@@ -84,47 +207,42 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   int pos = tree_start(n_wg, units, w);
   const int range0 = pos, end = tree_start(n_wg, units, w + 1);
 
-  // ---- per-lane LDS offsets (as in the prefill kernel) ----
-  const int xk = swz(j16);
-  unsigned k_off[2];
-  k_off[0] = (unsigned)((j16 * RC + (q4 ^ xk)) * 16);
-  k_off[1] = (unsigned)((j16 * RC + ((4 | q4) ^ xk)) * 16);
-  const int v_tok = 4 * q4 + (j16 >> 2), xv = swz(v_tok), cb = (j16 & 3) >> 1;
-  unsigned v_off[4];
-#pragma unroll
-  for (int d = 0; d < 4; ++d) v_off[d] = (unsigned)((v_tok * RC + (((d << 1) | cb) ^ xv)) * 16 + (j16 & 1) * 8);
-  int ld_tok[CPT], ld_byte[CPT];
+  // ---- per-lane LDS offsets: rows begin at whole 128 bytes, so that the pieces of a row differ in address bits 4 to 6 alone ----
+  static_assert(RC % 8 == 0, "rows of whole 128 bytes");
+  const unsigned k_off = (unsigned)((j16 * RC + (q4 ^ swz(j16))) * 16);
+  const int v_tok = 4 * q4 + (j16 >> 2);
+  const unsigned v_off = (unsigned)((v_tok * RC + (((j16 & 3) >> 1) ^ swz(v_tok))) * 16 + (j16 & 1) * 8);
+  const unsigned lds_q = lds_base + Tile::Q + wave * (RB * QL * 1024) + lane * 16;
+  unsigned ld_at[CPT];                                 // byte of this lane's piece within a page that holds the tile's 32 rows
 #pragma unroll
   for (int j = 0; j < CPT; ++j) {
-    const int x = (wave + j * TR_NW) * 64 + lane;
-    ld_tok[j] = x / RC;
-    ld_byte[j] = ((x % RC) ^ swz(ld_tok[j])) * 16;
+    const int x = (wave + j * TR_NW) * 64 + lane, tok = x / RC;
+    ld_at[j] = (unsigned)(tok * (RC * 16) + ((x % RC) ^ swz(tok)) * 16);
   }
   const int pt = a.page_tokens, shift = (pt & (pt - 1)) == 0 ? __builtin_ctz(pt) : -1;
   auto page_of = [&](int t) { return shift >= 0 ? t >> shift : t / pt; };
+  const bool one_page = pt % TR_TOK == 0;              // a tile never crosses a page
 
   while (pos < end) {
     // ---- the item of unit `pos` ----
     const int i = pos / per_slice, rem = pos - i * per_slice;
-    int b = 0, before = 0, tiles = 1;
-    for (int b0 = 0, base = 0; b0 < a.B; b0 += 64) {
-      int t_b;
-      const int u = tree_units(a, b0 + lane, &t_b), incl = tree_prefix(u) + base;
-      const unsigned long long past = __ballot(incl > rem);
-      if (past) {
-        const int src = __builtin_ctzll(past);
-        b = b0 + src;
-        before = __builtin_amdgcn_readlane(incl - u, src);
-        tiles = __builtin_amdgcn_readlane(t_b, src);
-        break;
-      }
-      base = __builtin_amdgcn_readlane(incl, 63);
+    int b = 0, before = 0;
+    TreeUnits u = front;
+    int incl = front_incl;
+    unsigned long long past = __ballot(incl > rem);
+    while (past == 0) {                              // ends: rem lies below the sum over all sequences
+      b += 64;
+      const int base = __builtin_amdgcn_readlane(incl, 63);
+      u = tree_units(a, b + lane);
+      incl = tree_prefix(u.units) + base;
+      past = __ballot(incl > rem);
     }
-    b = __builtin_amdgcn_readfirstlane(b);
+    const int src = __builtin_ctzll(past);
+    b += src;
+    before = __builtin_amdgcn_readlane(incl - u.units, src);
+    const int tiles = __builtin_amdgcn_readlane(u.tiles, src), L = __builtin_amdgcn_readlane(u.len.L, src);
+    const int keys = __builtin_amdgcn_readlane(u.len.keys, src), rows = __builtin_amdgcn_readlane(u.len.n, src) * a.H;
     const int rb = (rem - before) / tiles, t0 = rem - before - rb * tiles, t1 = min(tiles, t0 + (end - pos));
-    const TreeLens len = tree_lens(a, b);
-    const int L = __builtin_amdgcn_readfirstlane(len.L), keys = __builtin_amdgcn_readfirstlane(len.keys);
-    const int rows = __builtin_amdgcn_readfirstlane(len.n) * a.H;
     const int v = i * a.B + b, item = v * a.p.blocks + rb;
     const int row0 = rb * a.p.block + wave * (16 * RB);          // this wave's first row
     const bool alive = row0 < rows;
@@ -138,26 +256,32 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
     auto request_ids = [&](int c) {
       const int p = min(c * TR_IDS + wave * 64 + lane, a.max_pages - 1);
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(table + p),
-                                       (__attribute__((address_space(3))) void*)(reinterpret_cast<char*>(smem) + NSTAGE * Tile::BYTES +
-                                                                                 ((c & 3) * TR_IDS + wave * 64) * 4), 4, 0, 0);
+                                       (__attribute__((address_space(3))) void*)(lds + Tile::IDS + ((c & 3) * TR_IDS + wave * 64) * 4), 4, 0, 0);
     };
-    auto issue = [&](int t) {
-      const int c = __builtin_amdgcn_readfirstlane(page_of(t * TR_TOK)) / TR_IDS;
-      int page[CPT], off[CPT];
+    auto id_at = [&](int p) { return lds_base + Tile::IDS + (unsigned)(p & (TR_ID_RING - 1)) * 4; };
+    auto id_of = [&](int t) { return id_at(page_of(t * TR_TOK)); };
+    auto issue = [&](int t, unsigned id) {           // id: page of the tile, where tiles do not cross pages
+      const int k0 = t * TR_TOK, p0 = __builtin_amdgcn_readfirstlane(page_of(k0));
+      char* dst = lds + (t % NSTAGE) * Tile::BYTES + wave * 1024;
+      if (one_page && k0 + TR_TOK <= keys) {
+        const int page = __builtin_amdgcn_readfirstlane(id);
+        const char* src = pool + ((size_t)page * pt + (k0 - p0 * pt)) * (RC * 16);
 #pragma unroll
-      for (int j = 0; j < CPT; ++j) {
-        const int k = min(t * TR_TOK + ld_tok[j], keys - 1), p = page_of(k);
-        off[j] = k - p * pt;
-        const unsigned at = lds_ids + (unsigned)(p & (TR_ID_RING - 1)) * 4;
-        asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(page[j]) : "v"(at) : "memory");
+        for (int j = 0; j < CPT; ++j)
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + ld_at[j]),
+                                           (__attribute__((address_space(3))) void*)(dst + j * TR_NW * 1024), 16, 0, 0);
+      } else {
+        // rows of several pages, or past the end: those repeat the last token (and are masked)
+#pragma unroll 1
+        for (int j = 0; j < CPT; ++j) {
+          const int x = (wave + j * TR_NW) * 64 + here(lane), tok = x / RC, k = min(k0 + tok, keys - 1), p = page_of(k);
+          const int row_id = (int)lds_read_id(id_at(p));
+          const char* src = pool + ((size_t)row_id * pt + (k - p * pt)) * (RC * 16) + ((x % RC) ^ swz(tok)) * 16;
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                           (__attribute__((address_space(3))) void*)(dst + j * TR_NW * 1024), 16, 0, 0);
+        }
       }
-      char* dst = reinterpret_cast<char*>(smem) + (t % NSTAGE) * Tile::BYTES;
-#pragma unroll
-      for (int j = 0; j < CPT; ++j) {
-        const char* src = pool + ((size_t)page[j] * pt + off[j]) * (RC * 16) + ld_byte[j];
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                         (__attribute__((address_space(3))) void*)(dst + (wave + j * TR_NW) * 1024), 16, 0, 0);
-      }
+      const int c = p0 / TR_IDS;
       if (c != chunk) {
         chunk = c;
         request_ids(c + 1);
@@ -168,162 +292,46 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
     request_ids(chunk + 1);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __builtin_amdgcn_s_barrier();
-    for (int t = t0; t < t1 && t < t0 + NSTAGE - 1; ++t) issue(t);
+    for (int t = t0; t < t1 && t < t0 + NSTAGE - 1; ++t) issue(t, lds_read_id(id_of(t)));
 
-    // ---- queries as B operands: block r, lane holds row row0 + 16 r + j16 ----
-    bf16x8 q[RB][KS];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      const int row = min(row0 + 16 * r + j16, rows - 1);
-      const bf16_t* ql = static_cast<const bf16_t*>(a.q_lat) + ((size_t)v * all_rows + row) * DL;
-      const bf16_t* qp = static_cast<const bf16_t*>(a.q_pe) + ((size_t)b * all_rows + row) * 64;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int k0 = ks * 32 + q4 * 8;
-        q[r][ks] = *reinterpret_cast<const bf16x8*>(ks * 32 < DL ? ql + k0 : qp + (k0 - DL));
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[r][ks]));   // complete before the loop
-
-    f32x4 acc[RB][DB];
-    float m_run[RB], l_run[RB];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      m_run[r] = -INFINITY;
-      l_run[r] = 0.f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    for (int t = t0; t < t1; ++t) {
+    // In the middle of the values of tile t: tile t + 2 is there for all waves, tile t - 1 is no longer read by any and another takes its place.
+    auto arrived = [&](int t) {
       if (t + NSTAGE - 2 < t1)
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm((NSTAGE - 2) * CPT));
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm((NSTAGE - 4) * CPT));
       else
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      __builtin_amdgcn_s_barrier();                  // tile t visible to all waves, tile t - 1 no longer read
-      if (t + NSTAGE - 1 < t1) issue(t + NSTAGE - 1);
-      const unsigned tile = lds_base + (unsigned)((t % NSTAGE) * Tile::BYTES);
-      const bool tail = (t + 1) * TR_TOK > L;        // drafts, or past the end
-
-      f32x4 s[RB][2];
-      if (alive) {
+      __builtin_amdgcn_s_barrier();
+    };
+    auto refill = [&](int t, unsigned id) {
+      if (t + NSTAGE - 1 < t1) issue(t + NSTAGE - 1, id);
+    };
+    // Values of drafts are masked per row, and a weight of zero does not silence an infinity or a NaN: what is not finite in tile t becomes
+    // zero here, behind its scores and ahead of the product with its weights.  A row that sees such a draft has it in its score already.
+    auto clean = [&](int t) {
+      lds_barrier();
+#pragma unroll 1
+      for (int x = here(tid); x < TR_TOK * RC; x += TR_NW * 64) {
+        const int tok = x / RC, c = (x % RC) ^ swz(tok);
+        if (c >= DL / 8 || t * TR_TOK + tok < L) continue;
+        u32x4* at = smem + (t % NSTAGE) * (TR_TOK * RC) + x;
+        u32x4 u = *at;
 #pragma unroll
-        for (int r = 0; r < RB; ++r) s[r][0] = s[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-        constexpr int NQ = KS * 2;                   // K fragments, in order (ks, tb)
-        bf16x8 kf[KRING];
-        const unsigned ka[2] = {tile + k_off[0], tile + k_off[1]};
-        static_for<KRING>([&](auto ic) {
-          constexpr int x = decltype(ic)::value, ks = x / 2, tb = x % 2;
-          lds_read_b128<(ks >> 1) * 128 + tb * (16 * RC * 16)>(kf[x], ka[ks & 1]);
-        });
-        static_for<NQ>([&](auto ic) {
-          constexpr int x = decltype(ic)::value, ks = x / 2, tb = x % 2;
-          constexpr int ahead = (NQ - 1 - x) < KRING - 1 ? (NQ - 1 - x) : KRING - 1;
-          lds_wait<ahead>(kf[x % KRING]);
-#pragma unroll
-          for (int r = 0; r < RB; ++r) s[r][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x % KRING], q[r][ks], s[r][tb], 0, 0, 0);
-          if constexpr (x + KRING < NQ) {
-            constexpr int ks2 = (x + KRING) / 2, tb2 = (x + KRING) % 2;
-            lds_read_b128<(ks2 >> 1) * 128 + tb2 * (16 * RC * 16)>(kf[x % KRING], ka[ks2 & 1]);
-          }
-        });
+        for (int e = 0; e < 4; ++e) {
+          if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
+          if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+        }
+        *at = u;
       }
-      if (tail) {
-        // Values of drafts are masked per row, and a weight of zero does not silence an infinity or a NaN: what is not finite
-        // becomes zero here, behind the scores.  A row that sees such a draft has it in its score already.
-        lds_barrier();
-        for (int x = tid; x < TR_TOK * RC; x += TR_NW * 64) {
-          const int tok = x / RC, c = (x % RC) ^ swz(tok);
-          if (c >= DL / 8 || t * TR_TOK + tok < L) continue;
-          u32x4* at = smem + (t % NSTAGE) * (TR_TOK * RC) + x;
-          u32x4 u = *at;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
-            if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
-          }
-          *at = u;
-        }
-        lds_barrier();
-      }
-      if (!alive) continue;
+      lds_barrier();
+    };
+    auto first_tiles = [&]() {                       // tiles t0 and t0 + 1 are there
+      if (t0 + NSTAGE - 2 < t1)
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm((NSTAGE - 3) * CPT));
+      else
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      __builtin_amdgcn_s_barrier();
+    };
 
-      // the first V fragments start now: their LDS latency passes under the softmax arithmetic
-      u32x2 vlo[VRING], vhi[VRING];
-      unsigned va[4];
-#pragma unroll
-      for (int d = 0; d < 4; ++d) va[d] = tile + v_off[d];
-      static_for<VRING>([&](auto ic) {
-        constexpr int d = decltype(ic)::value;
-        lds_read_tr_b64<(d >> 2) * 128>(vlo[d], va[d & 3]);
-        lds_read_tr_b64<(d >> 2) * 128 + 16 * RC * 16>(vhi[d], va[d & 3]);
-      });
-
-      // ---- online softmax: lane = one row per block, tokens 32 t + 16 tb + 4 q4 + e ----
-      bf16x8 pb[RB];
-#pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        if (tail) {
-          const int row = min(row0 + 16 * r + j16, rows - 1);
-          const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H];
-#pragma unroll
-          for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int k = t * TR_TOK + 16 * tb + 4 * q4 + e, j = k - L;
-              if (j >= 0 && (k >= keys || !((bits >> (j & 63)) & 1))) s[r][tb][e] = -INFINITY;
-            }
-        }
-        float mx = s[r][0][0];
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[r][tb][e]);
-        mx *= a.scale_log2;
-        if (__any(mx > m_run[r] + LAZY)) {
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
-          const float m_new = fmaxf(m_run[r], mx);
-          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[r] - m_new);   // 0 the first time
-          l_run[r] *= alpha;
-          m_run[r] = m_new;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) acc[r][d] *= alpha;
-        }
-        const float ref = m_run[r] == -INFINITY ? 0.f : m_run[r];
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[r][tb][e], a.scale_log2, -ref));
-            l_run[r] += p;
-            // weights go into the second product in bf16, at most 2^-9 off each; their sum is that of the unrounded ones, so
-            // that lse has float accuracy
-            pb[r][4 * tb + e] = (bf16_t)p;
-          }
-      }
-
-      // ---- O^T += V^T P^T ----
-      static_for<DB>([&](auto ic) {
-        constexpr int d = decltype(ic)::value;
-        constexpr int ahead = (DB - 1 - d) < VRING - 1 ? (DB - 1 - d) : VRING - 1;
-        lds_wait<2 * ahead>(vlo[d % VRING], vhi[d % VRING]);
-        const u32x4 v4 = {vlo[d % VRING][0], vlo[d % VRING][1], vhi[d % VRING][0], vhi[d % VRING][1]};
-#pragma unroll
-        for (int r = 0; r < RB; ++r)
-          acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb[r], acc[r][d], 0, 0, 0);
-        if constexpr (d + VRING < DB) {
-          constexpr int d2 = d + VRING;
-          lds_read_tr_b64<(d2 >> 2) * 128>(vlo[d % VRING], va[d2 & 3]);
-          lds_read_tr_b64<(d2 >> 2) * 128 + 16 * RC * 16>(vhi[d % VRING], va[d2 & 3]);
-        }
-      });
-    }
-
-    // ---- the item's result, or a partial one ----
     const bool whole = t0 == 0 && t1 == tiles;
     const int slot = 2 * w + (pos == range0 ? 0 : 1);
     if (t0 == 0 && tid == 0) {
@@ -332,25 +340,247 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       a.plan[3 * item + 1] = last - w + 1;
       a.plan[3 * item + 2] = pos == range0 ? 0 : 1;
     }
+    pos += t1 - t0;
+    if (!alive) {                                    // no rows: this wave only loads
+      first_tiles();
+      for (int t = t0; t < t1; ++t) {
+        if ((t + 1) * TR_TOK > L) clean(t);
+        if (t == t1 - 1) break;
+        arrived(t);
+        refill(t, lds_read_id(id_of(t + NSTAGE - 1)));
+      }
+      continue;
+    }
+
+    // ---- queries as B operands: block r, lane holds row row0 + 16 r + j16 ----
+    bf16x8 q[RB][KS - QL];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-      const int local = wave * (16 * RB) + 16 * r + j16, row = row0 + 16 * r + j16;
+      const int row = min(row0 + 16 * r + j16, rows - 1);
+      const bf16_t* ql = static_cast<const bf16_t*>(a.q_lat) + ((size_t)v * all_rows + row) * DL + q4 * 8;
+      const bf16_t* qp = static_cast<const bf16_t*>(a.q_pe) + ((size_t)b * all_rows + row) * 64 + q4 * 8;
+      __builtin_amdgcn_sched_barrier(0);             // one block's addresses at a time
+      static_for<KS>([&](auto ic) {
+        constexpr int ks = decltype(ic)::value;
+        const bf16x8 x = *reinterpret_cast<const bf16x8*>(ks * 32 < DL ? ql + ks * 32 : qp + (ks * 32 - DL));
+        if constexpr (Reads::in_lds(ks))
+          *reinterpret_cast<bf16x8*>(lds + Tile::Q + ((wave * RB + r) * QL + ks / 2) * 1024 + lane * 16) = x;
+        else
+          q[r][Reads::in_regs(ks)] = x;
+      });
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));        // complete before the loop: nothing there waits for them
+    first_tiles();
+
+    f32x4 s[RB][2], next[RB][2];
+    // The reference starts at the lowest finite number: every finite score moves it, -inf keeps weight 0 against it.
+    float m_run[RB], l_run[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      m_run[r] = -FLT_MAX;
+      l_run[r] = 0.f;
+      next[r][0] = next[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    static_for<RB * DB>([](auto n) { acc_zero<decltype(n)::value>(); });
+    acc_keep();
+    u32x2 vlo[RING], vhi[RING];
+    auto read_v = [&](auto ic, unsigned va) {
+      constexpr int d = decltype(ic)::value;
+      lds_read_tr_b64<(d >> 2) * 128>(vlo[d % RING], va ^ ((d & 3) << 5));
+      lds_read_tr_b64<(d >> 2) * 128 + 16 * RC * 16>(vhi[d % RING], va ^ ((d & 3) << 5));
+    };
+    bf16x8 kf[RING];
+    auto read_k = [&](auto ic, unsigned ka) {
+      constexpr int x = decltype(ic)::value, ks = x / 2, tb = x % 2;
+      lds_read_b128<(ks >> 1) * 128 + tb * (16 * RC * 16)>(kf[x % RING], ka ^ ((ks & 1) << 6));
+    };
+    // Scores of a tile (at ka), whose first RING fragments are on their way; slice(x) runs behind fragment x.  with_v: the first V fragments
+    // (at va) follow the last K fragments.
+    auto scores = [&](unsigned ka, f32x4 (&s)[RB][2], auto with_v, unsigned va, auto&& slice) {
+      constexpr bool WV = decltype(with_v)::value;
+      bf16x8 qf[RB];
+      static_for<NQ>([&](auto ic) {
+        constexpr int x = decltype(ic)::value, ks = x / 2, tb = x % 2;
+        if constexpr (Reads::q_reads(x) > 0)
+          static_for<RB>([&](auto rc) {
+            constexpr int r = decltype(rc)::value;
+            lds_read_b128<(r * QL + (ks + 1) / 2) * 1024>(qf[r], lds_q);
+          });
+        lds_wait<Reads::younger(x, WV)>(kf[x % RING]);
+        if constexpr (Reads::in_lds(ks) && tb == 0)
+#pragma unroll
+          for (int r = 0; r < RB; ++r) lds_wait<Reads::younger(x, WV)>(qf[r]);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          if constexpr (ks == 0)
+            mm_first(s[r][tb], kf[x % RING], q[r][0]);
+          else if constexpr (Reads::in_lds(ks))
+            mm_score(s[r][tb], kf[x % RING], qf[r]);
+          else
+            mm_score(s[r][tb], kf[x % RING], q[r][Reads::in_regs(ks)]);
+        }
+        if constexpr (x + RING < NQ)
+          read_k(std::integral_constant<int, x + RING>{}, ka);
+        else if constexpr (WV)
+          read_v(std::integral_constant<int, x + RING - NQ>{}, va);
+        slice(ic);
+        acc_keep();
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    auto top_of = [&](const f32x4 (&s)[RB][2], int r) {
+      float m = fmaxf(s[r][0][0], s[r][0][1]);
+#pragma unroll
+      for (int e = 2; e < 8; ++e) m = fmaxf(m, s[r][e >> 2][e & 3]);
+      return m * a.scale_log2;
+    };
+    unsigned long long over = 0;                     // lanes with a score of the next tile far above their reference
+    auto look = [&](const f32x4 (&s)[RB][2], int r) { over |= __ballot(top_of(s, r) > m_run[r] + LAZY); };
+    auto tile_at = [&](int t) { return lds_base + (unsigned)((t % NSTAGE) * Tile::BYTES); };
+
+    // One tile: its scores are in s; the scores of the next one go into next under the exponentials of this one.
+    auto step = [&](int t, auto last_tile) {
+      constexpr bool LAST = decltype(last_tile)::value;
+      if ((t + 1) * TR_TOK > L) {                    // drafts, or past the end: masked here, and looked at again
+        over = 0;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          const int row = min(row0 + 16 * r + here(j16), rows - 1);
+          const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H];
+#pragma unroll
+          for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k = t * TR_TOK + 16 * tb + 4 * here(q4) + e, j = k - L;
+              if (j >= 0 && (k >= keys || !((bits >> (j & 63)) & 1))) s[r][tb][e] = -INFINITY;
+            }
+          look(s, r);
+        }
+        clean(t);
+      }
+      if (over) {
+        mm_settle_result();
+        static_for<RB>([&](auto rc) {
+          constexpr int r = decltype(rc)::value;
+          float m = top_of(s, r);
+          m = fmaxf(m, __shfl_xor(m, 16));
+          m = fmaxf(m, __shfl_xor(m, 32));
+          m = fmaxf(m, m_run[r]);
+          const float alpha = __builtin_amdgcn_exp2f(m_run[r] - m);
+          l_run[r] *= alpha;
+          m_run[r] = m;
+          static_for<DB>([&](auto d) { acc_scale<r * DB + decltype(d)::value>(alpha); });
+          acc_keep();
+        });
+        mm_settle_write();
+        over = 0;
+      }
+      // weights: lane = one row per block, tokens 32 t + 16 tb + 4 q4 + e.  They go into the second product in bf16, at most 2^-8
+      // off each; their sum is that of the unrounded ones, so that lse has float accuracy
+      bf16x8 pb[RB];
+      auto weights = [&](auto pc) {
+        constexpr int p = decltype(pc)::value, r = p / 4, tb = (p % 4) / 2, e = 2 * (p % 2);
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[r][tb][e], a.scale_log2, -m_run[r]));
+        const float y = __builtin_amdgcn_exp2f(fmaf(s[r][tb][e + 1], a.scale_log2, -m_run[r]));
+        l_run[r] += x + y;
+        pb[r][4 * tb + e] = (bf16_t)x;
+        pb[r][4 * tb + e + 1] = (bf16_t)y;
+        acc_keep();
+      };
+      const unsigned va = tile_at(t) + v_off;
+      if constexpr (!LAST) {
+        scores(tile_at(t + 1) + k_off, next, std::true_type{}, va, [&](auto ic) {
+          constexpr int x = decltype(ic)::value, p0 = x * PAIRS / NQ, p1 = (x + 1) * PAIRS / NQ;
+          static_for<p1 - p0>([&](auto k) { weights(std::integral_constant<int, p0 + decltype(k)::value>{}); });
+        });
+      } else {
+        static_for<RING>([&](auto ic) { lds_wait<0>(kf[decltype(ic)::value]); });     // (of no tile)
+        static_for<RING>([&](auto ic) { read_v(ic, va); });
+        static_for<PAIRS>(weights);
+      }
+
+      // O^T += V^T P^T; under it the next tile's maxima, the tile after that arrives, and its first K fragments (of whatever lies there behind the
+      // last tile) follow the last V fragments
+      const unsigned ka = tile_at(t + 2) + k_off;
+      unsigned id;
+      constexpr int middle = DB / 2 < DB - RING ? DB / 2 : DB - RING;
+      static_for<DB>([&](auto ic) {
+        constexpr int d = decltype(ic)::value, left = DB - 1 - d;
+        if constexpr (!LAST && d == middle) {
+          arrived(t);
+          asm volatile("ds_read_b32 %0, %1" : "=v"(id) : "v"(id_of(t + NSTAGE - 1)) : "memory");
+        }
+        lds_wait<2 * (left < RING - 1 ? left : RING - 1) + (!LAST && RING - 1 - left > 0 ? RING - 1 - left : 0)>(vlo[d % RING], vhi[d % RING]);
+        const u32x4 v4 = {vlo[d % RING][0], vlo[d % RING][1], vhi[d % RING][0], vhi[d % RING][1]};
+        if constexpr (d == 0) {
+#pragma unroll
+          for (int r = 0; r < RB; ++r) asm volatile("" : "+v"(pb[r]));      // written before the wait states
+          mm_settle_write();
+        }
+        static_for<RB>([&](auto r) { mm_out<decltype(r)::value * DB + d>(v4, pb[decltype(r)::value]); });
+        acc_keep();
+        if constexpr (d + RING < DB)
+          read_v(std::integral_constant<int, d + RING>{}, va);
+        else if constexpr (!LAST)
+          read_k(std::integral_constant<int, d + RING - DB>{}, ka);
+        if constexpr (!LAST && d == DB - 1) {                 // (the wait for the last V fragment covered the page id)
+          asm volatile("" : "+v"(id));
+          refill(t, id);
+        }
+        // the scores of the next tile are complete: 64 clocks of matrix instructions and more lie behind their last one
+        constexpr int from = DB - RB > 4 ? DB - RB : DB;
+        if constexpr (!LAST && d >= from) look(next, d - from);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (LAST) return;
+      if constexpr (DB - RB <= 4) {
+        mm_settle_result();
+#pragma unroll
+        for (int r = 0; r < RB; ++r) look(next, r);
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) s[r][tb] = next[r][tb];
+    };
+
+    {
+      static_for<RING>([&](auto ic) { read_k(ic, tile_at(t0) + k_off); });
+      scores(tile_at(t0) + k_off, s, std::false_type{}, 0u, [](auto) {});
+      static_for<RING>([&](auto ic) { read_k(ic, tile_at(t0 + 1) + k_off); });
+      mm_settle_result();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = 0; r < RB; ++r) look(s, r);
+    }
+#pragma unroll 1
+    for (int t = t0; t < t1 - 1; ++t) step(t, std::false_type{});
+    step(t1 - 1, std::true_type{});
+
+    // ---- the item's result, or a partial one ----
+    mm_settle_result();
+    static_for<RB>([&](auto rc) {
+      constexpr int r = decltype(rc)::value;
+      const int local = wave * (16 * RB) + 16 * r + here(j16), row = rb * a.p.block + local;
       float l = l_run[r];
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
-      if (!alive || row >= rows) continue;
+      const bool there = row < rows;
       const float inv = whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
       float* out = whole ? a.o_lat + ((size_t)v * all_rows + row) * DL : a.part_acc + ((size_t)slot * a.p.block + local) * DL;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(out + 16 * d + 4 * q4) = acc[r][d] * inv;
-      if (q4 == 0) {
+      static_for<DB>([&](auto dc) {
+        constexpr int d = decltype(dc)::value;
+        const f32x4 x = acc_read<r * DB + d>() * inv;
+        if (there) *reinterpret_cast<f32x4*>(out + 16 * d + 4 * q4) = x;
+      });
+      acc_keep();
+      if (there && q4 == 0) {
         if (!whole)
           *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)slot * a.p.block + local)) = make_float2(m_run[r], l);
         else if (a.lse)
           a.lse[(size_t)v * all_rows + row] = l != 0.f ? (m_run[r] + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
-    }
-    pos += t1 - t0;
+    });
   }
 }
 
@@ -359,14 +589,16 @@ bool tree_mfma_supported(const tpla_shape_t& sh) {
   return sh.dtype == TPLA_BF16 && sh.d_r == 64 && (dl == 64 || dl == 128 || dl == 256 || dl == 512);
 }
 
-// Blocks of 16 rows per wave.
+// Blocks of 16 rows per wave: the fewest tiles weighted by what one takes, 0.45 + 0.48 RB (16 sequences of 32768 tokens, 64 heads, us per tile and
+// workgroup: 1 block 0.91, 2 1.26, 3 1.74).  us by this number of blocks: 192 rows 294 / 232 / 199 (32 x 8192), 256 rows 145 / 128 / 151 (32 x 4096),
+// 512 rows 257 / 208 / 226 (16 x 8192), 1024 rows 1832 / 1335 / 1334 (16 x 32768).
 static int row_blocks(int dl, int rows) {
-  const int most = dl == 512 ? 1 : dl == 64 ? 4 : 2;
+  const int most = dl == 512 ? 1 : dl == 256 ? 3 : 4;
   int best = 1;
   double least = 1e30;
   for (int rb = 1; rb <= most; ++rb) {
-    if (rb == 3) continue;
-    const double t = (double)((rows + 64 * rb - 1) / (64 * rb)) * (1.0 + 0.35 * rb);
+    if (rb == 3 && dl != 256) continue;              // no such kernel
+    const double t = (double)((rows + 64 * rb - 1) / (64 * rb)) * (0.45 + 0.48 * rb);
     if (t < least) {
       least = t;
       best = rb;
@@ -384,15 +616,16 @@ void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, 
   const double most = (double)n_shards * sh.B * p->blocks * std::max(tiles, 1.0);
   p->n_wg = (int)std::min((double)device_cu_count(), most);
   p->n_splits = 1;
-  p->split_tokens = 8;         // fewest tiles of a range
+  p->split_tokens = 4;         // fewest tiles of a range
 }
 
-template <int DL, int RB>
+template <int DL, int RB, int QL = 0>
 static int launch_tree(const TreeArgs& a, hipStream_t st) {
-  const auto fn = tree_mfma_kernel<DL, RB>;
-  const int rc = allow_lds(reinterpret_cast<const void*>(fn), TreeTile<DL>::LDS, "tree_mfma_kernel");
+  const auto fn = tree_mfma_kernel<DL, RB, QL>;
+  constexpr int lds = TreeTile<DL, RB, QL>::LDS;
+  const int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, "tree_mfma_kernel");
   if (rc) return rc;
-  hipLaunchKernelGGL(fn, dim3(a.p.n_wg), dim3(TR_NW * 64), TreeTile<DL>::LDS, st, a);
+  hipLaunchKernelGGL(fn, dim3(a.p.n_wg), dim3(TR_NW * 64), lds, st, a);
   return check_launch("tree_mfma_kernel");
 }
 
@@ -400,11 +633,13 @@ int launch_tree_mfma(const TreeArgs& a, hipStream_t st) {
   switch (a.dl * 8 + a.p.block / 64) {
     case 64 * 8 + 1: return launch_tree<64, 1>(a, st);
     case 64 * 8 + 2: return launch_tree<64, 2>(a, st);
-    case 64 * 8 + 4: return launch_tree<64, 4>(a, st);
+    case 64 * 8 + 4: return launch_tree<64, 4, 1>(a, st);
     case 128 * 8 + 1: return launch_tree<128, 1>(a, st);
     case 128 * 8 + 2: return launch_tree<128, 2>(a, st);
+    case 128 * 8 + 4: return launch_tree<128, 4, 3>(a, st);
     case 256 * 8 + 1: return launch_tree<256, 1>(a, st);
     case 256 * 8 + 2: return launch_tree<256, 2>(a, st);
+    case 256 * 8 + 3: return launch_tree<256, 3, 2>(a, st);
     case 512 * 8 + 1: return launch_tree<512, 1>(a, st);
   }
   return fail(TPLA_ERR_UNSUPPORTED, "no kernel for slices of %d columns in blocks of %d rows", a.dl, a.p.block);
