@@ -25,7 +25,7 @@ static TreePlan plan_tree(const tpla_shape_t& sh, int n_shards, int T, int max_p
   }
   p.mfma = 0;
   p.n_wg = 0;
-  p.block = 8;
+  p.block = TREE_GENERIC_ROWS;
   p.blocks = (T * sh.H + p.block - 1) / p.block;
   // enough workgroups to fill the chip, not below 256 tokens each
   const double items = (double)n_shards * sh.B * p.blocks, tokens = (double)max_pages * sh.page_tokens;

@@ -331,6 +331,7 @@ int launch_rotary(RotaryArgs a, int dtype, hipStream_t st);
 struct TreePlan {
   int32_t mfma;                // the matrix-core kernel; otherwise the general one
   int32_t block, blocks;       // rows per item, items per (slice, sequence)
+  int32_t teams;               // mfma: 0 the kernel of many rows, else teams of the one of few
   int32_t n_wg;                // mfma: workgroups; partial slots 2 n_wg
   int32_t n_splits, split_tokens;   // general: splits of the longest sequence; slots items * n_splits
 };
@@ -351,6 +352,11 @@ struct TreeArgs {
   TreePlan p;
   float scale_log2;
 };
+__device__ __forceinline__ const void* tree_pool(const TreeArgs& a, int i) {       // (an index known at run time would put the array in scratch memory)
+  return i == 0 ? a.pools[0] : i == 1 ? a.pools[1] : i == 2 ? a.pools[2] : i == 3 ? a.pools[3] :
+         i == 4 ? a.pools[4] : i == 5 ? a.pools[5] : i == 6 ? a.pools[6] : a.pools[7];
+}
+constexpr int TREE_GENERIC_ROWS = 16;      // rows per item of the general kernel
 bool tree_mfma_supported(const tpla_shape_t& sh);
 void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p);
 int launch_tree_mfma(const TreeArgs& a, hipStream_t st);

@@ -8,8 +8,8 @@
 
 namespace tpla {
 
-constexpr int TG_ROWS = 8;          // rows per workgroup: two per wave
 constexpr int TG_DIMS = 1024;       // widest slice
+constexpr int TG_LDS = 64 * 1024;
 
 // A wave's own LDS writes are in place before what follows reads them (LDS operations of a wave complete in order).
 __device__ __forceinline__ void wave_lds_order() {
@@ -17,120 +17,149 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// grid: (items, splits).  A wave takes two rows; per 64 tokens a lane scores one token for both, then the lanes hold columns.
-// Masked tokens are not multiplied by zero but left out: their rows may hold anything.
-template <typename T>
-__global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a) {
-  extern __shared__ float sm[];                     // q [8][dl + d_r], weights [4][2][64]
-  const int w = a.dl + a.d_r, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float* weights = sm + TG_ROWS * w + wave * 128;
+// LDS of the general kernel, in floats: queries [16][w], weights [tokens][16], rows [tokens][w + 4] (an odd number of 16-byte pieces: the
+// lanes of a column spread over the banks).
+__host__ __device__ constexpr int tg_floats(int w, int tokens) { return TREE_GENERIC_ROWS * w + tokens * TREE_GENERIC_ROWS + tokens * (w + 4); }
+
+// grid: (items of 16 rows, splits).  The rows of `tokens` (a power of two up to 64) tokens are staged as floats; a wave scores them for its four
+// rows, 64 / tokens lanes per token, then its lanes hold columns.  Masked tokens are not multiplied by zero but left out: their rows
+// may hold anything.  DC: columns per lane.
+template <typename T, int DC>
+__global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int tokens) {
+  extern __shared__ __align__(16) float sm[];
+  constexpr int RW = TREE_GENERIC_ROWS / 4;
+  const int w = a.dl + a.d_r, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  float* weights = sm + TREE_GENERIC_ROWS * w;
+  float* tile = weights + tokens * TREE_GENERIC_ROWS;
   const int item = blockIdx.x, v = item / a.p.blocks, rb = item % a.p.blocks, i = v / a.B, b = v % a.B;
   const TreeLens len = tree_lens(a, b);
-  const int rows = len.n * a.H, all_rows = a.T * a.H, r0 = rb * TG_ROWS;
+  const int rows = len.n * a.H, all_rows = a.T * a.H, r0 = rb * TREE_GENERIC_ROWS;
   const int k0 = blockIdx.y * a.p.split_tokens, k1 = min(len.keys, k0 + a.p.split_tokens);
   const bool alive = r0 < rows && k0 < k1;          // the same in the whole workgroup
   const T* q_lat = static_cast<const T*>(a.q_lat) + (size_t)v * all_rows * a.dl;
   const T* q_pe = static_cast<const T*>(a.q_pe) + (size_t)b * all_rows * a.d_r;
-  const T* pool = static_cast<const T*>(i == 0 ? a.pools[0] : i == 1 ? a.pools[1] : i == 2 ? a.pools[2] : i == 3 ? a.pools[3] :
-                                        i == 4 ? a.pools[4] : i == 5 ? a.pools[5] : i == 6 ? a.pools[6] : a.pools[7]);
-  if (alive)
-    for (int x = tid; x < TG_ROWS * w; x += 256) {
-      const int r = min(r0 + x / w, rows - 1), c = x % w;
-      sm[x] = c < a.dl ? (float)q_lat[(size_t)r * a.dl + c] : (float)q_pe[(size_t)r * a.d_r + c - a.dl];
+  const T* pool = static_cast<const T*>(tree_pool(a, i));
+  const int rw = r0 + RW * wave;                    // this wave's rows: rw .. rw + 3
+  float m[RW], l[RW], acc[RW][DC];
+#pragma unroll
+  for (int e = 0; e < RW; ++e) {
+    m[e] = -INFINITY;
+    l[e] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DC; ++d) acc[e][d] = 0.f;
+  }
+  if (alive) {
+    for (int x = tid; x < TREE_GENERIC_ROWS * w / 8; x += 256) {
+      const int r = min(r0 + 8 * x / w, rows - 1), c = 8 * x % w;
+      const Vec8 q = c < a.dl ? load8_cached(q_lat + (size_t)r * a.dl + c) : load8_cached(q_pe + (size_t)r * a.d_r + c - a.dl);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sm[8 * x + e] = q.v[e];
     }
-  __syncthreads();
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  float acc[2][TG_DIMS / 64];
+    unsigned long long bits[RW];
 #pragma unroll
-  for (int d = 0; d < TG_DIMS / 64; ++d) acc[0][d] = acc[1][d] = 0.f;
-  const int rw = r0 + 2 * wave;                     // this wave's rows: rw, rw + 1
-  if (alive && rw < rows) {
-    unsigned long long bits[2];
+    for (int e = 0; e < RW; ++e) bits[e] = a.mask[(size_t)b * a.T + min(rw + e, rows - 1) / a.H];
+    const float* q = sm + RW * wave * w;
+    float* mine = weights + wave * tokens * RW;     // [tokens][RW]
+    const int parts = 64 / tokens, tok = lane % tokens, part = lane / tokens;
+    for (int t0 = k0; t0 < k1; t0 += tokens) {
+      __syncthreads();                              // the tile before this one is no longer read
+      for (int x = tid; x < tokens * (w / 8); x += 256) {
+        const int k = x / (w / 8), c = 8 * (x % (w / 8)), t = min(t0 + k, k1 - 1);
+        const int page = a.block_table[(size_t)b * a.max_pages + t / a.page_tokens];
+        const Vec8 r = load8_cached(pool + ((size_t)page * a.page_tokens + t % a.page_tokens) * w + c);
+        *reinterpret_cast<f32x4*>(tile + k * (w + 4) + c) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+        *reinterpret_cast<f32x4*>(tile + k * (w + 4) + c + 4) = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
+      }
+      __syncthreads();
+      if (rw >= rows) continue;
+      float s[RW];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) bits[e] = a.mask[(size_t)b * a.T + min(rw + e, rows - 1) / a.H];
-    const float* q = sm + 2 * wave * w;
-    for (int t0 = k0; t0 < k1; t0 += 64) {
-      const int t = min(t0 + lane, k1 - 1), nt = min(64, k1 - t0);
-      const int page = a.block_table[(size_t)b * a.max_pages + t / a.page_tokens];
-      const T* row = pool + ((size_t)page * a.page_tokens + t % a.page_tokens) * w;
-      float s[2] = {0.f, 0.f};
-      for (int c = 0; c < w; c += 8) {
-        const Vec8 x = load8_cached(row + c);
+      for (int e = 0; e < RW; ++e) s[e] = 0.f;
+      for (int c = 4 * part; c < w; c += 4 * parts) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(tile + tok * (w + 4) + c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s[0] = fmaf(x.v[e], q[c + e], s[0]);
-          s[1] = fmaf(x.v[e], q[w + c + e], s[1]);
+        for (int e = 0; e < RW; ++e) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(q + e * w + c);
+#pragma unroll
+          for (int z = 0; z < 4; ++z) s[e] = fmaf(x[z], y[z], s[e]);
         }
       }
+      const int t = t0 + tok, j = t - len.L;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int j = t0 + lane - len.L;
-        const bool sees = lane < nt && (j < 0 || ((bits[e] >> j) & 1));
+      for (int e = 0; e < RW; ++e) {
+        for (int d = tokens; d < 64; d <<= 1) s[e] += __shfl_xor(s[e], d);
+        const bool sees = t < k1 && (j < 0 || ((bits[e] >> (j & 63)) & 1));
         const float x = sees ? s[e] * a.scale_log2 : -INFINITY;
         const float m_new = fmaxf(m[e], wave_max(x));
         const float ref = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = exp2f(m[e] - ref), p = exp2f(x - ref);
-        l[e] = fmaf(l[e], alpha, wave_sum(p));
+        l[e] = fmaf(l[e], alpha, wave_sum(part == 0 ? p : 0.f));
         m[e] = m_new;
 #pragma unroll
-        for (int d = 0; d < TG_DIMS / 64; ++d) acc[e][d] *= alpha;
-        weights[64 * e + lane] = p;
+        for (int d = 0; d < DC; ++d) acc[e][d] *= alpha;
+        if (part == 0) mine[tok * RW + e] = p;
       }
       wave_lds_order();
-      const size_t row_at = row - pool;
+      const int nt = min(tokens, k1 - t0);
       for (int k = 0; k < nt; ++k) {
-        const float p0 = weights[k], p1 = weights[64 + k];
-        const size_t at = ((size_t)__builtin_amdgcn_readlane((int)(row_at >> 32), k) << 32) | (unsigned)__builtin_amdgcn_readlane((int)row_at, k);
+        const f32x4 p = *reinterpret_cast<const f32x4*>(mine + k * RW);
 #pragma unroll
-        for (int d = 0; d < TG_DIMS / 64; ++d)
-          if (64 * d + lane < a.dl) {
-            const float x = (float)pool[at + 64 * d + lane];
-            if (p0 != 0.f) acc[0][d] = fmaf(p0, x, acc[0][d]);
-            if (p1 != 0.f) acc[1][d] = fmaf(p1, x, acc[1][d]);
-          }
+        for (int d = 0; d < DC; ++d) {
+          const float x = tile[k * (w + 4) + min(64 * d + lane, w - 1)];
+#pragma unroll
+          for (int e = 0; e < RW; ++e) acc[e][d] = p[e] != 0.f ? fmaf(p[e], x, acc[e][d]) : acc[e][d];
+        }
       }
       wave_lds_order();
     }
   }
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
+  for (int e = 0; e < RW; ++e) {
     const int r = rw + e;
     if (r >= all_rows) continue;
     const size_t out = (size_t)v * all_rows + r;
     if (a.p.n_splits == 1) {
       const float inv = l[e] != 0.f ? 1.0f / l[e] : 0.f;
 #pragma unroll
-      for (int d = 0; d < TG_DIMS / 64; ++d)
+      for (int d = 0; d < DC; ++d)
         if (64 * d + lane < a.dl) a.o_lat[out * a.dl + 64 * d + lane] = r < rows ? acc[e][d] * inv : 0.f;
       if (a.lse && lane == 0) a.lse[out] = r < rows ? merge_lse(m[e], l[e]) : -INFINITY;
-    } else {
-      const size_t slot = ((size_t)item * a.p.n_splits + blockIdx.y) * TG_ROWS + (2 * wave + e);
+    } else if (r < rows) {
+      const size_t slot = ((size_t)item * a.p.n_splits + blockIdx.y) * TREE_GENERIC_ROWS + (RW * wave + e);
 #pragma unroll
-      for (int d = 0; d < TG_DIMS / 64; ++d)
+      for (int d = 0; d < DC; ++d)
         if (64 * d + lane < a.dl) a.part_acc[slot * a.dl + 64 * d + lane] = acc[e][d];
-      if (lane == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = make_float2(m[e], r < rows ? l[e] : 0.f);
+      if (lane == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * slot) = make_float2(m[e], l[e]);
     }
   }
 }
 
-int launch_tree_generic(const TreeArgs& a, int dtype, hipStream_t st) {
+template <typename T>
+static int launch_generic(const TreeArgs& a, hipStream_t st) {
+  const int w = a.dl + a.d_r;
+  int tokens = 64;
+  while (tokens > 4 && tg_floats(w, tokens) * 4 > TG_LDS) tokens /= 2;
+  const size_t lds = (size_t)tg_floats(w, tokens) * 4;
+  void (*fn)(TreeArgs, int) = a.dl <= 64 ? tree_generic_kernel<T, 1> : a.dl <= 256 ? tree_generic_kernel<T, 4> : tree_generic_kernel<T, TG_DIMS / 64>;
+  const int rc = allow_lds(reinterpret_cast<const void*>(fn), 160 * 1024, "tree_generic_kernel");
+  if (rc) return rc;
   const dim3 grid((unsigned)(a.n_shards * a.B * a.p.blocks), (unsigned)a.p.n_splits);
-  const size_t lds = ((size_t)TG_ROWS * (a.dl + a.d_r) + 4 * 128) * sizeof(float);
-  if (dtype == TPLA_F32)
-    hipLaunchKernelGGL(tree_generic_kernel<float>, grid, dim3(256), lds, st, a);
-  else
-    hipLaunchKernelGGL(tree_generic_kernel<bf16_t>, grid, dim3(256), lds, st, a);
+  hipLaunchKernelGGL(fn, grid, dim3(256), lds, st, a, tokens);
   return check_launch("tree_generic_kernel");
 }
 
-// Merge: a workgroup takes 8 rows of one item, a wave two of them one after the other.  Per row the lanes hold the references and
-// weights of 64 slots at a time, and the slots' rows are added in ascending order, MERGE_LOADS on their way together (each is a round trip
-// to memory).  Rows of drafts that do not exist get zeros and -inf here.  grid: (groups of 8 rows of a (slice, sequence), (slice, sequence)).
-constexpr int MERGE_ROWS = 8, MERGE_LOADS = 8;
-__global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a) {
+int launch_tree_generic(const TreeArgs& a, int dtype, hipStream_t st) {
+  return dtype == TPLA_F32 ? launch_generic<float>(a, st) : launch_generic<bf16_t>(a, st);
+}
+
+// Merge: a wave takes one row after another of an item, MERGE_LOADS slots' rows on their way together, the first of them requested with their references
+// (each is a round trip to memory); the lanes hold the references and weights of 64 slots at a time, and the rows are added in ascending order.  Rows of
+// drafts that do not exist get zeros and -inf here.  grid: (groups of `group` rows, a multiple of 4 that divides 16, of a (slice, sequence), (slice, sequence)).
+constexpr int MERGE_LOADS = 8;
+__global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int group) {
   const int v = blockIdx.y, b = v % a.B, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int all_rows = a.T * a.H, r0 = blockIdx.x * MERGE_ROWS;
-  const int item = v * a.p.blocks + r0 / a.p.block;             // whole groups of 8 lie in one
+  const int all_rows = a.T * a.H, r0 = blockIdx.x * group;
+  const int item = v * a.p.blocks + r0 / a.p.block;             // a group lies in one
   int first, next, step, n;
   if (a.p.mfma) {
     const int w0 = a.plan[3 * item];                            // (of an item without rows: whatever lies there, not used)
@@ -145,7 +174,7 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a) {
     n = a.p.n_splits;
   }
   const int rows = tree_lens(a, b).n * a.H;
-  for (int e = wave; e < MERGE_ROWS; e += 4) {
+  for (int e = wave; e < group; e += 4) {
     const int r = r0 + e;
     if (r >= all_rows) break;
     float* out = a.o_lat + ((size_t)v * all_rows + r) * a.dl;
@@ -157,22 +186,32 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a) {
     if (n == 1 && a.p.mfma) continue;                           // written by the workgroup that had it whole
     const size_t local = r % a.p.block;
     auto slot = [&](int s) { return (size_t)(s == 0 ? first : next + (s - 1) * step) * a.p.block + local; };
-    float M = -INFINITY, l = 0.f;
-    for (int s0 = 0; s0 < n; s0 += 64) M = fmaxf(M, wave_max(s0 + lane < n ? a.part_ml[2 * slot(s0 + lane)] : -INFINITY));
+    auto request = [&](f32x4 (&p)[MERGE_LOADS], int s0, int c) {
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k) p[k] = *reinterpret_cast<const f32x4*>(a.part_acc + slot(min(s0 + k, n - 1)) * a.dl + c);
+    };
+    f32x4 p[MERGE_LOADS];
+    request(p, 0, min(4 * lane, a.dl - 4));
+    float2 ml = make_float2(-INFINITY, 0.f);                    // of slot `lane`
+    if (lane < n) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot(lane));
+    float M = wave_max(ml.x);
+    for (int s0 = 64; s0 < n; s0 += 64) M = fmaxf(M, wave_max(s0 + lane < n ? a.part_ml[2 * slot(s0 + lane)] : -INFINITY));
     const float ref = M == -INFINITY ? 0.f : M;
+    float l = 0.f;
     for (int c0 = 0; c0 < a.dl; c0 += 256) {
       const int c = min(c0 + 4 * lane, a.dl - 4);
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
       for (int s0 = 0; s0 < n; s0 += 64) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (s0 + lane < n) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot(s0 + lane));
-        const float w = exp2f(ml.x - ref);
-        if (c0 == 0) l += wave_sum(ml.y * w);
+        float2 q = ml;
+        if (s0 > 0) {
+          q = make_float2(-INFINITY, 0.f);
+          if (s0 + lane < n) q = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot(s0 + lane));
+        }
+        const float w = exp2f(q.x - ref);
+        if (c0 == 0) l += wave_sum(q.y * w);
         const int here = min(64, n - s0);
         for (int s = 0; s < here; s += MERGE_LOADS) {
-          f32x4 p[MERGE_LOADS];
-#pragma unroll
-          for (int k = 0; k < MERGE_LOADS; ++k) p[k] = *reinterpret_cast<const f32x4*>(a.part_acc + slot(s0 + min(s + k, here - 1)) * a.dl + c);
+          if (c0 + s0 + s > 0) request(p, s0 + s, c);
 #pragma unroll
           for (int k = 0; k < MERGE_LOADS; ++k)
             if (s + k < here) x += p[k] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s + k));
@@ -186,7 +225,11 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a) {
 }
 
 int launch_tree_merge(const TreeArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((a.T * a.H + MERGE_ROWS - 1) / MERGE_ROWS), (unsigned)(a.n_shards * a.B)), dim3(256), 0, st, a);
+  // one row per wave while that leaves no more than some workgroups per compute unit
+  const int rows = a.T * a.H, n_v = a.n_shards * a.B;
+  int group = 4;
+  while (group < 16 && (long long)((rows + group - 1) / group) * n_v > 16LL * device_cu_count()) group *= 2;
+  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((rows + group - 1) / group), (unsigned)n_v), dim3(256), 0, st, a, group);
   return check_launch("tree_merge_kernel");
 }
 

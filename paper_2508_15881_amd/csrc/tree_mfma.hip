@@ -79,12 +79,12 @@ __device__ __forceinline__ int tree_prefix(int v) {      // inclusive sum over t
   }
   return v;
 }
-// Units (tiles) of sequence b: row blocks x tiles; none without drafts.
+// Units of sequence b (`unit` tokens of one row block): row blocks x units of its tokens; none without drafts.
 struct TreeUnits {
   TreeLens len;
   int tiles, units;
 };
-__device__ __forceinline__ TreeUnits tree_units(const TreeArgs& a, int b) {
+__device__ __forceinline__ TreeUnits tree_units(const TreeArgs& a, int unit, int b) {
   TreeUnits r;
   if (b >= a.B) {
     r.len = TreeLens{0, 0, 0};
@@ -92,10 +92,72 @@ __device__ __forceinline__ TreeUnits tree_units(const TreeArgs& a, int b) {
     return r;
   }
   r.len = tree_lens(a, b);
-  r.tiles = r.len.n > 0 ? max((r.len.keys + TR_TOK - 1) / TR_TOK, 1) : 0;
+  r.tiles = r.len.n > 0 ? max((r.len.keys + unit - 1) / unit, 1) : 0;
   r.units = r.tiles * ((r.len.n * a.H + a.p.block - 1) / a.p.block);
   return r;
 }
+
+// The range of units of this workgroup, [pos, end), and the item that unit `pos` lies in.
+template <int UNIT>
+struct TreeWalk {
+  TreeUnits front;             // the first 64 sequences stay in the lanes: a search among them loads nothing
+  int front_incl, per_slice, units, n_wg, w, pos, range0, end;
+  // the item
+  int i, b, v, item, rb, rows, L, keys, tiles, t0, t1, slot;
+  bool whole;
+
+  __device__ __forceinline__ bool begin(const TreeArgs& a) {
+    const int lane = threadIdx.x & 63;
+    front = tree_units(a, UNIT, lane);
+    front_incl = tree_prefix(front.units);
+    per_slice = __builtin_amdgcn_readlane(front_incl, 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) per_slice += __builtin_amdgcn_readlane(tree_prefix(tree_units(a, UNIT, b0 + lane).units), 63);
+    units = per_slice * a.n_shards;
+    n_wg = max(1, min(a.p.n_wg, units / a.p.split_tokens));             // no shorter ranges than pay
+    // ranges that lie side by side (the row blocks of a sequence, which read the same pages) on one XCD: workgroups go to the eight in turn
+    w = n_wg % 8 == 0 ? (blockIdx.x & 7) * (n_wg >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    if ((int)blockIdx.x >= n_wg || units == 0) return false;
+    range0 = pos = tree_start(n_wg, units, w);
+    end = tree_start(n_wg, units, w + 1);
+    return pos < end;
+  }
+  __device__ __forceinline__ void find(const TreeArgs& a) {
+    const int lane = threadIdx.x & 63;
+    i = pos / per_slice;
+    const int rem = pos - i * per_slice;
+    b = 0;
+    TreeUnits u = front;
+    int incl = front_incl;
+    unsigned long long past = __ballot(incl > rem);
+    while (past == 0) {                              // ends: rem lies below the sum over all sequences
+      b += 64;
+      const int base = __builtin_amdgcn_readlane(incl, 63);
+      u = tree_units(a, UNIT, b + lane);
+      incl = tree_prefix(u.units) + base;
+      past = __ballot(incl > rem);
+    }
+    const int src = __builtin_ctzll(past);
+    b += src;
+    const int before = __builtin_amdgcn_readlane(incl - u.units, src);
+    tiles = __builtin_amdgcn_readlane(u.tiles, src);
+    L = __builtin_amdgcn_readlane(u.len.L, src);
+    keys = __builtin_amdgcn_readlane(u.len.keys, src);
+    rows = __builtin_amdgcn_readlane(u.len.n, src) * a.H;
+    rb = (rem - before) / tiles;
+    t0 = rem - before - rb * tiles;
+    t1 = min(tiles, t0 + (end - pos));
+    v = i * a.B + b;
+    item = v * a.p.blocks + rb;
+    whole = t0 == 0 && t1 == tiles;
+    slot = 2 * w + (pos == range0 ? 0 : 1);
+    if (t0 == 0 && threadIdx.x == 0) {
+      a.plan[3 * item] = w;
+      a.plan[3 * item + 1] = tree_owner(n_wg, units, pos + tiles - 1) - w + 1;
+      a.plan[3 * item + 2] = slot & 1;
+    }
+    pos += t1 - t0;
+  }
+};
 
 // ---- matrix instructions on registers of our choice ----
 // The output accumulators are the accumulation registers a0 .. themselves, quad N of them at a[4 N : 4 N + 3], and everything else
@@ -194,18 +256,8 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, q4 = lane >> 4;
 
-  // ---- this workgroup's range of units ----
-  // (the first 64 sequences stay in the lanes: a search among them loads nothing)
-  const TreeUnits front = tree_units(a, lane);
-  const int front_incl = tree_prefix(front.units);
-  int per_slice = __builtin_amdgcn_readlane(front_incl, 63);
-  for (int b0 = 64; b0 < a.B; b0 += 64) per_slice += __builtin_amdgcn_readlane(tree_prefix(tree_units(a, b0 + lane).units), 63);
-  const int units = per_slice * a.n_shards;
-  const int n_wg = max(1, min(a.p.n_wg, units / a.p.split_tokens));     // no shorter ranges than pay
-  const int w = n_wg % 8 == 0 ? (blockIdx.x & 7) * (n_wg >> 3) + (blockIdx.x >> 3) : blockIdx.x;
-  if ((int)blockIdx.x >= n_wg || units == 0) return;
-  int pos = tree_start(n_wg, units, w);
-  const int range0 = pos, end = tree_start(n_wg, units, w + 1);
+  TreeWalk<TR_TOK> walk;
+  if (!walk.begin(a)) return;
 
   // ---- per-lane LDS offsets: rows begin at whole 128 bytes, so that the pieces of a row differ in address bits 4 to 6 alone ----
   static_assert(RC % 8 == 0, "rows of whole 128 bytes");
@@ -223,32 +275,13 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   auto page_of = [&](int t) { return shift >= 0 ? t >> shift : t / pt; };
   const bool one_page = pt % TR_TOK == 0;              // a tile never crosses a page
 
-  while (pos < end) {
-    // ---- the item of unit `pos` ----
-    const int i = pos / per_slice, rem = pos - i * per_slice;
-    int b = 0, before = 0;
-    TreeUnits u = front;
-    int incl = front_incl;
-    unsigned long long past = __ballot(incl > rem);
-    while (past == 0) {                              // ends: rem lies below the sum over all sequences
-      b += 64;
-      const int base = __builtin_amdgcn_readlane(incl, 63);
-      u = tree_units(a, b + lane);
-      incl = tree_prefix(u.units) + base;
-      past = __ballot(incl > rem);
-    }
-    const int src = __builtin_ctzll(past);
-    b += src;
-    before = __builtin_amdgcn_readlane(incl - u.units, src);
-    const int tiles = __builtin_amdgcn_readlane(u.tiles, src), L = __builtin_amdgcn_readlane(u.len.L, src);
-    const int keys = __builtin_amdgcn_readlane(u.len.keys, src), rows = __builtin_amdgcn_readlane(u.len.n, src) * a.H;
-    const int rb = (rem - before) / tiles, t0 = rem - before - rb * tiles, t1 = min(tiles, t0 + (end - pos));
-    const int v = i * a.B + b, item = v * a.p.blocks + rb;
+  while (walk.pos < walk.end) {
+    walk.find(a);
+    const int i = walk.i, b = walk.b, v = walk.v, rb = walk.rb, L = walk.L, keys = walk.keys, rows = walk.rows, t0 = walk.t0, t1 = walk.t1;
     const int row0 = rb * a.p.block + wave * (16 * RB);          // this wave's first row
     const bool alive = row0 < rows;
     const int all_rows = a.T * a.H;
-    const char* pool = static_cast<const char*>(i == 0 ? a.pools[0] : i == 1 ? a.pools[1] : i == 2 ? a.pools[2] : i == 3 ? a.pools[3] :
-                                                i == 4 ? a.pools[4] : i == 5 ? a.pools[5] : i == 6 ? a.pools[6] : a.pools[7]);
+    const char* pool = static_cast<const char*>(tree_pool(a, i));
     const int32_t* table = a.block_table + (size_t)b * a.max_pages;
 
     // ---- page ids and tiles on their way ----
@@ -332,15 +365,6 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       __builtin_amdgcn_s_barrier();
     };
 
-    const bool whole = t0 == 0 && t1 == tiles;
-    const int slot = 2 * w + (pos == range0 ? 0 : 1);
-    if (t0 == 0 && tid == 0) {
-      const int last = tree_owner(n_wg, units, pos + tiles - 1);
-      a.plan[3 * item] = w;
-      a.plan[3 * item + 1] = last - w + 1;
-      a.plan[3 * item + 2] = pos == range0 ? 0 : 1;
-    }
-    pos += t1 - t0;
     if (!alive) {                                    // no rows: this wave only loads
       first_tiles();
       for (int t = t0; t < t1; ++t) {
@@ -566,8 +590,8 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
       const bool there = row < rows;
-      const float inv = whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
-      float* out = whole ? a.o_lat + ((size_t)v * all_rows + row) * DL : a.part_acc + ((size_t)slot * a.p.block + local) * DL;
+      const float inv = walk.whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
+      float* out = walk.whole ? a.o_lat + ((size_t)v * all_rows + row) * DL : a.part_acc + ((size_t)walk.slot * a.p.block + local) * DL;
       static_for<DB>([&](auto dc) {
         constexpr int d = decltype(dc)::value;
         const f32x4 x = acc_read<r * DB + d>() * inv;
@@ -575,12 +599,264 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       });
       acc_keep();
       if (there && q4 == 0) {
-        if (!whole)
-          *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)slot * a.p.block + local)) = make_float2(m_run[r], l);
+        if (!walk.whole)
+          *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)walk.slot * a.p.block + local)) = make_float2(m_run[r], l);
         else if (a.lse)
           a.lse[(size_t)v * all_rows + row] = l != 0.f ? (m_run[r] + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
     });
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: up to 64 (TEAMS = 2) or 128 (TEAMS = 1) per item.  What bounds these is how fast one compute unit gets through its cache rows, and a
+// single wave per SIMD leaves most of its time to waits.  Here 8 waves of 16 rows share rounds of 64 tokens, two waves per SIMD: one's
+// matrix products run under the other's exponentials and reads.  TEAMS = 2: four waves take the first 32 tokens of a round and four the
+// others, for the same 64 rows, and their results are joined through LDS at the end of the item.
+constexpr int TP_NW = 8, TP_TOK = 64;
+
+template <int DL>
+struct PairTile {
+  static constexpr int RC = (DL + 64) / 8;
+  static constexpr int BYTES = TP_TOK * RC * 16;       // a round
+  static constexpr int CPT = TP_TOK * RC / 64 / TP_NW;
+  static constexpr int NSTAGE = 3;
+  static constexpr int IDS = NSTAGE * BYTES, LDS = IDS + TR_ID_RING * 4;
+  static_assert(TP_TOK * RC % (64 * TP_NW) == 0, "every wave issues the same number of loads");
+  static_assert(4 * (DL / 16 + 1) * 1024 <= NSTAGE * BYTES, "the join of two teams fits the ring");
+};
+
+template <int DL, int TEAMS>
+__global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
+  using Tile = PairTile<DL>;
+  constexpr int RC = Tile::RC, CPT = Tile::CPT, NSTAGE = Tile::NSTAGE;
+  constexpr int KS = (DL + 64) / 32, DB = DL / 16, NQ = 2 * KS;
+  constexpr int KRING = 6, VRING = 4, TEAM = TP_NW / TEAMS;
+  extern __shared__ u32x4 smem[];
+  char* const lds = reinterpret_cast<char*>(smem);
+  const unsigned lds_base = lds_at(lds);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), team = wave / TEAM, member = wave % TEAM;
+  const int j16 = lane & 15, q4 = lane >> 4;
+  TreeWalk<TP_TOK> walk;
+  if (!walk.begin(a)) return;
+
+  const unsigned k_off = (unsigned)((j16 * RC + (q4 ^ swz(j16))) * 16);
+  const int v_tok = 4 * q4 + (j16 >> 2);
+  const unsigned v_off = (unsigned)((v_tok * RC + (((j16 & 3) >> 1) ^ swz(v_tok))) * 16 + (j16 & 1) * 8);
+  unsigned ld_at[CPT];                                 // byte of this lane's piece within a page that holds the round's 64 rows
+#pragma unroll
+  for (int j = 0; j < CPT; ++j) {
+    const int x = (wave + j * TP_NW) * 64 + lane, tok = x / RC;
+    ld_at[j] = (unsigned)(tok * (RC * 16) + ((x % RC) ^ swz(tok)) * 16);
+  }
+  const int pt = a.page_tokens, shift = (pt & (pt - 1)) == 0 ? __builtin_ctz(pt) : -1;
+  auto page_of = [&](int t) { return shift >= 0 ? t >> shift : t / pt; };
+  const bool one_page = pt % TP_TOK == 0;
+
+  while (walk.pos < walk.end) {
+    walk.find(a);
+    const int b = walk.b, v = walk.v, L = walk.L, keys = walk.keys, rows = walk.rows, t0 = walk.t0, t1 = walk.t1;
+    const int row0 = walk.rb * a.p.block + member * 16, all_rows = a.T * a.H;
+    const bool alive = row0 < rows;
+    const char* pool = static_cast<const char*>(tree_pool(a, walk.i));
+    const int32_t* table = a.block_table + (size_t)b * a.max_pages;
+
+    // ---- page ids and rounds on their way (as in the kernel above; a chunk of ids is at least 4 rounds, 2 are requested ahead) ----
+    int chunk = page_of(t0 * TP_TOK) / TR_IDS;
+    auto request_ids = [&](int c) {
+      if (wave >= TR_IDS / 64) return;
+      const int p = min(c * TR_IDS + wave * 64 + lane, a.max_pages - 1);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(table + p),
+                                       (__attribute__((address_space(3))) void*)(lds + Tile::IDS + ((c & 3) * TR_IDS + wave * 64) * 4), 4, 0, 0);
+    };
+    auto id_at = [&](int p) { return lds_base + Tile::IDS + (unsigned)(p & (TR_ID_RING - 1)) * 4; };
+    auto issue = [&](int t) {
+      const int k0 = t * TP_TOK, p0 = __builtin_amdgcn_readfirstlane(page_of(k0));
+      char* dst = lds + (t % NSTAGE) * Tile::BYTES + wave * 1024;
+      if (one_page && k0 + TP_TOK <= keys) {
+        const int page = __builtin_amdgcn_readfirstlane(lds_read_id(id_at(p0)));
+        const char* src = pool + ((size_t)page * pt + (k0 - p0 * pt)) * (RC * 16);
+#pragma unroll
+        for (int j = 0; j < CPT; ++j)
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + ld_at[j]),
+                                           (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, 2 /* streaming: not kept in L2 */);
+      } else {
+        // rows of several pages, or past the end: those repeat the last token (and are masked)
+#pragma unroll 1
+        for (int j = 0; j < CPT; ++j) {
+          const int x = (wave + j * TP_NW) * 64 + here(lane), tok = x / RC, k = min(k0 + tok, keys - 1), p = page_of(k);
+          const int row_id = (int)lds_read_id(id_at(p));
+          const char* src = pool + ((size_t)row_id * pt + (k - p * pt)) * (RC * 16) + ((x % RC) ^ swz(tok)) * 16;
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                           (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, 2 /* streaming: not kept in L2 */);
+        }
+      }
+      const int c = p0 / TR_IDS;
+      if (c != chunk) {
+        chunk = c;
+        request_ids(c + 1);
+      }
+    };
+    lds_barrier();                                   // the item before this one no longer reads LDS
+    request_ids(chunk);
+    request_ids(chunk + 1);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __builtin_amdgcn_s_barrier();
+    for (int t = t0; t < t1 && t < t0 + NSTAGE - 1; ++t) issue(t);
+
+    bf16x8 q[KS];
+    {
+      const int row = min(row0 + j16, rows - 1);
+      const bf16_t* ql = static_cast<const bf16_t*>(a.q_lat) + ((size_t)v * all_rows + row) * DL + q4 * 8;
+      const bf16_t* qp = static_cast<const bf16_t*>(a.q_pe) + ((size_t)b * all_rows + row) * 64 + q4 * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const bf16x8*>(ks * 32 < DL ? ql + ks * 32 : qp + (ks * 32 - DL));
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[ks]));   // complete before the loop
+    }
+    f32x4 acc[DB];
+    float m_run = -FLT_MAX, l_run = 0.f;             // see the kernel above
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    auto clean = [&](int t, int first, int n) {      // rows first .. first + n - 1 of round t; see the kernel above
+      lds_barrier();
+#pragma unroll 1
+      for (int x = here(tid); x < n * RC; x += TP_NW * 64) {
+        const int tok = first + x / RC, c = (x % RC) ^ swz(tok);
+        if (c >= DL / 8 || t * TP_TOK + tok < L) continue;
+        u32x4* at = smem + (t % NSTAGE) * (TP_TOK * RC) + first * RC + x;
+        u32x4 u = *at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
+          if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+        }
+        *at = u;
+      }
+      lds_barrier();
+    };
+
+    // 32 tokens of round t, rows 32 sub ..
+    auto tile_of = [&](int t, int sub) {
+      const unsigned tile = lds_base + (unsigned)((t % NSTAGE) * Tile::BYTES + sub * (32 * RC * 16));
+      const bool tail = (t + 1) * TP_TOK > L;
+      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      if (alive) {
+        bf16x8 kf[KRING];
+        const unsigned ka = tile + k_off;
+        auto read_k = [&](auto ic) {
+          constexpr int x = decltype(ic)::value, ks = x / 2, tb = x % 2;
+          lds_read_b128<(ks >> 1) * 128 + tb * (16 * RC * 16)>(kf[x % KRING], ka ^ ((ks & 1) << 6));
+        };
+        static_for<KRING>(read_k);
+        static_for<NQ>([&](auto ic) {
+          constexpr int x = decltype(ic)::value, left = NQ - 1 - x;
+          lds_wait<(left < KRING - 1 ? left : KRING - 1)>(kf[x % KRING]);
+          s[x % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x % KRING], q[x / 2], s[x % 2], 0, 0, 0);
+          if constexpr (x + KRING < NQ) read_k(std::integral_constant<int, x + KRING>{});
+        });
+      }
+      if (tail) clean(t, TEAMS == 2 ? 0 : 32 * sub, TEAMS == 2 ? TP_TOK : 32);
+      if (!alive) return;
+      u32x2 vlo[VRING], vhi[VRING];
+      const unsigned va = tile + v_off;
+      auto read_v = [&](auto ic) {
+        constexpr int d = decltype(ic)::value;
+        lds_read_tr_b64<(d >> 2) * 128>(vlo[d % VRING], va ^ ((d & 3) << 5));
+        lds_read_tr_b64<(d >> 2) * 128 + 16 * RC * 16>(vhi[d % VRING], va ^ ((d & 3) << 5));
+      };
+      if (tail) {
+        const int row = min(row0 + here(j16), rows - 1);
+        const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k = t * TP_TOK + 32 * sub + 16 * tb + 4 * here(q4) + e, j = k - L;
+            if (j >= 0 && (k >= keys || !((bits >> (j & 63)) & 1))) s[tb][e] = -INFINITY;
+          }
+      }
+      static_for<VRING>(read_v);
+      float mx = fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+      for (int e = 2; e < 8; ++e) mx = fmaxf(mx, s[e >> 2][e & 3]);
+      mx *= a.scale_log2;
+      if (__any(mx > m_run + LAZY)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = fmaxf(mx, m_run);
+        const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
+        l_run *= alpha;
+        m_run = mx;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+      }
+      bf16x8 pb;                                     // weights in bf16, their sum from the unrounded ones
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], a.scale_log2, -m_run));
+        l_run += p;
+        pb[e] = (bf16_t)p;
+      }
+      static_for<DB>([&](auto ic) {
+        constexpr int d = decltype(ic)::value, left = DB - 1 - d;
+        lds_wait<2 * (left < VRING - 1 ? left : VRING - 1)>(vlo[d % VRING], vhi[d % VRING]);
+        const u32x4 v4 = {vlo[d % VRING][0], vlo[d % VRING][1], vhi[d % VRING][0], vhi[d % VRING][1]};
+        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb, acc[d], 0, 0, 0);
+        if constexpr (d + VRING < DB) read_v(std::integral_constant<int, d + VRING>{});
+      });
+    };
+
+    for (int t = t0; t < t1; ++t) {
+      if (t + 1 < t1)
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm((NSTAGE - 2) * CPT));
+      else
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      __builtin_amdgcn_s_barrier();                  // round t is there for all waves, round t - 1 is no longer read
+      if (t + NSTAGE - 1 < t1) issue(t + NSTAGE - 1);
+      if constexpr (TEAMS == 2) {
+        tile_of(t, team);
+      } else {
+#pragma unroll 1
+        for (int sub = 0; sub < 2; ++sub) tile_of(t, sub);
+      }
+    }
+
+    // ---- the two teams' halves of the tokens, then the result ----
+    if constexpr (TEAMS == 2) {
+      lds_barrier();                                 // the last round is no longer read
+      char* const at = lds + member * ((DB + 1) * 1024) + lane * 16;
+      if (team == 1) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(at + d * 1024) = acc[d];
+        *reinterpret_cast<float2*>(at + DB * 1024) = make_float2(m_run, l_run);
+      }
+      lds_barrier();
+      if (team == 1) continue;
+      const float2 ml = *reinterpret_cast<const float2*>(at + DB * 1024);
+      const float m = fmaxf(m_run, ml.x), mine = __builtin_amdgcn_exp2f(m_run - m), theirs = __builtin_amdgcn_exp2f(ml.x - m);
+      m_run = m;
+      l_run = l_run * mine + ml.y * theirs;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) acc[d] = acc[d] * mine + *reinterpret_cast<const f32x4*>(at + d * 1024) * theirs;
+    }
+    float l = l_run;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const int local = member * 16 + j16, row = row0 + j16;
+    if (!alive || row >= rows) continue;
+    const float inv = walk.whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
+    float* out = walk.whole ? a.o_lat + ((size_t)v * all_rows + row) * DL : a.part_acc + ((size_t)walk.slot * a.p.block + local) * DL;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(out + 16 * d + 4 * q4) = acc[d] * inv;
+    if (q4 == 0) {
+      if (!walk.whole)
+        *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)walk.slot * a.p.block + local)) = make_float2(m_run, l);
+      else if (a.lse)
+        a.lse[(size_t)v * all_rows + row] = l != 0.f ? (m_run + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
   }
 }
 
@@ -610,13 +886,14 @@ static int row_blocks(int dl, int rows) {
 void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p) {
   const int dl = sh.d_c / sh.g;
   p->mfma = 1;
-  p->block = 64 * row_blocks(dl, T * sh.H);
+  p->teams = dl == 512 ? 0 : T * sh.H <= 64 ? 2 : T * sh.H <= 128 ? 1 : 0;
+  p->block = p->teams ? 128 / p->teams : 64 * row_blocks(dl, T * sh.H);
   p->blocks = (T * sh.H + p->block - 1) / p->block;
   const double tiles = ((double)max_pages * sh.page_tokens + TR_TOK - 1) / TR_TOK;
   const double most = (double)n_shards * sh.B * p->blocks * std::max(tiles, 1.0);
   p->n_wg = (int)std::min((double)device_cu_count(), most);
   p->n_splits = 1;
-  p->split_tokens = 4;         // fewest tiles of a range
+  p->split_tokens = p->teams ? 2 : 4;         // fewest units of a range
 }
 
 template <int DL, int RB, int QL = 0>
@@ -629,7 +906,28 @@ static int launch_tree(const TreeArgs& a, hipStream_t st) {
   return check_launch("tree_mfma_kernel");
 }
 
+template <int DL, int TEAMS>
+static int launch_pair(const TreeArgs& a, hipStream_t st) {
+  const auto fn = tree_pair_kernel<DL, TEAMS>;
+  constexpr int lds = PairTile<DL>::LDS;
+  const int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, "tree_pair_kernel");
+  if (rc) return rc;
+  hipLaunchKernelGGL(fn, dim3(a.p.n_wg), dim3(TP_NW * 64), lds, st, a);
+  return check_launch("tree_pair_kernel");
+}
+
 int launch_tree_mfma(const TreeArgs& a, hipStream_t st) {
+  if (a.p.teams) {
+    switch (a.dl * 8 + a.p.teams) {
+      case 64 * 8 + 1: return launch_pair<64, 1>(a, st);
+      case 64 * 8 + 2: return launch_pair<64, 2>(a, st);
+      case 128 * 8 + 1: return launch_pair<128, 1>(a, st);
+      case 128 * 8 + 2: return launch_pair<128, 2>(a, st);
+      case 256 * 8 + 1: return launch_pair<256, 1>(a, st);
+      case 256 * 8 + 2: return launch_pair<256, 2>(a, st);
+    }
+    return fail(TPLA_ERR_UNSUPPORTED, "no kernel of %d teams for slices of %d columns", a.p.teams, a.dl);
+  }
   switch (a.dl * 8 + a.p.block / 64) {
     case 64 * 8 + 1: return launch_tree<64, 1>(a, st);
     case 64 * 8 + 2: return launch_tree<64, 2>(a, st);
