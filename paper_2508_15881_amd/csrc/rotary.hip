@@ -9,77 +9,122 @@
 namespace tpla {
 
 constexpr int RO_THREADS = 256;
+constexpr int RO_BATCH = 4;        // rows per thread on their way together
 
 template <typename T>
 struct alignas(16) Eight {
   T v[8];
 };
 
-// grid: (token blocks, head blocks).  LDS: [tokens][rot / 2] pairs of (cos, sin), amplitude included.
-// VEC: a thread takes 8 columns (and, for halves, their 8 partners); otherwise one pair or one copied column.
+// What a thread does to one row.  VEC: 8 columns (of halves' rotated columns 8 and their 8 partners), otherwise one pair or one copied column.
+template <typename T, bool VEC>
+struct RowPart;
+template <typename T>
+struct RowPart<T, true> {
+  Eight<T> p, q;
+  __device__ __forceinline__ void load(const RotaryArgs& a, const T* src, int at, bool two) {
+    p = *reinterpret_cast<const Eight<T>*>(src + at);
+    if (two) q = *reinterpret_cast<const Eight<T>*>(src + at + a.rot / 2);
+  }
+  // turn: (cos, sin) of this token's pairs
+  __device__ __forceinline__ void store(const RotaryArgs& a, T* dst, int at, bool two, const float2* turn) {
+    if (two) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 cs = turn[at + e];
+        const float x = (float)p.v[e], y = (float)q.v[e];
+        p.v[e] = (T)(x * cs.x - y * cs.y);
+        q.v[e] = (T)(x * cs.y + y * cs.x);
+      }
+      *reinterpret_cast<Eight<T>*>(dst + at + a.rot / 2) = q;
+    } else if (a.layout == TPLA_ROTARY_INTERLEAVED) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        if (at + e < a.rot) {
+          const float2 cs = turn[(at + e) / 2];
+          const float x = (float)p.v[e], y = (float)p.v[e + 1];
+          p.v[e] = (T)(x * cs.x - y * cs.y);
+          p.v[e + 1] = (T)(x * cs.y + y * cs.x);
+        }
+    }
+    *reinterpret_cast<Eight<T>*>(dst + at) = p;
+  }
+};
+template <typename T>
+struct RowPart<T, false> {
+  T p, q;
+  __device__ __forceinline__ void load(const RotaryArgs& a, const T* src, int at, bool two) {
+    p = src[at];
+    if (two) q = src[at + (a.layout == TPLA_ROTARY_HALF ? a.rot / 2 : 1)];
+  }
+  __device__ __forceinline__ void store(const RotaryArgs& a, T* dst, int at, bool two, const float2* turn) {
+    const bool half = a.layout == TPLA_ROTARY_HALF;
+    if (two) {
+      const float2 cs = turn[half ? at : at / 2];
+      const float x = (float)p, y = (float)q;
+      p = (T)(x * cs.x - y * cs.y);
+      dst[at + (half ? a.rot / 2 : 1)] = (T)(x * cs.y + y * cs.x);
+    }
+    dst[at] = p;
+  }
+};
+
+// grid: (blocks of tokens, blocks of heads).  LDS: [tokens][rot / 2] pairs of (cos, sin), amplitude included.  A thread keeps its part of a row and
+// takes rows lanes_per_row threads apart, RO_BATCH of them on their way together; the keys are one more head.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a) {
-  extern __shared__ float2 turn[];
+  extern __shared__ float2 turns[];
   const int pairs = a.rot / 2, tid = threadIdx.x;
   const long long t0 = (long long)blockIdx.x * a.block_tokens;
   const int nt = (int)min((long long)a.block_tokens, a.T - t0);
   for (int x = tid; x < nt * pairs; x += RO_THREADS) {
-    const double turns = (double)a.positions[t0 + x / pairs] * (a.freq[x % pairs] * 0.15915494309189533577);
+    const double turn = (double)a.positions[t0 + x / pairs] * (a.freq[x % pairs] * 0.15915494309189533577);
     float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+    sincospif((float)(2.0 * (turn - rint(turn))), &s, &c);
     if (a.inverse) s = -s;
-    turn[x] = make_float2(c * a.amplitude, s * a.amplitude);
+    turns[x] = make_float2(c * a.amplitude, s * a.amplitude);
   }
   __syncthreads();
-  const int heads = (a.q ? a.H : 0) + (a.k ? 1 : 0);
-  const int h0 = blockIdx.y * a.block_heads, nh = min(a.block_heads, heads - h0);
   const bool half = a.layout == TPLA_ROTARY_HALF;
-  // work per row: VEC: pieces of 8 columns, of the rotated ones of halves the first half's only
-  const int lead = VEC ? (half ? pairs / 8 : 0) : pairs;
-  const int per_row = VEC ? lead + (half ? (a.d_r - a.rot) / 8 : a.d_r / 8) : pairs + (a.d_r - a.rot);
-  for (int x = tid; x < nt * nh * per_row; x += RO_THREADS) {
-    const int w = x % per_row, row = x / per_row, h = h0 + row % nh, tt = row / nh;
-    const long long t = t0 + tt;
-    const bool key = h == heads - 1 && a.k;
-    const T* src = static_cast<const T*>(key ? a.k : a.q) + (key ? t * a.k_ts : t * a.q_ts + h * a.q_hs);
-    T* dst = static_cast<T*>(key ? a.k_out : a.q_out) + (key ? t * a.ko_ts : t * a.qo_ts + h * a.qo_hs);
-    const float2* tr = turn + tt * pairs;
-    if constexpr (VEC) {
-      if (half && w < lead) {
-        const Eight<T> p = *reinterpret_cast<const Eight<T>*>(src + 8 * w), q = *reinterpret_cast<const Eight<T>*>(src + pairs + 8 * w);
-        Eight<T> u, v;
+  // parts of a row: rotated ones (halves: of the first half), then what is copied
+  const int lead = VEC ? (half ? pairs / 8 : a.d_r / 8) : pairs;
+  const int parts = VEC ? (half ? lead + (a.d_r - a.rot) / 8 : lead) : pairs + (a.d_r - a.rot);
+  const int at_once = max(1, RO_THREADS / parts);
+  const int heads = (a.q ? a.H : 0) + (a.k ? 1 : 0);
+  const int h0 = blockIdx.y * a.block_heads, nh = min(a.block_heads, heads - h0), rows = nt * nh;
+  for (int part = tid % parts; part < parts; part += RO_THREADS) {       // (once, unless a row has more parts than there are threads)
+    const int first = tid / parts;
+    if (first >= at_once) continue;
+    const bool two = VEC ? half && part < lead : part < lead;
+    const int at = VEC ? (part < lead ? 8 * part : a.rot + 8 * (part - lead)) : part < lead ? (half ? part : 2 * part) : a.rot + part - lead;
+    // row = token * nh + head, walked without divisions
+    const int dt = at_once / nh, dh = at_once % nh;
+    int tt = first / nh, h = first % nh;
+    for (int row = first; row < rows; row += RO_BATCH * at_once) {
+      RowPart<T, VEC> x[RO_BATCH];
+      T* dst[RO_BATCH];
+      int tok[RO_BATCH];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 cs = tr[8 * w + e];
-          const float p0 = (float)p.v[e], q0 = (float)q.v[e];
-          u.v[e] = (T)(p0 * cs.x - q0 * cs.y);
-          v.v[e] = (T)(p0 * cs.y + q0 * cs.x);
+      for (int k = 0; k < RO_BATCH; ++k) {
+        dst[k] = nullptr;
+        if (row + k * at_once < rows) {
+          const long long t = t0 + tt;
+          const bool key = a.k && h0 + h == heads - 1;
+          const T* src = key ? static_cast<const T*>(a.k) + t * a.k_ts : static_cast<const T*>(a.q) + t * a.q_ts + (h0 + h) * a.q_hs;
+          dst[k] = key ? static_cast<T*>(a.k_out) + t * a.ko_ts : static_cast<T*>(a.q_out) + t * a.qo_ts + (h0 + h) * a.qo_hs;
+          tok[k] = tt;
+          x[k].load(a, src, at, two);
         }
-        *reinterpret_cast<Eight<T>*>(dst + 8 * w) = u;
-        *reinterpret_cast<Eight<T>*>(dst + pairs + 8 * w) = v;
-      } else {
-        const int c0 = half ? a.rot + 8 * (w - lead) : 8 * w;
-        Eight<T> p = *reinterpret_cast<const Eight<T>*>(src + c0);
+        tt += dt;
+        h += dh;
+        if (h >= nh) {
+          h -= nh;
+          ++tt;
+        }
+      }
 #pragma unroll
-        for (int e = 0; e < 8; e += 2)
-          if (c0 + e < a.rot && !half) {
-            const float2 cs = tr[(c0 + e) / 2];
-            const float p0 = (float)p.v[e], q0 = (float)p.v[e + 1];
-            p.v[e] = (T)(p0 * cs.x - q0 * cs.y);
-            p.v[e + 1] = (T)(p0 * cs.y + q0 * cs.x);
-          }
-        *reinterpret_cast<Eight<T>*>(dst + c0) = p;
-      }
-    } else {
-      if (w < pairs) {
-        const int i = half ? w : 2 * w, j = half ? w + pairs : 2 * w + 1;
-        const float2 cs = tr[w];
-        const float p0 = (float)src[i], q0 = (float)src[j];
-        dst[i] = (T)(p0 * cs.x - q0 * cs.y);
-        dst[j] = (T)(p0 * cs.y + q0 * cs.x);
-      } else {
-        dst[pairs + w] = src[pairs + w];
-      }
+      for (int k = 0; k < RO_BATCH; ++k)
+        if (dst[k]) x[k].store(a, dst[k], at, two, turns + tok[k] * pairs);
     }
   }
 }
