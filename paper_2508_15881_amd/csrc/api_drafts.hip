@@ -25,7 +25,10 @@ static TreePlan plan_tree(const tpla_shape_t& sh, int n_shards, int T, int max_p
   }
   p.mfma = 0;
   p.n_wg = 0;
-  p.block = TREE_GENERIC_ROWS;
+  p.teams = 0;
+  // Four rows per wave read LDS a third as often; one row per wave where that leaves compute units idle (two sequences of 128 tokens, 20
+  // rows, 32 columns: 17.9 us with four, 11.6 with one).
+  p.block = (double)n_shards * sh.B * ((T * sh.H + 15) / 16) >= device_cu_count() ? 16 : 4;
   p.blocks = (T * sh.H + p.block - 1) / p.block;
   // enough workgroups to fill the chip, not below 256 tokens each
   const double items = (double)n_shards * sh.B * p.blocks, tokens = (double)max_pages * sh.page_tokens;

@@ -356,7 +356,6 @@ __device__ __forceinline__ const void* tree_pool(const TreeArgs& a, int i) {    
   return i == 0 ? a.pools[0] : i == 1 ? a.pools[1] : i == 2 ? a.pools[2] : i == 3 ? a.pools[3] :
          i == 4 ? a.pools[4] : i == 5 ? a.pools[5] : i == 6 ? a.pools[6] : a.pools[7];
 }
-constexpr int TREE_GENERIC_ROWS = 16;      // rows per item of the general kernel
 bool tree_mfma_supported(const tpla_shape_t& sh);
 void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p);
 int launch_tree_mfma(const TreeArgs& a, hipStream_t st);

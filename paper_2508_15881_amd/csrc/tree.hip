@@ -10,6 +10,8 @@ namespace tpla {
 
 constexpr int TG_DIMS = 1024;       // widest slice
 constexpr int TG_LDS = 64 * 1024;
+constexpr int TG_TOKENS = 4;        // tokens per lane whose products are on their way together; 8 groups of them are 32 tokens
+constexpr int TG_BATCH = 8;         // pieces of 8 per thread on their way together
 
 // A wave's own LDS writes are in place before what follows reads them (LDS operations of a wave complete in order).
 __device__ __forceinline__ void wave_lds_order() {
@@ -17,29 +19,31 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// LDS of the general kernel, in floats: queries [16][w], weights [tokens][16], rows [tokens][w + 4] (an odd number of 16-byte pieces: the
+// LDS of the general kernel, in floats: queries [rows][w], weights [tokens][rows], rows [stage][w + 4] (an odd number of 16-byte pieces: the
 // lanes of a column spread over the banks).
-__host__ __device__ constexpr int tg_floats(int w, int tokens) { return TREE_GENERIC_ROWS * w + tokens * TREE_GENERIC_ROWS + tokens * (w + 4); }
+__host__ __device__ constexpr int tg_floats(int w, int rows, int tokens, int stage) { return rows * w + tokens * rows + stage * (w + 4); }
 
-// grid: (items of 16 rows, splits).  The rows of `tokens` (a power of two up to 64) tokens are staged as floats; a wave scores them for its four
-// rows, 64 / tokens lanes per token, then its lanes hold columns.  Masked tokens are not multiplied by zero but left out: their rows
+// grid: (items of 4 RW rows, splits).  The rows of `stage` tokens are staged as floats, as many as LDS holds: short contexts are two round trips to
+// memory and not two for every 64 tokens.  Of these a wave scores `tokens` (a power of two up to 64 that divides stage) at a time for its RW rows,
+// 64 / tokens lanes per token, then its lanes hold columns.  Masked tokens are not multiplied by zero but left out: their rows
 // may hold anything.  DC: columns per lane.
-template <typename T, int DC>
-__global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int tokens) {
+template <typename T, int DC, int RW>
+__global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int tokens, int stage) {
   extern __shared__ __align__(16) float sm[];
-  constexpr int RW = TREE_GENERIC_ROWS / 4;
+  constexpr int ROWS = 4 * RW;
+  typedef float Weights __attribute__((ext_vector_type(RW)));
   const int w = a.dl + a.d_r, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  float* weights = sm + TREE_GENERIC_ROWS * w;
-  float* tile = weights + tokens * TREE_GENERIC_ROWS;
+  float* weights = sm + ROWS * w;
+  float* staged = weights + tokens * ROWS;
   const int item = blockIdx.x, v = item / a.p.blocks, rb = item % a.p.blocks, i = v / a.B, b = v % a.B;
   const TreeLens len = tree_lens(a, b);
-  const int rows = len.n * a.H, all_rows = a.T * a.H, r0 = rb * TREE_GENERIC_ROWS;
+  const int rows = len.n * a.H, all_rows = a.T * a.H, r0 = rb * ROWS;
   const int k0 = blockIdx.y * a.p.split_tokens, k1 = min(len.keys, k0 + a.p.split_tokens);
   const bool alive = r0 < rows && k0 < k1;          // the same in the whole workgroup
   const T* q_lat = static_cast<const T*>(a.q_lat) + (size_t)v * all_rows * a.dl;
   const T* q_pe = static_cast<const T*>(a.q_pe) + (size_t)b * all_rows * a.d_r;
   const T* pool = static_cast<const T*>(tree_pool(a, i));
-  const int rw = r0 + RW * wave;                    // this wave's rows: rw .. rw + 3
+  const int rw = r0 + RW * wave;                    // this wave's rows: rw .. rw + RW - 1
   float m[RW], l[RW], acc[RW][DC];
 #pragma unroll
   for (int e = 0; e < RW; ++e) {
@@ -49,7 +53,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
     for (int d = 0; d < DC; ++d) acc[e][d] = 0.f;
   }
   if (alive) {
-    for (int x = tid; x < TREE_GENERIC_ROWS * w / 8; x += 256) {
+    for (int x = tid; x < ROWS * w / 8; x += 256) {
       const int r = min(r0 + 8 * x / w, rows - 1), c = 8 * x % w;
       const Vec8 q = c < a.dl ? load8_cached(q_lat + (size_t)r * a.dl + c) : load8_cached(q_pe + (size_t)r * a.d_r + c - a.dl);
 #pragma unroll
@@ -61,57 +65,97 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
     const float* q = sm + RW * wave * w;
     float* mine = weights + wave * tokens * RW;     // [tokens][RW]
     const int parts = 64 / tokens, tok = lane % tokens, part = lane / tokens;
-    for (int t0 = k0; t0 < k1; t0 += tokens) {
-      __syncthreads();                              // the tile before this one is no longer read
-      for (int x = tid; x < tokens * (w / 8); x += 256) {
-        const int k = x / (w / 8), c = 8 * (x % (w / 8)), t = min(t0 + k, k1 - 1);
-        const int page = a.block_table[(size_t)b * a.max_pages + t / a.page_tokens];
-        const Vec8 r = load8_cached(pool + ((size_t)page * a.page_tokens + t % a.page_tokens) * w + c);
-        *reinterpret_cast<f32x4*>(tile + k * (w + 4) + c) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
-        *reinterpret_cast<f32x4*>(tile + k * (w + 4) + c + 4) = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
+    // narrow slices: groups of lanes take different tokens
+    const int cols = a.dl > 32 || tokens < 64 ? 64 : a.dl > 16 ? 32 : a.dl > 8 ? 16 : 8, groups = 64 / cols;
+    const int col = lane % cols, group = lane / cols;
+    for (int s0 = k0; s0 < k1; s0 += stage) {
+      __syncthreads();                              // the rows before these are no longer read
+      const int pieces = w / 8, here = min(stage, (k1 - s0 + tokens - 1) / tokens * tokens), all = here * pieces;
+      for (int x0 = tid; x0 < all; x0 += 256 * TG_BATCH) {
+        int at[TG_BATCH];
+        size_t row[TG_BATCH];
+#pragma unroll
+        for (int e = 0; e < TG_BATCH; ++e) {
+          const int x = min(x0 + 256 * e, all - 1), k = x / pieces, t = min(s0 + k, k1 - 1), p = t / a.page_tokens;
+          at[e] = k * (w + 4) + 8 * (x - k * pieces);
+          row[e] = ((size_t)a.block_table[(size_t)b * a.max_pages + p] * a.page_tokens + (t - p * a.page_tokens)) * w + 8 * (x - k * pieces);
+        }
+        Vec8 r[TG_BATCH];
+#pragma unroll
+        for (int e = 0; e < TG_BATCH; ++e) r[e] = load8_cached(pool + row[e]);
+#pragma unroll
+        for (int e = 0; e < TG_BATCH; ++e)
+          if (x0 + 256 * e < all) {
+            *reinterpret_cast<f32x4*>(staged + at[e]) = f32x4{r[e].v[0], r[e].v[1], r[e].v[2], r[e].v[3]};
+            *reinterpret_cast<f32x4*>(staged + at[e] + 4) = f32x4{r[e].v[4], r[e].v[5], r[e].v[6], r[e].v[7]};
+          }
       }
       __syncthreads();
       if (rw >= rows) continue;
-      float s[RW];
+      for (int t0 = s0; t0 < s0 + here; t0 += tokens) {
+        const float* tile = staged + (t0 - s0) * (w + 4);
+        float s[RW];
 #pragma unroll
-      for (int e = 0; e < RW; ++e) s[e] = 0.f;
-      for (int c = 4 * part; c < w; c += 4 * parts) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(tile + tok * (w + 4) + c);
+        for (int e = 0; e < RW; ++e) s[e] = 0.f;
+        for (int c = 4 * part; c < w; c += 4 * parts) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(tile + tok * (w + 4) + c);
+#pragma unroll
+          for (int e = 0; e < RW; ++e) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(q + e * w + c);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) s[e] = fmaf(x[z], y[z], s[e]);
+          }
+        }
+        const int t = t0 + tok, j = t - len.L;
 #pragma unroll
         for (int e = 0; e < RW; ++e) {
-          const f32x4 y = *reinterpret_cast<const f32x4*>(q + e * w + c);
+          for (int d = tokens; d < 64; d <<= 1) s[e] += __shfl_xor(s[e], d);
+          const bool sees = t < k1 && (j < 0 || ((bits[e] >> (j & 63)) & 1));
+          const float x = sees ? s[e] * a.scale_log2 : -INFINITY;
+          const float m_new = fmaxf(m[e], wave_max(x));
+          const float ref = m_new == -INFINITY ? 0.f : m_new;
+          const float alpha = exp2f(m[e] - ref), p = exp2f(x - ref);
+          l[e] = fmaf(l[e], alpha, wave_sum(part == 0 ? p : 0.f));
+          m[e] = m_new;
 #pragma unroll
-          for (int z = 0; z < 4; ++z) s[e] = fmaf(x[z], y[z], s[e]);
+          for (int d = 0; d < DC; ++d) acc[e][d] *= alpha;
+          if (part == 0) mine[tok * RW + e] = p;
         }
-      }
-      const int t = t0 + tok, j = t - len.L;
+        wave_lds_order();
+        // (tokens past the end have weight 0; of committed ones nothing is masked)
+        const int plain = min(len.L, k1) - t0;
+        for (int k = 0; k < tokens; k += TG_TOKENS * groups) {
+          Weights p[TG_TOKENS];
+          float x[TG_TOKENS][DC];
 #pragma unroll
-      for (int e = 0; e < RW; ++e) {
-        for (int d = tokens; d < 64; d <<= 1) s[e] += __shfl_xor(s[e], d);
-        const bool sees = t < k1 && (j < 0 || ((bits[e] >> (j & 63)) & 1));
-        const float x = sees ? s[e] * a.scale_log2 : -INFINITY;
-        const float m_new = fmaxf(m[e], wave_max(x));
-        const float ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = exp2f(m[e] - ref), p = exp2f(x - ref);
-        l[e] = fmaf(l[e], alpha, wave_sum(part == 0 ? p : 0.f));
-        m[e] = m_new;
+          for (int u = 0; u < TG_TOKENS; ++u) {
+            const int kk = k + u * groups + group;
+            p[u] = *reinterpret_cast<const Weights*>(mine + kk * RW);
 #pragma unroll
-        for (int d = 0; d < DC; ++d) acc[e][d] *= alpha;
-        if (part == 0) mine[tok * RW + e] = p;
-      }
-      wave_lds_order();
-      const int nt = min(tokens, k1 - t0);
-      for (int k = 0; k < nt; ++k) {
-        const f32x4 p = *reinterpret_cast<const f32x4*>(mine + k * RW);
+            for (int d = 0; d < DC; ++d) x[u][d] = tile[kk * (w + 4) + min(64 * d + col, w - 1)];
+          }
+          if (k + TG_TOKENS * groups <= plain) {
 #pragma unroll
-        for (int d = 0; d < DC; ++d) {
-          const float x = tile[k * (w + 4) + min(64 * d + lane, w - 1)];
+            for (int u = 0; u < TG_TOKENS; ++u)
 #pragma unroll
-          for (int e = 0; e < RW; ++e) acc[e][d] = p[e] != 0.f ? fmaf(p[e], x, acc[e][d]) : acc[e][d];
+              for (int d = 0; d < DC; ++d)
+#pragma unroll
+                for (int e = 0; e < RW; ++e) acc[e][d] = fmaf(p[u][e], x[u][d], acc[e][d]);
+          } else {
+#pragma unroll
+            for (int u = 0; u < TG_TOKENS; ++u)
+#pragma unroll
+              for (int d = 0; d < DC; ++d)
+#pragma unroll
+                for (int e = 0; e < RW; ++e) acc[e][d] = p[u][e] != 0.f ? fmaf(p[u][e], x[u][d], acc[e][d]) : acc[e][d];
+          }
         }
+        wave_lds_order();
       }
-      wave_lds_order();
     }
+#pragma unroll
+    for (int e = 0; e < RW; ++e)
+      for (int d = cols; d < 64; d <<= 1) acc[e][0] += __shfl_xor(acc[e][0], d);
   }
 #pragma unroll
   for (int e = 0; e < RW; ++e) {
@@ -125,7 +169,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
         if (64 * d + lane < a.dl) a.o_lat[out * a.dl + 64 * d + lane] = r < rows ? acc[e][d] * inv : 0.f;
       if (a.lse && lane == 0) a.lse[out] = r < rows ? merge_lse(m[e], l[e]) : -INFINITY;
     } else if (r < rows) {
-      const size_t slot = ((size_t)item * a.p.n_splits + blockIdx.y) * TREE_GENERIC_ROWS + (RW * wave + e);
+      const size_t slot = ((size_t)item * a.p.n_splits + blockIdx.y) * ROWS + (RW * wave + e);
 #pragma unroll
       for (int d = 0; d < DC; ++d)
         if (64 * d + lane < a.dl) a.part_acc[slot * a.dl + 64 * d + lane] = acc[e][d];
@@ -134,22 +178,25 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
   }
 }
 
-template <typename T>
+template <typename T, int RW>
 static int launch_generic(const TreeArgs& a, hipStream_t st) {
-  const int w = a.dl + a.d_r;
+  const int w = a.dl + a.d_r, rows = 4 * RW;
   int tokens = 64;
-  while (tokens > 4 && tg_floats(w, tokens) * 4 > TG_LDS) tokens /= 2;
-  const size_t lds = (size_t)tg_floats(w, tokens) * 4;
-  void (*fn)(TreeArgs, int) = a.dl <= 64 ? tree_generic_kernel<T, 1> : a.dl <= 256 ? tree_generic_kernel<T, 4> : tree_generic_kernel<T, TG_DIMS / 64>;
+  while (tokens > 4 && tg_floats(w, rows, tokens, tokens) * 4 > TG_LDS) tokens /= 2;
+  int stage = tokens;
+  while (stage < 256 && stage < a.p.split_tokens && tg_floats(w, rows, tokens, 2 * stage) * 4 <= TG_LDS) stage *= 2;
+  const size_t lds = (size_t)tg_floats(w, rows, tokens, stage) * 4;
+  void (*fn)(TreeArgs, int, int) = a.dl <= 64 ? tree_generic_kernel<T, 1, RW> : a.dl <= 256 ? tree_generic_kernel<T, 4, RW> : tree_generic_kernel<T, TG_DIMS / 64, RW>;
   const int rc = allow_lds(reinterpret_cast<const void*>(fn), 160 * 1024, "tree_generic_kernel");
   if (rc) return rc;
   const dim3 grid((unsigned)(a.n_shards * a.B * a.p.blocks), (unsigned)a.p.n_splits);
-  hipLaunchKernelGGL(fn, grid, dim3(256), lds, st, a, tokens);
+  hipLaunchKernelGGL(fn, grid, dim3(256), lds, st, a, tokens, stage);
   return check_launch("tree_generic_kernel");
 }
 
 int launch_tree_generic(const TreeArgs& a, int dtype, hipStream_t st) {
-  return dtype == TPLA_F32 ? launch_generic<float>(a, st) : launch_generic<bf16_t>(a, st);
+  if (a.p.block == 4) return dtype == TPLA_F32 ? launch_generic<float, 1>(a, st) : launch_generic<bf16_t, 1>(a, st);
+  return dtype == TPLA_F32 ? launch_generic<float, 4>(a, st) : launch_generic<bf16_t, 4>(a, st);
 }
 
 // Merge: a wave takes one row after another of an item, MERGE_LOADS slots' rows on their way together, the first of them requested with their references
@@ -228,7 +275,7 @@ int launch_tree_merge(const TreeArgs& a, hipStream_t st) {
   // one row per wave while that leaves no more than some workgroups per compute unit
   const int rows = a.T * a.H, n_v = a.n_shards * a.B;
   int group = 4;
-  while (group < 16 && (long long)((rows + group - 1) / group) * n_v > 16LL * device_cu_count()) group *= 2;
+  while (group < 16 && group < a.p.block && (long long)((rows + group - 1) / group) * n_v > 16LL * device_cu_count()) group *= 2;
   hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((rows + group - 1) / group), (unsigned)n_v), dim3(256), 0, st, a, group);
   return check_launch("tree_merge_kernel");
 }

@@ -632,6 +632,8 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
   constexpr int RC = Tile::RC, CPT = Tile::CPT, NSTAGE = Tile::NSTAGE;
   constexpr int KS = (DL + 64) / 32, DB = DL / 16, NQ = 2 * KS;
   constexpr int KRING = 6, VRING = 4, TEAM = TP_NW / TEAMS;
+  // streaming, not kept in L2, where no other row block reads these rows (32 x 32768 tokens, 64 rows: 284 -> 271 us with merge and combine)
+  constexpr int STREAM = TEAMS == 2 ? 2 : 0;
   extern __shared__ u32x4 smem[];
   char* const lds = reinterpret_cast<char*>(smem);
   const unsigned lds_base = lds_at(lds);
@@ -680,7 +682,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
 #pragma unroll
         for (int j = 0; j < CPT; ++j)
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + ld_at[j]),
-                                           (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, 2 /* streaming: not kept in L2 */);
+                                           (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, STREAM);
       } else {
         // rows of several pages, or past the end: those repeat the last token (and are masked)
 #pragma unroll 1
@@ -689,7 +691,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
           const int row_id = (int)lds_read_id(id_at(p));
           const char* src = pool + ((size_t)row_id * pt + (k - p * pt)) * (RC * 16) + ((x % RC) ^ swz(tok)) * 16;
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                           (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, 2 /* streaming: not kept in L2 */);
+                                           (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, STREAM);
         }
       }
       const int c = p0 / TR_IDS;
@@ -865,35 +867,35 @@ bool tree_mfma_supported(const tpla_shape_t& sh) {
   return sh.dtype == TPLA_BF16 && sh.d_r == 64 && (dl == 64 || dl == 128 || dl == 256 || dl == 512);
 }
 
-// Blocks of 16 rows per wave: the fewest tiles weighted by what one takes, 0.45 + 0.48 RB (16 sequences of 32768 tokens, 64 heads, us per tile and
-// workgroup: 1 block 0.91, 2 1.26, 3 1.74).  us by this number of blocks: 192 rows 294 / 232 / 199 (32 x 8192), 256 rows 145 / 128 / 151 (32 x 4096),
-// 512 rows 257 / 208 / 226 (16 x 8192), 1024 rows 1832 / 1335 / 1334 (16 x 32768).
-static int row_blocks(int dl, int rows) {
-  const int most = dl == 512 ? 1 : dl == 256 ? 3 : 4;
-  int best = 1;
-  double least = 1e30;
-  for (int rb = 1; rb <= most; ++rb) {
-    if (rb == 3 && dl != 256) continue;              // no such kernel
-    const double t = (double)((rows + 64 * rb - 1) / (64 * rb)) * (0.45 + 0.48 * rb);
-    if (t < least) {
-      least = t;
-      best = rb;
+// The kernel and the rows of an item, from the rows R of a sequence and the 32-token tiles of 64 rows per compute unit (by the block table's width:
+// the host does not know the lengths).  Medians of 8 calls with their merge, us, over batches of 1 to 64 sequences of 300 to 32768 tokens
+// (lengths from two thirds of that on):
+//   little work: 64 rows on 4 waves (A).  More workgroups, shorter prologues, smaller partial results.  256-wide, 16 x 1237 tokens: R = 128 A 34.5,
+//     128 rows on 8 waves (B) 42.8, 192 rows (C) 46; R = 256 44.4 / 50 / 54; R = 512 (39 tiles) 67 / 64 / 71; one sequence of 1237, R = 1664 37.4 / 37.6 / 40.4
+//   up to 64 rows: two teams of 4 waves (D).  64 x 8192 tokens, R = 48 to 64: 256-wide A 129.7, D 127; 128-wide 187 / 177; 64-wide 313 / 273
+//   more: B, or C (256 rows of narrower slices) where its blocks are filled and long enough.  256-wide: R = 80, 64 x 8192: B 166, C 206; R = 192 317 / 235; 16 x
+//     4096: R = 192 66 / 71, R = 512 112 / 117, R = 1024 197 / 189.  128-wide, 64 x 2048: R = 256 155 / 154, 384 212 / 243, 1024 518 / 471; 64-wide 829 / 724.
+// Per tile C takes 1.38 (256-wide) and 1.8 (narrower) times what B takes.  (128 rows on 4 waves are within 4 % of B below 256 rows, up to 13 % slower above,
+// and were not kept.)  512-wide slices have A alone: the accumulators of more rows do not fit.
+void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p) {
+  const int dl = sh.d_c / sh.g, rows = T * sh.H, large = dl == 256 ? 192 : 256, cus = device_cu_count();
+  const double tiles = std::max(((double)max_pages * sh.page_tokens + TR_TOK - 1) / TR_TOK, 1.0), per_row_block = (double)n_shards * sh.B * tiles / cus;
+  const auto blocks = [&](int of) { return (rows + of - 1) / of; };
+  p->mfma = 1;
+  p->teams = 0;
+  p->block = 64;
+  if (dl < 512 && per_row_block * blocks(64) >= 32) {
+    p->teams = rows <= 64 ? 2 : 1;
+    p->block = 128 / p->teams;
+    if (rows > 128 && per_row_block * blocks(large) >= 24 && blocks(large) * (dl == 256 ? 1.38 : 1.8) < blocks(128)) {
+      p->teams = 0;
+      p->block = large;
     }
   }
-  return best;
-}
-
-void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p) {
-  const int dl = sh.d_c / sh.g;
-  p->mfma = 1;
-  p->teams = dl == 512 ? 0 : T * sh.H <= 64 ? 2 : T * sh.H <= 128 ? 1 : 0;
-  p->block = p->teams ? 128 / p->teams : 64 * row_blocks(dl, T * sh.H);
-  p->blocks = (T * sh.H + p->block - 1) / p->block;
-  const double tiles = ((double)max_pages * sh.page_tokens + TR_TOK - 1) / TR_TOK;
-  const double most = (double)n_shards * sh.B * p->blocks * std::max(tiles, 1.0);
-  p->n_wg = (int)std::min((double)device_cu_count(), most);
+  p->blocks = blocks(p->block);
+  p->n_wg = (int)std::min((double)cus, (double)n_shards * sh.B * p->blocks * tiles);
   p->n_splits = 1;
-  p->split_tokens = p->teams ? 2 : 4;         // fewest units of a range
+  p->split_tokens = 4;         // fewest units of a range: a partial result costs as much as some (one user of 1237 tokens, R = 64: 4 tiles 21 us, 8 25)
 }
 
 template <int DL, int RB, int QL = 0>
@@ -930,13 +932,10 @@ int launch_tree_mfma(const TreeArgs& a, hipStream_t st) {
   }
   switch (a.dl * 8 + a.p.block / 64) {
     case 64 * 8 + 1: return launch_tree<64, 1>(a, st);
-    case 64 * 8 + 2: return launch_tree<64, 2>(a, st);
     case 64 * 8 + 4: return launch_tree<64, 4, 1>(a, st);
     case 128 * 8 + 1: return launch_tree<128, 1>(a, st);
-    case 128 * 8 + 2: return launch_tree<128, 2>(a, st);
     case 128 * 8 + 4: return launch_tree<128, 4, 3>(a, st);
     case 256 * 8 + 1: return launch_tree<256, 1>(a, st);
-    case 256 * 8 + 2: return launch_tree<256, 2>(a, st);
     case 256 * 8 + 3: return launch_tree<256, 3, 2>(a, st);
     case 512 * 8 + 1: return launch_tree<512, 1>(a, st);
   }

@@ -11,6 +11,10 @@ from draft_common import TreeProblem, assert_close, chain_masks, out_buffers, ru
 pytestmark = pytest.mark.gpu
 
 
+# Which kernel a call takes depends on the rows of a sequence and on the width of the block table: a wide one is work for all of the chip.
+WIDE = 1 << 17
+
+
 @pytest.mark.parametrize("dtype,dl,g,H,T,lens,drafts,pt", [
     ("bf16", 256, 2, 16, 4, [130, 1, 64, 0, 1000], [4, 1, 3, 2, 4], 64),
     ("bf16", 256, 2, 64, 3, [33, 500], [3, 2], 64),                  # 192 rows
@@ -28,7 +32,10 @@ pytestmark = pytest.mark.gpu
     ("bf16", 512, 1, 64, 2, [64, 31], [2, 1], 16),
     ("bf16", 72, 2, 6, 5, [70, 3], [5, 4], 16),                      # a width of the general kernel
     ("f32", 32, 2, 4, 5, [128, 60, 0], [5, 3, 2], 64),
+    ("f32", 8, 2, 3, 2, [70, 1], [2, 1], 64),                        # eight columns
+    ("f32", 16, 2, 3, 2, [70, 1], [2, 1], 64),
     ("f32", 256, 2, 3, 6, [900, 1], [6, 6], 64),
+    ("f32", 64, 8, 64, 16, [90, 33], [16, 16], 64),                  # enough rows for four per wave
     ("f32", 1024, 1, 2, 3, [65], [3], 16),
 ])
 def test_against_the_definition(dtype, dl, g, H, T, lens, drafts, pt):
@@ -38,14 +45,39 @@ def test_against_the_definition(dtype, dl, g, H, T, lens, drafts, pt):
     assert_close(p, *run_all(p))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_empty_masks_and_drafts_that_do_not_exist(dtype):
+@pytest.mark.parametrize("dl,g,H,T,lens,drafts,pt", [
+    # up to 64 rows: two teams
+    (256, 2, 16, 4, [130, 1, 64, 0, 1000], [4, 1, 3, 2, 4], 64),
+    (256, 2, 5, 7, [31, 62, 640], [7, 1, 5], 16),
+    (256, 1, 16, 2, [700, 77, 64, 63], [2, 2, 1, 2], 1),
+    (256, 1, 64, 1, [1500, 300, 32, 96], [1, 1, 1, 1], 3),
+    (128, 4, 16, 3, [300, 65, 4000], [3, 1, 2], 32), (64, 8, 64, 1, [257, 40], [1, 1], 64),
+    # up to 128 rows, and several blocks of 128
+    (256, 2, 16, 5, [130, 1, 64, 0, 1000], [5, 1, 3, 2, 4], 64), (256, 1, 64, 4, [95, 96, 97, 31], [4, 3, 2, 4], 128),
+    (256, 1, 16, 6, [700, 77], [6, 2], 1), (128, 2, 64, 2, [300, 65, 2500], [2, 1, 2], 16), (64, 4, 16, 8, [64, 63, 513], [8, 7, 8], 64),
+    (128, 1, 64, 6, [333], [5], 64),
+    # 192 rows (256-wide), 256 rows (narrower)
+    (256, 2, 64, 3, [33, 500, 0, 1], [3, 2, 3, 1], 64), (256, 1, 64, 12, [95, 1200], [12, 7], 16), (256, 1, 24, 8, [64, 900, 32], [8, 8, 1], 3),
+    (256, 1, 64, 3, [6000, 65], [3, 3], 64), (256, 1, 64, 3, [200, 90], [3, 2], 1),
+    (128, 2, 64, 4, [300, 65, 31, 32], [4, 4, 1, 3], 64), (128, 1, 64, 16, [700, 3], [16, 11], 32),
+    (64, 2, 64, 4, [257, 40], [4, 2], 64), (64, 1, 32, 16, [5, 1000], [16, 9], 16),
+    # 512-wide slices
+    (512, 1, 64, 2, [64, 31, 3000], [2, 1, 2], 64),
+])
+def test_against_the_definition_over_wide_tables(dl, g, H, T, lens, drafts, pt):
+    print("tree, wide table", dl, g, H, T, lens, drafts, pt, flush=True)
+    p = TreeProblem(lens, drafts, T, H=H, g=g, dl=dl, pt=pt, seed=dl + H + T, max_pages=WIDE)
+    assert_close(p, *run_all(p))
+
+
+@pytest.mark.parametrize("dtype,H,wide", [("bf16", 16, None), ("f32", 16, None), ("bf16", 16, WIDE), ("bf16", 32, WIDE), ("bf16", 48, WIDE)])
+def test_empty_masks_and_drafts_that_do_not_exist(dtype, H, wide):
     lens, drafts, T = [0, 0, 70, 5], [3, 0, 4, 2], 4
     masks = np.zeros((4, T), dtype=np.uint64)
     masks[0] = [0, 2, 4, 0]                                  # draft 0 of an empty sequence sees nothing
     masks[2] = [0, np.uint64(0xFFFFFFFFFFFFFFFF), 1, 8]      # bits beyond the drafts are ignored
     masks[3] = [np.uint64(1) << np.uint64(63), 3, 3, 3]
-    p = TreeProblem(lens, drafts, T, masks=masks, dtype=dtype, seed=5)
+    p = TreeProblem(lens, drafts, T, H=H, masks=masks, dtype=dtype, seed=5, max_pages=wide)
     o, lse = run_all(p)
     assert_close(p, o, lse)
     assert (o[:, 0, 0] == 0).all() and (lse[:, 0, 0] == -np.inf).all()
@@ -53,11 +85,11 @@ def test_empty_masks_and_drafts_that_do_not_exist(dtype):
     assert (o[:, 3, 2:] == 0).all() and (lse[:, 3, 2:] == -np.inf).all()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype,H,wide", [("bf16", 16, None), ("f32", 16, None), ("bf16", 8, WIDE), ("bf16", 16, WIDE), ("bf16", 32, WIDE)])
 @pytest.mark.parametrize("L", [0, 50, 64, 95])
-def test_what_a_masked_draft_holds_reaches_nobody_else(dtype, L):
+def test_what_a_masked_draft_holds_reaches_nobody_else(dtype, H, wide, L):
     T = 6
-    p = TreeProblem([L, 40], [T, T], T, masks=chain_masks(2, T), dtype=dtype, seed=7)
+    p = TreeProblem([L, 40], [T, T], T, H=H, masks=chain_masks(2, T), dtype=dtype, seed=7, max_pages=wide)
     p.masks[0] = [1, 2, 5, 9, 17, 33]                        # draft 1 is seen by itself alone
     clean = p.expected()
     nan, inf = (np.float32("nan"), np.float32("inf")) if dtype == "f32" else (0x7FC0, 0x7F80)
@@ -82,8 +114,9 @@ def test_a_committed_row_that_is_not_a_number_is_seen_by_all_of_its_sequence():
     assert_close(p, o, lse, clean)
 
 
-def test_large_and_lowest_scores():
-    p = TreeProblem([200], [3], 3, seed=9)
+@pytest.mark.parametrize("H,wide", [(16, None), (16, WIDE), (40, WIDE), (64, WIDE)])
+def test_a_reference_that_moves(H, wide):
+    p = TreeProblem([200], [3], 3, H=H, seed=9, max_pages=wide)
     p.q_lat = wl.to_storage(wl.as_f64(p.q_lat, "bf16") * 400.0, "bf16")    # a few tokens carry everything, the reference moves
     assert_close(p, *run_all(p))
 
@@ -122,14 +155,16 @@ def test_no_draft_lengths_means_all():
     assert_close(p, *run_all(p, drafts=None))
 
 
-@pytest.mark.parametrize("H,T,lens", [(16, 2, [9000, 40, 3000]), (64, 4, [5003, 1200]), (64, 16, [700, 3000]), (16, 1, [20000])])
-def test_long_contexts_are_cut_and_joined(H, T, lens):
-    p = TreeProblem(lens, [T] * len(lens), T, H=H, g=1, seed=12)
+@pytest.mark.parametrize("wide", [None, WIDE])
+@pytest.mark.parametrize("H,T,lens", [(16, 2, [9000, 40, 3000]), (64, 4, [5003, 1200]), (64, 16, [700, 3000]), (16, 1, [20000]), (64, 3, [4000])])
+def test_long_contexts_are_cut_and_joined(H, T, lens, wide):
+    p = TreeProblem(lens, [T] * len(lens), T, H=H, g=1, seed=12, max_pages=wide)
     assert_close(p, *run_all(p))
 
 
-def test_same_bits_every_time_and_on_another_stream():
-    p = TreeProblem([3000, 77, 512], [6, 2, 5], 6, H=32, seed=13)
+@pytest.mark.parametrize("H,wide", [(32, None), (8, WIDE), (20, WIDE), (32, WIDE)])
+def test_same_bits_every_time_and_on_another_stream(H, wide):
+    p = TreeProblem([3000, 77, 512], [6, 2, 5], 6, H=H, seed=13, max_pages=wide)
     d = p.device()
     a = run_all(p, d)
     b = run_all(p, d)
