@@ -415,8 +415,9 @@ int tpla_validate_block_table(const tpla_shape_t* shape, const int32_t* block_ta
  * ---- Speculative decode: several drafted tokens per sequence and step ----
  * Drafts are written to the cache behind the committed tokens (tpla_extend_sequences gives pages, slots and positions,
  * tpla_apply_rotary turns queries and keys, tpla_append_token_sliced with B T rows writes), attended to in one pass
- * (tpla_decode_shards_tree), and the accepted ones are moved together (tpla_commit_drafts).  Nothing here needs the host
- * between two steps; every call can be captured into a graph.
+ * (tpla_decode_shards_tree), and the accepted ones are moved together (tpla_commit_drafts).  No call waits for the host or
+ * allocates, so each can be captured into a graph; calls that share a workspace, or whose outputs others read, follow each
+ * other on one stream.
  */
 
 /*
@@ -432,10 +433,12 @@ int tpla_validate_block_table(const tpla_shape_t* shape, const int32_t* block_ta
  * at cu_tokens[b] .. cu_tokens[b + 1] - 1; n_tokens is the room in slots and positions, entries behind the last token get
  * slot -1 and position 0.  row_tokens > 0: token i of b is at b * row_tokens + i, add_lens is clipped to row_tokens, the
  * rest of a row gets slot -1 and position 0, n_tokens = B * row_tokens.  cu_tokens int32 [B + 1] is the prefix sum of
- * add_lens either way, clipped to n_tokens.  counts int32 [2]: pages taken from the front of free_pages, pages that were
- * missing.  Negative lengths count as 0, lengths beyond the row as the row's.  pages_held_out may be pages_held.  All
- * pointers but counts' meaning above are int32 DEVICE arrays; depths [B, row_tokens] or NULL; free_pages may be NULL with
- * n_free = 0.  Only shape->B and page_tokens are read (the shape is checked whole).
+ * add_lens either way, clipped to n_tokens.  counts int32 [2]: pages taken from the front of free_pages (the caller's next
+ * list begins behind them), pages that were missing.  A sequence keeps the pages of rejected drafts and uses them first.
+ * Negative lengths count as 0, lengths beyond the row as the row's.  pages_held_out may be pages_held (for more than 1024
+ * tokens a separate array saves a launch); no other overlap.  All pointers are int32 DEVICE arrays; depths
+ * [B, row_tokens] or NULL; free_pages may be NULL with n_free = 0.  Only shape->B and page_tokens are read (the shape is
+ * checked whole).
  */
 int tpla_extend_sequences(const tpla_shape_t* shape, const int32_t* seq_lens, const int32_t* add_lens, int32_t row_tokens,
                           const int32_t* depths, const int32_t* free_pages, int32_t n_free, const int32_t* pages_held,

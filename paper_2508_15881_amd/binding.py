@@ -376,25 +376,29 @@ def tpla_rotary_frequencies(rot_dim, base=10000.0, factor=1.0, original_position
     return freq
 
 
-def _view(x, dims):
-    """Address and the strides (in elements) of a tensor whose innermost dimension is dense."""
-    if x is None:
-        return (None,) + (0,) * (dims - 1)
-    if x.dim() != dims or (x.shape[-1] > 1 and x.stride(-1) != 1):
-        raise ValueError("libtpla needs a tensor of %d dimensions, the innermost one dense" % dims)
-    return (x.data_ptr(),) + x.stride()[:-1]
+def _view(x, shape):
+    """Address and strides (in elements) of a tensor of this shape whose innermost dimension is dense."""
+    strides = x.stride() if x is not None else ()
+    if not strides or x.shape != shape or strides[-1] != 1:
+        raise ValueError("libtpla needs a tensor of shape %r, the innermost dimension dense" % (shape,))
+    return x.data_ptr(), strides
 
 
 def tpla_apply_rotary(shape, layout, inverse, rot_dim, freq, amplitude, positions, T, q, q_out, k, k_out, stream=None):
     """q, q_out [T, H, d_r] and k, k_out [T, d_r] may be views (a part of a wider projection): their strides, which the C
     call takes after each pointer, are read off the tensors.  q (with q_out) or k (with k_out) may be None."""
-    for x, y, want in ((q, q_out, (T, shape.H, shape.d_r)), (k, k_out, (T, shape.d_r))):
-        for z in (x, y):
-            if z is not None and tuple(z.shape) != want:
-                raise ValueError("libtpla needs a tensor of shape %r, got %r" % (want, tuple(z.shape)))
+    qp = qop = kp = kop = None
+    qs = qos = (0, 0)
+    ks = kos = (0,)
+    if q is not None or q_out is not None:
+        rows = (T, shape.H, shape.d_r)
+        (qp, qs), (qop, qos) = _view(q, rows), _view(q_out, rows)
+    if k is not None or k_out is not None:
+        rows = (T, shape.d_r)
+        (kp, ks), (kop, kos) = _view(k, rows), _view(k_out, rows)
     _check(load_library().tpla_apply_rotary(
-        ctypes.byref(shape), layout, inverse, rot_dim, _ptr(freq), amplitude, _ptr(positions), T, *_view(q, 3), *_view(q_out, 3),
-        *_view(k, 2), *_view(k_out, 2), _stream(stream)))
+        ctypes.byref(shape), layout, inverse, rot_dim, _ptr(freq), amplitude, _ptr(positions), T, qp, qs[0], qs[1], qop, qos[0],
+        qos[1], kp, ks[0], kop, kos[0], _stream(stream)))
 
 
 def tpla_workspace_bytes_tree(shape, T, max_pages_per_seq):

@@ -116,6 +116,70 @@ class DecodeStep:
         return graph
 
 
+def tree_masks(parents):
+    """Masks and depths of draft trees on the host: parents int [.., T], parents[.., t] < t the draft that t continues,
+    -1 where it continues the committed tokens.  Returns (masks uint64, depths int32) of the same shape: a draft sees what
+    its parent sees, and itself."""
+    parents = np.asarray(parents)
+    masks, depths = np.zeros(parents.shape, dtype=np.uint64), np.zeros(parents.shape, dtype=np.int32)
+    for t in range(parents.shape[-1]):
+        p = parents[..., t]
+        if np.any(p >= t) or np.any(p < -1):
+            raise ValueError("a draft's parent comes before it")
+        has, at = p >= 0, np.maximum(p, 0)[..., None]
+        masks[..., t] = np.where(has, np.take_along_axis(masks, at, -1)[..., 0], np.uint64(0)) | (np.uint64(1) << np.uint64(t))
+        depths[..., t] = np.where(has, np.take_along_axis(depths, at, -1)[..., 0] + 1, 0)
+    return masks, depths
+
+
+class DraftStep:
+    """Buffers and call order of one speculative layer-step: T drafted tokens per sequence get pages, slots and positions,
+    are rotated, written to the slice caches and attended to in one pass; later the accepted ones are committed."""
+
+    def __init__(self, shape, T, max_pages_per_seq, frequencies, layout=B.TPLA_ROTARY_INTERLEAVED, amplitude=1.0, device="cuda"):
+        self.shape, self.T, self.max_pages = shape, int(T), int(max_pages_per_seq)
+        self.layout, self.amplitude = layout, float(amplitude)
+        self.rows = B.TplaShape.from_buffer_copy(shape)     # B T tokens for the calls that take one row each
+        self.rows.B = shape.B * self.T
+        self.freq = torch.as_tensor(frequencies, dtype=torch.float64).to(device)
+        st = torch_dtype(shape.dtype)
+        g, Bn, H, dl, n = shape.g, shape.B, shape.H, shape.d_c // shape.g, shape.B * self.T
+        ints = lambda k: torch.zeros(k, dtype=torch.int32, device=device)  # noqa: E731
+        self.slots, self.positions, self.cu, self.counts = ints(n), ints(n), ints(Bn + 1), ints(2)
+        self.q_pe = torch.empty((n, H, shape.d_r), dtype=st, device=device)
+        self.k_pe = torch.empty((n, shape.d_r), dtype=st, device=device)
+        self.q_lat = torch.empty((g, Bn, self.T, H, dl), dtype=st, device=device)
+        self.o_lat = torch.empty((g, Bn, self.T, H, dl), dtype=torch.float32, device=device)
+        self.lse = torch.empty((g, Bn, self.T, H), dtype=torch.float32, device=device)
+        self.o = torch.empty((Bn, self.T, H, shape.d_v), dtype=st, device=device)
+        self.ws_bytes = B.tpla_workspace_bytes_tree(shape, self.T, self.max_pages)
+        if self.ws_bytes == 0:
+            raise B.TplaError(-2, B.tpla_last_error())
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+
+    def place(self, seq_lens, draft_lens, depths, free_pages, n_free, pages_held, block_table):
+        """Pages, slots and positions of the drafts (once per step, for all layers); pages_held is updated."""
+        B.tpla_extend_sequences(self.shape, seq_lens, draft_lens, self.T, depths, free_pages, n_free, pages_held, pages_held, block_table,
+                                self.max_pages, self.cu, self.slots, self.positions, self.slots.numel(), self.counts)
+
+    def run(self, q_nope, q_pe, c_t, k_pe, W_UK_t, W_UV_t, shard_pools, block_table, seq_lens, draft_lens, masks, mu=None, alpha=None,
+            rms_eps=1e-6):
+        """q_nope [B, T, H, d_n], q_pe [B T, H, d_r] and k_pe [B T, d_r] before rotation (views of a projection will do), c_t
+        [B, T, d_c] the drafts' latents in the basis of the caches.  Returns o [B, T, H, d_v] in the storage type."""
+        B.tpla_apply_rotary(self.shape, self.layout, 0, 2 * self.freq.numel(), self.freq, self.amplitude, self.positions, self.rows.B,
+                            q_pe, self.q_pe, k_pe, self.k_pe)
+        B.tpla_append_token_sliced(self.rows, c_t, self.k_pe, alpha, rms_eps, self.slots, shard_pools)
+        B.tpla_absorb_query(self.rows, q_nope, W_UK_t, mu, self.q_lat)
+        B.tpla_decode_shards_tree_combine(self.shape, self.T, self.q_lat, self.q_pe, shard_pools, block_table, self.max_pages, seq_lens,
+                                          draft_lens, masks, self.workspace, self.ws_bytes, W_UV_t, self.o, self.shape.dtype, self.o_lat,
+                                          self.lse)
+        return self.o
+
+    def commit(self, accepted, n_accepted, seq_lens, new_lens, block_table, shard_pools):
+        """Accepted drafts' rows behind the committed ones (per layer); new_lens may be seq_lens where one layer is all."""
+        B.tpla_commit_drafts(self.shape, self.T, accepted, n_accepted, seq_lens, block_table, self.max_pages, shard_pools, new_lens)
+
+
 def transform_weights(shape, mode, signs, U, W_UK, W_UV):
     """W_UK [H,d_n,d_c] -> W_UK U (last axis); W_UV [H,d_c,d_v] -> U^T W_UV (middle axis)."""
     W_UK_t = torch.empty_like(W_UK)

@@ -131,3 +131,14 @@ def test_rotary_frequencies():
         with pytest.raises(tp.TplaError) as e:
             tp.tpla_rotary_frequencies(**bad)
         assert e.value.code == -2
+
+
+def test_tree_masks():
+    from paper_2508_15881_amd import pipeline as pl
+    masks, depths = pl.tree_masks([-1, 0, 0, 1, -1])
+    assert masks.tolist() == [1, 3, 5, 11, 16] and depths.tolist() == [0, 1, 1, 2, 0]
+    masks, depths = pl.tree_masks(np.stack([np.arange(-1, 63), np.full(64, -1)]))
+    assert masks[0, 63] == 2 ** 64 - 1 and masks[1, 63] == 2 ** 63 and depths[0].tolist() == list(range(64)) and not depths[1].any()
+    for bad in ([0], [-1, 1], [-1, -2]):
+        with pytest.raises(ValueError):
+            pl.tree_masks(bad)
