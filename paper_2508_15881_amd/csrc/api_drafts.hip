@@ -60,7 +60,7 @@ static int check_tree(const tpla_shape_t* sh, int n_shards, int32_t T, int32_t m
     return fail(TPLA_ERR_UNSUPPORTED, "d_c/g=%d above 1024, or d_c/g + d_r=%d above 1984", dl, dl + sh->d_r);
   *p = plan_tree(*sh, n_shards, T, max_pages);
   const double tiles = ((double)max_pages * sh->page_tokens + 31) / 32, items = (double)n_shards * sh->B * p->blocks;
-  if (p->mfma ? items * tiles >= 2147483647.0 : items * p->n_splits >= 2147483647.0 || p->n_splits > 65535)
+  if (p->mfma ? items * (tiles + 8) >= 2147483647.0 : items * p->n_splits >= 2147483647.0 || p->n_splits > 65535)
     return fail(TPLA_ERR_UNSUPPORTED, "n_shards * B * row blocks * max_pages_per_seq too large");
   return TPLA_OK;
 }

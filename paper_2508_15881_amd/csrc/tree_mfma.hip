@@ -79,26 +79,28 @@ __device__ __forceinline__ int tree_prefix(int v) {      // inclusive sum over t
   }
   return v;
 }
-// Units of sequence b (`unit` tokens of one row block): row blocks x units of its tokens; none without drafts.
+// Units of sequence b: `unit` tokens of one row block are a tile, and an item is its tiles behind START units that hold none.
+// Those stand for what an item costs a workgroup besides its tiles (its queries, the first tiles' way from memory, its result),
+// so that ranges with many short items end with the others.
 struct TreeUnits {
   TreeLens len;
-  int tiles, units;
+  int tiles, blocks;           // no drafts: none
 };
 __device__ __forceinline__ TreeUnits tree_units(const TreeArgs& a, int unit, int b) {
   TreeUnits r;
   if (b >= a.B) {
     r.len = TreeLens{0, 0, 0};
-    r.tiles = r.units = 0;
+    r.tiles = r.blocks = 0;
     return r;
   }
   r.len = tree_lens(a, b);
   r.tiles = r.len.n > 0 ? max((r.len.keys + unit - 1) / unit, 1) : 0;
-  r.units = r.tiles * ((r.len.n * a.H + a.p.block - 1) / a.p.block);
+  r.blocks = (r.len.n * a.H + a.p.block - 1) / a.p.block;
   return r;
 }
 
 // The range of units of this workgroup, [pos, end), and the item that unit `pos` lies in.
-template <int UNIT>
+template <int UNIT, int START>
 struct TreeWalk {
   TreeUnits front;             // the first 64 sequences stay in the lanes: a search among them loads nothing
   int front_incl, per_slice, units, n_wg, w, pos, range0, end;
@@ -106,56 +108,71 @@ struct TreeWalk {
   int i, b, v, item, rb, rows, L, keys, tiles, t0, t1, slot;
   bool whole;
 
+  static __device__ __forceinline__ int units_of(const TreeUnits& u) { return u.blocks * (u.tiles + START); }
   __device__ __forceinline__ bool begin(const TreeArgs& a) {
     const int lane = threadIdx.x & 63;
     front = tree_units(a, UNIT, lane);
-    front_incl = tree_prefix(front.units);
+    front_incl = tree_prefix(units_of(front));
     per_slice = __builtin_amdgcn_readlane(front_incl, 63);
-    for (int b0 = 64; b0 < a.B; b0 += 64) per_slice += __builtin_amdgcn_readlane(tree_prefix(tree_units(a, UNIT, b0 + lane).units), 63);
+    int tiles_all = __builtin_amdgcn_readlane(tree_prefix(front.blocks * front.tiles), 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) {
+      const TreeUnits u = tree_units(a, UNIT, b0 + lane);
+      per_slice += __builtin_amdgcn_readlane(tree_prefix(units_of(u)), 63);
+      tiles_all += __builtin_amdgcn_readlane(tree_prefix(u.blocks * u.tiles), 63);
+    }
     units = per_slice * a.n_shards;
-    n_wg = max(1, min(a.p.n_wg, units / a.p.split_tokens));             // no shorter ranges than pay
+    n_wg = max(1, min(a.p.n_wg, tiles_all * a.n_shards / a.p.split_tokens));             // no shorter ranges than pay
     // ranges that lie side by side (the row blocks of a sequence, which read the same pages) on one XCD: workgroups go to the eight in turn
     w = n_wg % 8 == 0 ? (blockIdx.x & 7) * (n_wg >> 3) + (blockIdx.x >> 3) : blockIdx.x;
     if ((int)blockIdx.x >= n_wg || units == 0) return false;
     range0 = pos = tree_start(n_wg, units, w);
     end = tree_start(n_wg, units, w + 1);
-    return pos < end;
+    return true;
   }
-  __device__ __forceinline__ void find(const TreeArgs& a) {
+  // The next item with tiles in the range; false: there is none.
+  __device__ __forceinline__ bool find(const TreeArgs& a) {
     const int lane = threadIdx.x & 63;
-    i = pos / per_slice;
-    const int rem = pos - i * per_slice;
-    b = 0;
-    TreeUnits u = front;
-    int incl = front_incl;
-    unsigned long long past = __ballot(incl > rem);
-    while (past == 0) {                              // ends: rem lies below the sum over all sequences
-      b += 64;
-      const int base = __builtin_amdgcn_readlane(incl, 63);
-      u = tree_units(a, UNIT, b + lane);
-      incl = tree_prefix(u.units) + base;
-      past = __ballot(incl > rem);
+    while (pos < end) {
+      i = pos / per_slice;
+      const int rem = pos - i * per_slice;
+      b = 0;
+      TreeUnits u = front;
+      int incl = front_incl;
+      unsigned long long past = __ballot(incl > rem);
+      while (past == 0) {                            // ends: rem lies below the sum over all sequences
+        b += 64;
+        const int base = __builtin_amdgcn_readlane(incl, 63);
+        u = tree_units(a, UNIT, b + lane);
+        incl = tree_prefix(units_of(u)) + base;
+        past = __ballot(incl > rem);
+      }
+      const int src = __builtin_ctzll(past);
+      b += src;
+      const int before = __builtin_amdgcn_readlane(incl - units_of(u), src);
+      tiles = __builtin_amdgcn_readlane(u.tiles, src);
+      const int span = tiles + START;
+      rb = (rem - before) / span;
+      const int at = rem - before - rb * span, stop = min(span, at + (end - pos));
+      t0 = max(at - START, 0);
+      t1 = stop - START;
+      const int first = pos;
+      pos += stop - at;
+      if (t1 <= t0) continue;                        // the range ends before the item's first tile
+      L = __builtin_amdgcn_readlane(u.len.L, src);
+      keys = __builtin_amdgcn_readlane(u.len.keys, src);
+      rows = __builtin_amdgcn_readlane(u.len.n, src) * a.H;
+      v = i * a.B + b;
+      item = v * a.p.blocks + rb;
+      whole = t0 == 0 && t1 == tiles;
+      slot = 2 * w + (first == range0 ? 0 : 1);
+      if (t0 == 0 && threadIdx.x == 0) {
+        a.plan[3 * item] = w;
+        a.plan[3 * item + 1] = tree_owner(n_wg, units, first - at + span - 1) - w + 1;
+        a.plan[3 * item + 2] = slot & 1;
+      }
+      return true;
     }
-    const int src = __builtin_ctzll(past);
-    b += src;
-    const int before = __builtin_amdgcn_readlane(incl - u.units, src);
-    tiles = __builtin_amdgcn_readlane(u.tiles, src);
-    L = __builtin_amdgcn_readlane(u.len.L, src);
-    keys = __builtin_amdgcn_readlane(u.len.keys, src);
-    rows = __builtin_amdgcn_readlane(u.len.n, src) * a.H;
-    rb = (rem - before) / tiles;
-    t0 = rem - before - rb * tiles;
-    t1 = min(tiles, t0 + (end - pos));
-    v = i * a.B + b;
-    item = v * a.p.blocks + rb;
-    whole = t0 == 0 && t1 == tiles;
-    slot = 2 * w + (pos == range0 ? 0 : 1);
-    if (t0 == 0 && threadIdx.x == 0) {
-      a.plan[3 * item] = w;
-      a.plan[3 * item + 1] = tree_owner(n_wg, units, pos + tiles - 1) - w + 1;
-      a.plan[3 * item + 2] = slot & 1;
-    }
-    pos += t1 - t0;
+    return false;
   }
 };
 
@@ -256,7 +273,9 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, q4 = lane >> 4;
 
-  TreeWalk<TR_TOK> walk;
+  // A small item costs 7 us besides 0.95 a tile (R = 64, 4 sequences of 300 to 600 tokens: 32.3 us without start units, 29.3 with
+  // six; one user of 1237 tokens 40.1 and 36.2).  The wide blocks' items are long: starts cost them 1 % (8192 tokens, 512 rows: 206, 210).
+  TreeWalk<TR_TOK, RB == 1 ? 6 : 0> walk;
   if (!walk.begin(a)) return;
 
   // ---- per-lane LDS offsets: rows begin at whole 128 bytes, so that the pieces of a row differ in address bits 4 to 6 alone ----
@@ -275,8 +294,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   auto page_of = [&](int t) { return shift >= 0 ? t >> shift : t / pt; };
   const bool one_page = pt % TR_TOK == 0;              // a tile never crosses a page
 
-  while (walk.pos < walk.end) {
-    walk.find(a);
+  while (walk.find(a)) {
     const int i = walk.i, b = walk.b, v = walk.v, rb = walk.rb, L = walk.L, keys = walk.keys, rows = walk.rows, t0 = walk.t0, t1 = walk.t1;
     const int row0 = rb * a.p.block + wave * (16 * RB);          // this wave's first row
     const bool alive = row0 < rows;
@@ -640,7 +658,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), team = wave / TEAM, member = wave % TEAM;
   const int j16 = lane & 15, q4 = lane >> 4;
-  TreeWalk<TP_TOK> walk;
+  TreeWalk<TP_TOK, 0> walk;                            // (rounds are long: four start units gain nothing for 16 heads and lose 2 % for 64 rows of 32768 tokens)
   if (!walk.begin(a)) return;
 
   const unsigned k_off = (unsigned)((j16 * RC + (q4 ^ swz(j16))) * 16);
@@ -656,8 +674,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
   auto page_of = [&](int t) { return shift >= 0 ? t >> shift : t / pt; };
   const bool one_page = pt % TP_TOK == 0;
 
-  while (walk.pos < walk.end) {
-    walk.find(a);
+  while (walk.find(a)) {
     const int b = walk.b, v = walk.v, L = walk.L, keys = walk.keys, rows = walk.rows, t0 = walk.t0, t1 = walk.t1;
     const int row0 = walk.rb * a.p.block + member * 16, all_rows = a.T * a.H;
     const bool alive = row0 < rows;
