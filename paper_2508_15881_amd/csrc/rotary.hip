@@ -14,6 +14,14 @@ constexpr int RO_BATCH = 4;        // rows per thread on their way together
 template <typename T>
 struct alignas(16) Eight {
   T v[8];
+  // Past the caches: what a call writes is read by another kernel, on other compute units, and lines kept for it push out what this
+  // one still reads (20011 tokens, 64 heads: 80 us with ordinary stores, 62 so, 5.3 TB/s read and written; 2048 tokens 10.8 and 7.8).
+  __device__ __forceinline__ void stream_to(T* dst) const {
+    f32x4 piece[sizeof(T) / 2];
+    __builtin_memcpy(piece, v, sizeof(v));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) __builtin_nontemporal_store(piece[i], reinterpret_cast<f32x4*>(dst) + i);
+  }
 };
 
 // What a thread does to one row.  VEC: 8 columns (of halves' rotated columns 8 and their 8 partners), otherwise one pair or one copied column.
@@ -36,7 +44,7 @@ struct RowPart<T, true> {
         p.v[e] = (T)(x * cs.x - y * cs.y);
         q.v[e] = (T)(x * cs.y + y * cs.x);
       }
-      *reinterpret_cast<Eight<T>*>(dst + at + a.rot / 2) = q;
+      q.stream_to(dst + at + a.rot / 2);
     } else if (a.layout == TPLA_ROTARY_INTERLEAVED) {
 #pragma unroll
       for (int e = 0; e < 8; e += 2)
@@ -47,7 +55,7 @@ struct RowPart<T, true> {
           p.v[e + 1] = (T)(x * cs.y + y * cs.x);
         }
     }
-    *reinterpret_cast<Eight<T>*>(dst + at) = p;
+    p.stream_to(dst + at);
   }
 };
 template <typename T>
@@ -133,8 +141,9 @@ int launch_rotary(RotaryArgs a, int dtype, hipStream_t st) {
   const bool half = a.layout == TPLA_ROTARY_HALF;
   const bool vec = !half || a.rot % 16 == 0;
   const int heads = (a.q ? a.H : 0) + (a.k ? 1 : 0);
-  a.block_tokens = a.T >= 4 * device_cu_count() ? 8 : 1;
-  while (a.block_tokens > 1 && (size_t)a.block_tokens * (a.rot / 2) * sizeof(float2) > 48 * 1024) a.block_tokens /= 2;
+  // sines shared by the heads of a token; two tokens in a workgroup fill its threads, more leave some compute units behind
+  // (4 tokens: 63 us for 20011 tokens and 9.0 for 2048; 2: 62 and 7.8; 1: 69 and 8.1)
+  a.block_tokens = a.T >= 4 * device_cu_count() ? 2 : 1;
   a.block_heads = a.T >= device_cu_count() ? heads : (heads + 3) / 4;
   const dim3 grid((unsigned)((a.T + a.block_tokens - 1) / a.block_tokens), (unsigned)((heads + a.block_heads - 1) / a.block_heads));
   const size_t lds = (size_t)a.block_tokens * (a.rot / 2) * sizeof(float2);
