@@ -189,6 +189,11 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
   if (!isfinite(amplitude)) return fail(TPLA_ERR_SHAPE, "amplitude is not finite");
   if (rot_dim > 8192) return fail(TPLA_ERR_UNSUPPORTED, "rot_dim=%d above 8192", rot_dim);
   const int esz = shape->dtype == TPLA_F32 ? 4 : 2;
+  // the stride of a dimension of size 1, and those of a pair that is not there, mean nothing
+  if (T <= 1) q_token_stride = q_out_token_stride = k_token_stride = k_out_token_stride = 0;
+  if (shape->H == 1) q_head_stride = q_out_head_stride = 0;
+  if (!q) q_token_stride = q_head_stride = q_out_token_stride = q_out_head_stride = 0;
+  if (!k) k_token_stride = k_out_token_stride = 0;
   const int64_t strides[] = {q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, k_token_stride, k_out_token_stride};
   for (int64_t s : strides) {
     if (s < 0) return fail(TPLA_ERR_SHAPE, "a stride is negative");

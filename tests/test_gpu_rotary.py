@@ -126,3 +126,36 @@ def test_captured_and_replayed_on_a_side_stream():
         torch.cuda.synchronize()
         want, size = rotate64(x.double().cpu(), pos.cpu(), freq, 64, 0)
         assert_close(y, want, size, st)
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_widest_rows(layout):
+    T, d_r, st = 1100, 8192, torch.bfloat16
+    g = torch.Generator().manual_seed(layout)
+    k = torch.randn((T, d_r), generator=g).to(st)
+    pos = torch.randint(0, 100000, (T,), generator=g).to(torch.int32)
+    freq = tp.tpla_rotary_frequencies(d_r)
+    kd = k.cuda()
+    tp.tpla_apply_rotary(shape(1, d_r, st), layout, 0, d_r, torch.from_numpy(freq).cuda(), 1.0, pos.cuda(), T, None, None, kd, kd)
+    torch.cuda.synchronize()
+    want, size = rotate64(k.double(), pos, freq, d_r, layout)
+    assert_close(kd, want, size, st)
+
+
+@pytest.mark.parametrize("T,H", [(1, 6), (5, 1), (1, 1)])
+def test_strides_of_single_tokens_and_heads_mean_nothing(T, H):
+    st = torch.bfloat16
+    wide = torch.randn((T, H, 64)).to(st).cuda()
+    q = torch.as_strided(wide, (T, H, 64), (3 if T == 1 else H * 64, 1 if H == 1 else 64, 1))
+    k = torch.as_strided(torch.randn((T, 64)).to(st).cuda(), (T, 64), (7 if T == 1 else 64, 1))
+    before, kb = q.clone(), k.clone()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") + 41
+    freq = tp.tpla_rotary_frequencies(64)
+    qo, ko = torch.empty((T, H, 64), dtype=st, device="cuda"), torch.empty((T, 64), dtype=st, device="cuda")
+    call = lambda *t: tp.tpla_apply_rotary(shape(H, 64, st), 0, 0, 64, torch.from_numpy(freq).cuda(), 1.0, pos, T, *t)  # noqa: E731
+    call(q, qo, k, ko)
+    call(q, q, k, k)
+    torch.cuda.synchronize()
+    for got, x in ((qo, before), (ko, kb), (q, before), (k, kb)):
+        want, size = rotate64(x.double().cpu(), pos.cpu(), freq, 64, 0)
+        assert_close(got, want, size, st)
