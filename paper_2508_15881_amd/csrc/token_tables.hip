@@ -272,8 +272,8 @@ __global__ void __launch_bounds__(CM_THREADS) commit_drafts_kernel(CommitArgs a)
     src_of[tid] = moves ? ((long long)table[from / pt] * pt + from % pt) * a.row_bytes : -1;
     dst_of[tid] = ((long long)table[to / pt] * pt + to % pt) * a.row_bytes;
   }
-  if (tid == 0) a.new_lens[b] = L + n;               // (nothing reads it, or the length it may replace, from here on)
   __syncthreads();
+  if (tid == 0) a.new_lens[b] = L + n;               // (every wave has read the length that it may replace)
   const unsigned pieces = a.row_bytes / 16, per_row = pieces * a.n_shards;
   // whole rows per step, so that no row is written while another thread has yet to read it; a row wider than a step goes in parts, whose
   // pieces are their own
