@@ -435,10 +435,12 @@ int tpla_validate_block_table(const tpla_shape_t* shape, const int32_t* block_ta
  * rest of a row gets slot -1 and position 0, n_tokens = B * row_tokens.  cu_tokens int32 [B + 1] is the prefix sum of
  * add_lens either way, clipped to n_tokens.  counts int32 [2]: pages taken from the front of free_pages (the caller's next
  * list begins behind them), pages that were missing.  A sequence keeps the pages of rejected drafts and uses them first.
- * Negative lengths count as 0, lengths beyond the row as the row's.  pages_held_out may be pages_held (for more than 1024
- * tokens a separate array saves a launch); no other overlap.  All pointers are int32 DEVICE arrays; depths
- * [B, row_tokens] or NULL; free_pages may be NULL with n_free = 0.  Only shape->B and page_tokens are read (the shape is
- * checked whole).
+ * Where pages were missing, table entries behind pages_held_out[b] are as they were: before anything reads such tokens, call
+ * again with pages_held_out for pages_held and more free pages, which places them all, or shorten the lengths.
+ * Negative lengths count as 0, lengths beyond the row as the row's; a negative table entry gives slot
+ * -1.  pages_held_out may be pages_held (for more than 1024 tokens a separate array saves a launch); no other
+ * overlap.  All pointers are int32 DEVICE arrays; depths [B, row_tokens] or NULL; free_pages may be NULL with n_free =
+ * 0.  Only shape->B and page_tokens are read (the shape is checked whole).
  */
 int tpla_extend_sequences(const tpla_shape_t* shape, const int32_t* seq_lens, const int32_t* add_lens, int32_t row_tokens,
                           const int32_t* depths, const int32_t* free_pages, int32_t n_free, const int32_t* pages_held,
@@ -462,10 +464,11 @@ int tpla_rotary_frequencies(int32_t rot_dim, double base, double factor, int32_t
  *     (x, y) -> amplitude * (x cos a_j - y sin a_j, x sin a_j + y cos a_j)
  * for the rot_dim / 2 pairs of `layout`; columns rot_dim .. d_r - 1 are copied.  inverse = 1 turns by -a_j: the transpose,
  * hence the gradient with respect to the input.  Angles are formed in double, sine and cosine and the products in float, one
- * rounding on the way out.  q, k, q_out, k_out in shape->dtype with strides in elements (innermost dense), so that they may be
- * columns of a wider projection; pointers and strides in whole 16 bytes (TPLA_ERR_ALIGN).  An output may be its input, with
- * the same strides; no other overlap.  q with q_out, or k with k_out, may be NULL.  freq double [rot_dim / 2] and positions
- * int32 [T] on the device; rot_dim even, 2 .. d_r.  Only H, d_r and dtype of shape are read (the shape is checked whole).
+ * rounding on the way out.  q, k, q_out, k_out in shape->dtype with strides in elements (innermost dense), so that they
+ * may be columns of a wider projection; pointers and strides in whole 16 bytes (TPLA_ERR_ALIGN; the stride of a single
+ * token or head means nothing).  An output may be its input, with the same strides; no other overlap.  q with q_out, or k
+ * with k_out, may be NULL.  freq double [rot_dim / 2] and positions int32 [T] on the device; rot_dim even, 2 ..
+ * d_r.  Only H, d_r and dtype of shape are read (the shape is checked whole).
  */
 int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse, int32_t rot_dim, const double* freq,
                       float amplitude, const int32_t* positions, int64_t T, const void* q, int64_t q_token_stride,
@@ -512,11 +515,11 @@ int tpla_decode_shards_tree_combine(const tpla_shape_t* shape, int32_t T, const 
 /*
  * The accepted drafts of every sequence behind its committed tokens: for k < n_accepted[b], in all g pools,
  *     row of token seq_lens[b] + k  =  row of token seq_lens[b] + accepted[b, k]   (as it was before the call)
- * and new_lens[b] = seq_lens[b] + n_accepted[b].  accepted int32 [B, T]: indices into the drafts, ascending (a path of a
- * tree whose parents come before their children); n_accepted int32 [B], clipped to [0, T] and to the block-table row.
- * Entries outside [0, T) are clipped; an order that is not ascending gives wrong rows, never an access outside the pages
- * listed.  new_lens may be seq_lens.  No two sequences may share the pages that hold their drafts.  Rows are copied bit for
- * bit.  d_n, d_v, H of shape are not used.
+ * and new_lens[b] = seq_lens[b] + n_accepted[b].  accepted int32 [B, T]: indices into the drafts, strictly ascending (a
+ * path of a tree whose parents come before their children); n_accepted int32 [B], clipped to [0, T] and to the
+ * block-table row. Entries outside [0, T) are clipped; another order gives wrong rows, never an access outside the
+ * pages that the block-table row lists.  new_lens may be seq_lens.  No two sequences may share the pages that hold their
+ * drafts.  Rows are copied bit for bit.  d_n, d_v, H of shape are not used.
  */
 int tpla_commit_drafts(const tpla_shape_t* shape, int32_t T, const int32_t* accepted, const int32_t* n_accepted,
                        const int32_t* seq_lens, const int32_t* block_table, int32_t max_pages_per_seq,

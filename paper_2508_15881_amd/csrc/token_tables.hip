@@ -47,14 +47,14 @@ __device__ __forceinline__ int last_not_above(const T* v, int n, T x) {
   return lo;
 }
 
-// Slots and positions of tokens first, first + step, ... below a.n_tokens: each is a search among the sequences, their lengths, and a table entry.
-// cu: [B + 1], in LDS or memory.
-__device__ __forceinline__ void place_tokens(const ExtendArgs& a, const int32_t* cu, int first, int step) {
-  for (int at0 = first; at0 < a.n_tokens; at0 += EX_BATCH * step) {
+// Slots and positions of EX_BATCH tokens, first, first + step, ..., below a.n_tokens: each is a search among the sequences, their lengths, and a
+// table entry.  cu: [B + 1], in LDS or memory.
+__device__ __forceinline__ void place_tokens(const ExtendArgs& a, const int32_t* cu, long long first, int step) {
+  if (first < a.n_tokens) {
     int slot[EX_BATCH], position[EX_BATCH];
 #pragma unroll
     for (int k = 0; k < EX_BATCH; ++k) {
-      const int at = min(at0 + k * step, a.n_tokens - 1);
+      const int at = (int)min(first + k * step, (long long)a.n_tokens - 1);
       int b, i;
       bool there;
       if (a.row_tokens) {
@@ -69,14 +69,14 @@ __device__ __forceinline__ void place_tokens(const ExtendArgs& a, const int32_t*
       const int L = held_tokens(a, b);
       const long long t = (long long)L + i, page = t / a.page_tokens;
       const int entry = a.block_table[(size_t)b * a.max_pages + min(page, (long long)a.max_pages - 1)];
-      slot[k] = there && page < a.held_out[b] ? entry * a.page_tokens + (int)(t - page * a.page_tokens) : -1;
+      slot[k] = there && page < a.held_out[b] && entry >= 0 ? entry * a.page_tokens + (int)(t - page * a.page_tokens) : -1;
       position[k] = there ? clip_int(a.depths ? (long long)L + a.depths[at] : t, 2147483647LL) : 0;
     }
 #pragma unroll
     for (int k = 0; k < EX_BATCH; ++k)
-      if (at0 + k * step < a.n_tokens) {
-        a.slots[at0 + k * step] = slot[k];
-        a.positions[at0 + k * step] = position[k];
+      if (first + k * step < a.n_tokens) {
+        a.slots[first + k * step] = slot[k];
+        a.positions[first + k * step] = position[k];
       }
   }
 }
@@ -143,10 +143,7 @@ __global__ void __launch_bounds__(256) place_tokens_kernel(ExtendArgs a) {
     __syncthreads();
   }
   // the tokens of a workgroup lie side by side: few sequences, whole lines of slots
-  const int begin = blockIdx.x * (256 * EX_BATCH);
-  ExtendArgs mine = a;
-  mine.n_tokens = min((long long)a.n_tokens, (long long)begin + 256 * EX_BATCH);
-  place_tokens(mine, local ? cu_of : a.cu, begin + threadIdx.x, 256);
+  place_tokens(a, local ? cu_of : a.cu, (long long)blockIdx.x * (256 * EX_BATCH) + threadIdx.x, 256);
 }
 
 // The usual case, at most EX_ROOM sequences, in one launch: every workgroup takes the prefix sums over all sequences for itself (their lengths

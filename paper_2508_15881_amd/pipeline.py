@@ -158,7 +158,8 @@ class DraftStep:
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 
     def place(self, seq_lens, draft_lens, depths, free_pages, n_free, pages_held, block_table):
-        """Pages, slots and positions of the drafts (once per step, for all layers); pages_held is updated."""
+        """Pages, slots and positions of the drafts (once per step, for all layers); pages_held is updated, counts are the pages
+        taken from free_pages and those that were missing (which the caller provides in another call, or drafts less)."""
         B.tpla_extend_sequences(self.shape, seq_lens, draft_lens, self.T, depths, free_pages, n_free, pages_held, pages_held, block_table,
                                 self.max_pages, self.cu, self.slots, self.positions, self.slots.numel(), self.counts)
 

@@ -106,6 +106,32 @@ def test_extend_runs_out_of_pages(n_free):
     assert got[5][0] == n_free and got[5][1] > 0 and (got[3] == -1).any()
 
 
+@pytest.mark.parametrize("in_place,n", [(False, 40), (True, 40), (True, 3000)])
+def test_extend_again_with_more_pages(in_place, n):
+    """What the first call could not place, the second does, from where it stopped; the result is that of one call with all pages."""
+    r = np.random.default_rng(6)
+    lens, adds, held, table, free = problem(r, 9, 16, 50, n)
+    want = extend_plain(16, lens, adds, 0, None, free, held, table, sum(adds))
+    got = extend(16, lens, adds, 0, None, free[:7], held, table, sum(adds), in_place)
+    again = extend(16, lens, adds, 0, None, free[got[5][0]:], got[1], got[0], sum(adds), in_place)
+    assert_same(again[:5], want[:5])
+    assert got[5][0] + again[5][0] == want[5][0] and again[5][1] == 0
+
+
+@pytest.mark.parametrize("in_place,n", [(False, 40), (True, 3000)])
+def test_extend_negative_table_entries(in_place, n):
+    """Pages that a sequence counts as held but that its row does not name (-1): no slot."""
+    lens, held = [40, 33], [4, 4]
+    table = np.array([[0, 1, 2, -1] + [-1] * 400, [-2 ** 31, 5, -7, 6] + [-1] * 400], dtype=np.int32)
+    adds, free = [n, 25], np.arange(10, 400, dtype=np.int32)
+    got = extend(16, lens, adds, 0, None, free, held, table, n + 25, in_place)
+    want = extend_plain(16, lens, adds, 0, None, free, held, table, n + 25)
+    t = np.concatenate([np.arange(40, 40 + n), np.arange(33, 58)])
+    row = got[0][np.repeat([0, 1], [n, 25]), t // 16]
+    assert_same(got[:3] + (np.where(row < 0, -1, got[3]),) + got[4:], want[:3] + (np.where(row < 0, -1, want[3]),) + want[4:])
+    assert (got[3][row < 0] == -1).all()
+
+
 def test_extend_beyond_the_row_and_out_of_range():
     r = np.random.default_rng(5)
     lens, adds, held, table, free = problem(r, 8, 16, 60, 100, max_pages=5)
