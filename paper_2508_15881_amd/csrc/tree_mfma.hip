@@ -105,7 +105,7 @@ struct TreeWalk {
   TreeUnits front;             // the first 64 sequences stay in the lanes: a search among them loads nothing
   int front_incl, per_slice, units, n_wg, w, pos, range0, end;
   // the item
-  int i, b, v, item, rb, rows, L, keys, tiles, t0, t1, slot;
+  int i, b, v, item, rb, rows, L, keys, tiles, t0, t1, slot, last;
   bool whole;
 
   static __device__ __forceinline__ int units_of(const TreeUnits& u) { return u.blocks * (u.tiles + START); }
@@ -157,6 +157,7 @@ struct TreeWalk {
       t1 = stop - START;
       const int first = pos;
       pos += stop - at;
+      last = first - at + span - 1;
       if (t1 <= t0) continue;                        // the range ends before the item's first tile
       L = __builtin_amdgcn_readlane(u.len.L, src);
       keys = __builtin_amdgcn_readlane(u.len.keys, src);
@@ -165,14 +166,17 @@ struct TreeWalk {
       item = v * a.p.blocks + rb;
       whole = t0 == 0 && t1 == tiles;
       slot = 2 * w + (first == range0 ? 0 : 1);
-      if (t0 == 0 && threadIdx.x == 0) {
-        a.plan[3 * item] = w;
-        a.plan[3 * item + 1] = tree_owner(n_wg, units, first - at + span - 1) - w + 1;
-        a.plan[3 * item + 2] = slot & 1;
-      }
       return true;
     }
     return false;
+  }
+  // Where the merge finds the item's results: whoever has its first tile says so, once its first loads are on their way (512 rows, 64-wide
+  // slices: 352 us ahead of them, 347 so).
+  __device__ __forceinline__ void note(const TreeArgs& a) const {
+    if (t0 != 0 || threadIdx.x != 0) return;
+    a.plan[3 * item] = w;
+    a.plan[3 * item + 1] = tree_owner(n_wg, units, last) - w + 1;
+    a.plan[3 * item + 2] = slot & 1;
   }
 };
 
@@ -274,7 +278,8 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   const int j16 = lane & 15, q4 = lane >> 4;
 
   // A small item costs 7 us besides 0.95 a tile (R = 64, 4 sequences of 300 to 600 tokens: 32.3 us without start units, 29.3 with
-  // six; one user of 1237 tokens 40.1 and 36.2).  The wide blocks' items are long: starts cost them 1 % (8192 tokens, 512 rows: 206, 210).
+  // six; one user of 1237 tokens 40.1 and 36.2).  The wide blocks' items are long: start units cost them 2 % (8192 tokens, 512 rows,
+  // 64-wide slices: 352 and 360; 192 rows, 256-wide ones: 184 and 188).
   TreeWalk<TR_TOK, RB == 1 ? 6 : 0> walk;
   if (!walk.begin(a)) return;
 
@@ -344,6 +349,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __builtin_amdgcn_s_barrier();
     for (int t = t0; t < t1 && t < t0 + NSTAGE - 1; ++t) issue(t, lds_read_id(id_of(t)));
+    walk.note(a);
 
     // In the middle of the values of tile t: tile t + 2 is there for all waves, tile t - 1 is no longer read by any and another takes its place.
     auto arrived = [&](int t) {
@@ -723,6 +729,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __builtin_amdgcn_s_barrier();
     for (int t = t0; t < t1 && t < t0 + NSTAGE - 1; ++t) issue(t);
+    walk.note(a);
 
     bf16x8 q[KS];
     {
