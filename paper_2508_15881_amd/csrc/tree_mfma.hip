@@ -634,9 +634,11 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
 
 // ---------------------------------------------------------------------------
 // Few rows: up to 64 (TEAMS = 2) or 128 (TEAMS = 1) per item.  What bounds these is how fast one compute unit gets through its cache rows, and a
-// single wave per SIMD leaves most of its time to waits.  Here 8 waves of 16 rows share rounds of 64 tokens, two waves per SIMD: one's
-// matrix products run under the other's exponentials and reads.  TEAMS = 2: four waves take the first 32 tokens of a round and four the
-// others, for the same 64 rows, and their results are joined through LDS at the end of the item.
+// single wave per SIMD leaves most of its time to waits.  Here 8 waves share rounds of 64 tokens, two waves per SIMD: one's matrix products run
+// under the other's exponentials and reads.  A wave has 16 rows.  Where an item has fewer blocks of 16 than there are waves, the waves left over
+// take the second 32 tokens of every round for the first blocks, and what both have is joined through LDS at the end of the item (with TEAMS = 2
+// that is every block).  Waves 0 .. 3 lie on different SIMDs, so few blocks have one each: 64 x 8192 tokens, 16 rows: 121 us with the second wave on
+// another SIMD, 142 with it on the same; 80 rows: 212 with five waves, 198 with eight.
 constexpr int TP_NW = 8, TP_TOK = 64;
 
 template <int DL>
@@ -654,15 +656,16 @@ template <int DL, int TEAMS>
 __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
   using Tile = PairTile<DL>;
   constexpr int RC = Tile::RC, CPT = Tile::CPT, NSTAGE = Tile::NSTAGE;
-  constexpr int KS = (DL + 64) / 32, DB = DL / 16, NQ = 2 * KS;
-  constexpr int KRING = 6, VRING = 4, TEAM = TP_NW / TEAMS;
-  // streaming, not kept in L2, where no other row block reads these rows (32 x 32768 tokens, 64 rows: 284 -> 271 us with merge and combine)
-  constexpr int STREAM = TEAMS == 2 ? 2 : 0;
+  constexpr int KS = (DL + 64) / 32, DB = DL / 16;
+  constexpr int KRING = 6, VRING = 4;
+  // streaming, not kept in L2 (32 x 32768 tokens, 64 rows: 284 -> 271 us with merge and combine; 64 x 8192, 80 rows: 204 -> 198; sixteen blocks of
+  // 128 rows, which find the rows of each other in the last-level cache, lose nothing)
+  constexpr int STREAM = 2;
   extern __shared__ u32x4 smem[];
   char* const lds = reinterpret_cast<char*>(smem);
   const unsigned lds_base = lds_at(lds);
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), team = wave / TEAM, member = wave % TEAM;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, q4 = lane >> 4;
   TreeWalk<TP_TOK, 0> walk;                            // (rounds are long: four start units gain nothing for 16 heads and lose 2 % for 64 rows of 32768 tokens)
   if (!walk.begin(a)) return;
@@ -682,8 +685,11 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
 
   while (walk.find(a)) {
     const int b = walk.b, v = walk.v, L = walk.L, keys = walk.keys, rows = walk.rows, t0 = walk.t0, t1 = walk.t1;
+    // Blocks of 16 rows; where there are fewer than waves, the first `joined` have a second wave, which takes the other half of every round.
+    const int n_blocks = min((rows - walk.rb * a.p.block + 15) / 16, TP_NW), joined = min(n_blocks, TP_NW - n_blocks);
+    const int team = wave < n_blocks ? 0 : 1, member = team ? wave - n_blocks : wave;
+    const bool alive = wave < n_blocks + joined, both = member >= joined;
     const int row0 = walk.rb * a.p.block + member * 16, all_rows = a.T * a.H;
-    const bool alive = row0 < rows;
     const char* pool = static_cast<const char*>(tree_pool(a, walk.i));
     const int32_t* table = a.block_table + (size_t)b * a.max_pages;
 
@@ -746,13 +752,13 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    auto clean = [&](int t, int first, int n) {      // rows first .. first + n - 1 of round t; see the kernel above
+    auto clean = [&](int t) {                        // round t; see the kernel above
       lds_barrier();
 #pragma unroll 1
-      for (int x = here(tid); x < n * RC; x += TP_NW * 64) {
-        const int tok = first + x / RC, c = (x % RC) ^ swz(tok);
+      for (int x = here(tid); x < TP_TOK * RC; x += TP_NW * 64) {
+        const int tok = x / RC, c = (x % RC) ^ swz(tok);
         if (c >= DL / 8 || t * TP_TOK + tok < L) continue;
-        u32x4* at = smem + (t % NSTAGE) * (TP_TOK * RC) + first * RC + x;
+        u32x4* at = smem + (t % NSTAGE) * (TP_TOK * RC) + x;
         u32x4 u = *at;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -764,40 +770,44 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
       lds_barrier();
     };
 
-    // 32 tokens of round t, rows 32 sub ..
-    auto tile_of = [&](int t, int sub) {
+    // 32 SUBS tokens of round t, from its token 32 sub on.  (Both halves at once, not one after the other: one wait for the first fragments, one
+    // step of the softmax, four independent sums.)
+    auto tile_of = [&](auto subs, int t, int sub) {
+      constexpr int SUBS = decltype(subs)::value, TB = 2 * SUBS, N = KS * TB, NV = DB * SUBS;
       const unsigned tile = lds_base + (unsigned)((t % NSTAGE) * Tile::BYTES + sub * (32 * RC * 16));
       const bool tail = (t + 1) * TP_TOK > L;
-      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      f32x4 s[TB];
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) s[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (alive) {
         bf16x8 kf[KRING];
         const unsigned ka = tile + k_off;
         auto read_k = [&](auto ic) {
-          constexpr int x = decltype(ic)::value, ks = x / 2, tb = x % 2;
+          constexpr int x = decltype(ic)::value, ks = x / TB, tb = x % TB;
           lds_read_b128<(ks >> 1) * 128 + tb * (16 * RC * 16)>(kf[x % KRING], ka ^ ((ks & 1) << 6));
         };
         static_for<KRING>(read_k);
-        static_for<NQ>([&](auto ic) {
-          constexpr int x = decltype(ic)::value, left = NQ - 1 - x;
+        static_for<N>([&](auto ic) {
+          constexpr int x = decltype(ic)::value, left = N - 1 - x;
           lds_wait<(left < KRING - 1 ? left : KRING - 1)>(kf[x % KRING]);
-          s[x % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x % KRING], q[x / 2], s[x % 2], 0, 0, 0);
-          if constexpr (x + KRING < NQ) read_k(std::integral_constant<int, x + KRING>{});
+          s[x % TB] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x % KRING], q[x / TB], s[x % TB], 0, 0, 0);
+          if constexpr (x + KRING < N) read_k(std::integral_constant<int, x + KRING>{});
         });
       }
-      if (tail) clean(t, TEAMS == 2 ? 0 : 32 * sub, TEAMS == 2 ? TP_TOK : 32);
+      if (tail) clean(t);
       if (!alive) return;
       u32x2 vlo[VRING], vhi[VRING];
       const unsigned va = tile + v_off;
-      auto read_v = [&](auto ic) {
-        constexpr int d = decltype(ic)::value;
-        lds_read_tr_b64<(d >> 2) * 128>(vlo[d % VRING], va ^ ((d & 3) << 5));
-        lds_read_tr_b64<(d >> 2) * 128 + 16 * RC * 16>(vhi[d % VRING], va ^ ((d & 3) << 5));
+      auto read_v = [&](auto ic) {                   // block d of the columns, 32 tokens of it
+        constexpr int x = decltype(ic)::value, d = x / SUBS, at = (x % SUBS) * (32 * RC * 16) + (d >> 2) * 128;
+        lds_read_tr_b64<at>(vlo[x % VRING], va ^ ((d & 3) << 5));
+        lds_read_tr_b64<at + 16 * RC * 16>(vhi[x % VRING], va ^ ((d & 3) << 5));
       };
       if (tail) {
         const int row = min(row0 + here(j16), rows - 1);
         const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H];
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
+        for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int k = t * TP_TOK + 32 * sub + 16 * tb + 4 * here(q4) + e, j = k - L;
@@ -807,7 +817,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
       static_for<VRING>(read_v);
       float mx = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
-      for (int e = 2; e < 8; ++e) mx = fmaxf(mx, s[e >> 2][e & 3]);
+      for (int e = 2; e < 4 * TB; ++e) mx = fmaxf(mx, s[e >> 2][e & 3]);
       mx *= a.scale_log2;
       if (__any(mx > m_run + LAZY)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -819,19 +829,19 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) acc[d] *= alpha;
       }
-      bf16x8 pb;                                     // weights in bf16, their sum from the unrounded ones
+      bf16x8 pb[SUBS];                               // weights in bf16, their sum from the unrounded ones
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 4 * TB; ++e) {
         const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], a.scale_log2, -m_run));
         l_run += p;
-        pb[e] = (bf16_t)p;
+        pb[e >> 3][e & 7] = (bf16_t)p;
       }
-      static_for<DB>([&](auto ic) {
-        constexpr int d = decltype(ic)::value, left = DB - 1 - d;
-        lds_wait<2 * (left < VRING - 1 ? left : VRING - 1)>(vlo[d % VRING], vhi[d % VRING]);
-        const u32x4 v4 = {vlo[d % VRING][0], vlo[d % VRING][1], vhi[d % VRING][0], vhi[d % VRING][1]};
-        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb, acc[d], 0, 0, 0);
-        if constexpr (d + VRING < DB) read_v(std::integral_constant<int, d + VRING>{});
+      static_for<NV>([&](auto ic) {
+        constexpr int x = decltype(ic)::value, d = x / SUBS, left = NV - 1 - x;
+        lds_wait<2 * (left < VRING - 1 ? left : VRING - 1)>(vlo[x % VRING], vhi[x % VRING]);
+        const u32x4 v4 = {vlo[x % VRING][0], vlo[x % VRING][1], vhi[x % VRING][0], vhi[x % VRING][1]};
+        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb[x % SUBS], acc[d], 0, 0, 0);
+        if constexpr (x + VRING < NV) read_v(std::integral_constant<int, x + VRING>{});
       });
     };
 
@@ -842,31 +852,34 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
       __builtin_amdgcn_s_barrier();                  // round t is there for all waves, round t - 1 is no longer read
       if (t + NSTAGE - 1 < t1) issue(t + NSTAGE - 1);
-      if constexpr (TEAMS == 2) {
-        tile_of(t, team);
-      } else {
-#pragma unroll 1
-        for (int sub = 0; sub < 2; ++sub) tile_of(t, sub);
+      if constexpr (TEAMS == 1) {
+        if (both) {
+          tile_of(std::integral_constant<int, 2>{}, t, 0);
+          continue;
+        }
       }
+      tile_of(std::integral_constant<int, 1>{}, t, team);
     }
 
-    // ---- the two teams' halves of the tokens, then the result ----
-    if constexpr (TEAMS == 2) {
+    // ---- the halves of a block's tokens, then the result ----
+    if (joined > 0) {
       lds_barrier();                                 // the last round is no longer read
       char* const at = lds + member * ((DB + 1) * 1024) + lane * 16;
-      if (team == 1) {
+      if (alive && team == 1) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(at + d * 1024) = acc[d];
         *reinterpret_cast<float2*>(at + DB * 1024) = make_float2(m_run, l_run);
       }
       lds_barrier();
       if (team == 1) continue;
-      const float2 ml = *reinterpret_cast<const float2*>(at + DB * 1024);
-      const float m = fmaxf(m_run, ml.x), mine = __builtin_amdgcn_exp2f(m_run - m), theirs = __builtin_amdgcn_exp2f(ml.x - m);
-      m_run = m;
-      l_run = l_run * mine + ml.y * theirs;
+      if (!both) {
+        const float2 ml = *reinterpret_cast<const float2*>(at + DB * 1024);
+        const float m = fmaxf(m_run, ml.x), mine = __builtin_amdgcn_exp2f(m_run - m), theirs = __builtin_amdgcn_exp2f(ml.x - m);
+        m_run = m;
+        l_run = l_run * mine + ml.y * theirs;
 #pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = acc[d] * mine + *reinterpret_cast<const f32x4*>(at + d * 1024) * theirs;
+        for (int d = 0; d < DB; ++d) acc[d] = acc[d] * mine + *reinterpret_cast<const f32x4*>(at + d * 1024) * theirs;
+      }
     }
     float l = l_run;
     l += __shfl_xor(l, 16);
