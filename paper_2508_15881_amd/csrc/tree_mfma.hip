@@ -905,15 +905,16 @@ bool tree_mfma_supported(const tpla_shape_t& sh) {
 }
 
 // The kernel and the rows of an item, from the rows R of a sequence and the 32-token tiles of 64 rows per compute unit (by the block table's width:
-// the host does not know the lengths).  Medians of 8 calls with their merge, us, over batches of 1 to 64 sequences of 300 to 32768 tokens
+// the host does not know the lengths).  Best of three runs of 8 calls with their merge, us, over batches of 1 to 64 sequences of 300 to 32768 tokens
 // (lengths from two thirds of that on):
-//   little work: 64 rows on 4 waves (A).  More workgroups, shorter prologues, smaller partial results.  256-wide, 16 x 1237 tokens: R = 128 A 34.5,
-//     128 rows on 8 waves (B) 42.8, 192 rows (C) 46; R = 256 44.4 / 50 / 54; R = 512 (39 tiles) 67 / 64 / 71; one sequence of 1237, R = 1664 37.4 / 37.6 / 40.4
-//   up to 64 rows: two teams of 4 waves (D).  64 x 8192 tokens, R = 48 to 64: 256-wide A 129.7, D 127; 128-wide 187 / 177; 64-wide 313 / 273
-//   more: B, or C (256 rows of narrower slices) where its blocks are filled and long enough.  256-wide: R = 80, 64 x 8192: B 166, C 206; R = 192 317 / 235; 16 x
-//     4096: R = 192 66 / 71, R = 512 112 / 117, R = 1024 197 / 189.  128-wide, 64 x 2048: R = 256 155 / 154, 384 212 / 243, 1024 518 / 471; 64-wide 829 / 724.
-// Per tile C takes 1.38 (256-wide) and 1.8 (narrower) times what B takes.  (128 rows on 4 waves are within 4 % of B below 256 rows, up to 13 % slower above,
-// and were not kept.)  512-wide slices have A alone: the accumulators of more rows do not fit.
+//   little work: 64 rows on 4 waves (A).  More workgroups, shorter prologues, smaller partial results.  256-wide, 16 x 1237 tokens: R = 128 A 31,
+//     128 rows on 8 waves (B) 43, 192 rows (C) 47; 16 x 4096, R = 80 to 192 A 45 to 62, B 50 to 67.  64-wide slices pass sooner: one sequence of 8192,
+//     R = 80 A 26.5, B 23.4
+//   up to 64 rows: two teams of 4 waves (D).  64 x 8192 tokens, R = 48: 256-wide A 130.5, D 126.9, B 140; 128-wide 168.6 / 167.4 / 175; 64-wide 282 / 260 / 274
+//   more: B, or C (256 rows of narrower slices) where its blocks are filled and long enough.  256-wide: R = 80, 64 x 8192: B 161, C 211; R = 192 315 / 247; 64 x
+//     2048: R = 384 171 / 170, 512 206 / 219.  128-wide, R = 1024: 64 x 2048 489 / 473, 16 x 1237 113 / 125; R = 192, 64 x 2048 135 / 143; 64-wide 741 / 730, 164 / 173.
+// Per tile C takes 1.45 (256-wide) and 1.95 (narrower) times what B takes for a full block, and B's last block half of that and what its rows add.
+// (128 rows on 4 waves were up to 13 % slower than B and not kept.)  512-wide slices have A alone: the accumulators of more rows do not fit.
 void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, TreePlan* p) {
   const int dl = sh.d_c / sh.g, rows = T * sh.H, large = dl == 256 ? 192 : 256, cus = device_cu_count();
   const double tiles = std::max(((double)max_pages * sh.page_tokens + TR_TOK - 1) / TR_TOK, 1.0), per_row_block = (double)n_shards * sh.B * tiles / cus;
@@ -921,10 +922,11 @@ void tree_mfma_plan(const tpla_shape_t& sh, int n_shards, int T, int max_pages, 
   p->mfma = 1;
   p->teams = 0;
   p->block = 64;
-  if (dl < 512 && per_row_block * blocks(64) >= 32) {
+  if (dl < 512 && per_row_block * blocks(64) >= (dl == 64 ? 14 : 40)) {
     p->teams = rows <= 64 ? 2 : 1;
     p->block = 128 / p->teams;
-    if (rows > 128 && per_row_block * blocks(large) >= 24 && blocks(large) * (dl == 256 ? 1.38 : 1.8) < blocks(128)) {
+    const double pair = rows / 128 + (rows % 128 ? 0.5 + rows % 128 / 256.0 : 0.0), wide = blocks(large) * (dl == 256 ? 1.45 : 1.95);
+    if (rows > 128 && per_row_block * blocks(large) >= (dl == 256 ? 24 : 100) && wide < pair) {
       p->teams = 0;
       p->block = large;
     }
