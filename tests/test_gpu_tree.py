@@ -262,3 +262,29 @@ def test_captured_into_a_graph():
             assert_close(h, o.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64))
     again = run_all(q, e)
     assert all(np.array_equal(x, y) for x, y in zip(again, want_q))
+
+
+@pytest.mark.parametrize("dl,g", [(256, 2), (128, 2), (64, 4)])
+@pytest.mark.parametrize("lens", [[63, 64, 65, 0, 31, 32, 33, 95], [1500, 700, 1100, 333, 64, 2000, 129, 905]])
+def test_every_number_of_row_blocks(dl, g, lens):
+    """Blocks of 16 rows 1 to 8 of an item: a block alone has both halves of a round, one with a second wave half of it."""
+    p = TreeProblem(lens, [1, 2, 3, 4, 5, 6, 7, 8], 8, H=16, g=g, dl=dl, seed=dl + len(lens) + lens[0], max_pages=WIDE)
+    o, lse = run_all(p)
+    assert_close(p, o, lse)
+
+
+@pytest.mark.parametrize("T", [3, 5, 6, 7])
+def test_masked_infinities_where_blocks_have_one_or_two_waves(T):
+    for L in (0, 37, 63, 64, 90):
+        p = TreeProblem([L, 40, 700], [T, T - 1, T], T, H=16, masks=chain_masks(3, T), seed=L + T, max_pages=WIDE)
+        p.masks[:, 1:] &= ~np.uint64(1)                          # draft 0 is seen by itself alone
+        clean = p.expected()
+        for b in range(3):
+            page, off = p.row_of(b, [L, 40, 700][b])
+            for i in range(2):
+                p.pools[i][page, off, ::2] = 0x7FC0
+                p.pools[i][page, off, 1::2] = 0x7F80
+        o, lse = run_all(p)
+        assert np.isnan(o[:, :, 0]).all() and np.isnan(lse[:, :, 0]).all()
+        o[:, :, 0], lse[:, :, 0] = clean[0][:, :, 0], clean[1][:, :, 0]
+        assert_close(p, o, lse, clean)
