@@ -467,7 +467,7 @@ int tpla_rotary_frequencies(int32_t rot_dim, double base, double factor, int32_t
  * rounding on the way out.  q, k, q_out, k_out in shape->dtype with strides in elements (innermost dense), so that they
  * may be columns of a wider projection; pointers and strides in whole 16 bytes (TPLA_ERR_ALIGN; the stride of a single
  * token or head means nothing).  An output may be its input, with the same strides; no other overlap.  q with q_out, or k
- * with k_out, may be NULL.  freq double [rot_dim / 2] and positions int32 [T] on the device; rot_dim even, 2 ..
+ * with k_out, may be NULL; T = 0 does nothing.  freq double [rot_dim / 2] and positions int32 [T] on the device; rot_dim even, 2 ..
  * d_r.  Only H, d_r and dtype of shape are read (the shape is checked whole).
  */
 int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse, int32_t rot_dim, const double* freq,

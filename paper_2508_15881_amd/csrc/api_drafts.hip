@@ -180,17 +180,18 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
                       int64_t k_token_stride, void* k_out, int64_t k_out_token_stride, void* stream) {
   int rc = check_shape(shape);
   if (rc) return rc;
-  if (!freq || !positions) return fail(TPLA_ERR_NULL, "freq/positions is NULL");
-  if (!q != !q_out || !k != !k_out || (!q && !k)) return fail(TPLA_ERR_NULL, "q and q_out, or k and k_out, or both pairs are needed");
   if (layout != TPLA_ROTARY_INTERLEAVED && layout != TPLA_ROTARY_HALF) return fail(TPLA_ERR_SHAPE, "unknown rotary layout %d", layout);
   if (rot_dim < 2 || rot_dim % 2 || rot_dim > shape->d_r)
     return fail(TPLA_ERR_SHAPE, "rot_dim=%d must be even and in 2 .. d_r=%d", rot_dim, shape->d_r);
   if (T < 0 || T > (int64_t)2147483647) return fail(TPLA_ERR_SHAPE, "T=%lld out of range", (long long)T);
   if (!isfinite(amplitude)) return fail(TPLA_ERR_SHAPE, "amplitude is not finite");
   if (rot_dim > 8192) return fail(TPLA_ERR_UNSUPPORTED, "rot_dim=%d above 8192", rot_dim);
+  if (T == 0) return TPLA_OK;                        // (tensors of no tokens may have no address)
+  if (!freq || !positions) return fail(TPLA_ERR_NULL, "freq/positions is NULL");
+  if (!q != !q_out || !k != !k_out || (!q && !k)) return fail(TPLA_ERR_NULL, "q and q_out, or k and k_out, or both pairs are needed");
   const int esz = shape->dtype == TPLA_F32 ? 4 : 2;
   // the stride of a dimension of size 1, and those of a pair that is not there, mean nothing
-  if (T <= 1) q_token_stride = q_out_token_stride = k_token_stride = k_out_token_stride = 0;
+  if (T == 1) q_token_stride = q_out_token_stride = k_token_stride = k_out_token_stride = 0;
   if (shape->H == 1) q_head_stride = q_out_head_stride = 0;
   if (!q) q_token_stride = q_head_stride = q_out_token_stride = q_out_head_stride = 0;
   if (!k) k_token_stride = k_out_token_stride = 0;
@@ -208,7 +209,6 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
     return fail(TPLA_ERR_SHAPE, "in place needs equal strides");
   if (!aligned16(freq) || !aligned16(positions) || !aligned16(q) || !aligned16(q_out) || !aligned16(k) || !aligned16(k_out))
     return fail(TPLA_ERR_ALIGN, "pointers must be 16-byte aligned");
-  if (T == 0) return TPLA_OK;
   RotaryArgs a;
   a.freq = freq;
   a.positions = positions;

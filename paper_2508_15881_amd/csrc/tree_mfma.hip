@@ -5,7 +5,7 @@
 //   S^T[token, row] = K[token, :] . Q[row, :]           M = tokens (LDS), N = rows (Q in registers for the whole item)
 //   O^T[dim, row]  += V^T[dim, token] . P^T[token, row]  V = the first dl columns of the same LDS rows, read transposed
 // A workgroup is 4 waves of RB blocks of 16 rows.  Every wave reads the whole tile from LDS, and a fragment it reads feeds RB
-// MFMAs: RB decides how far LDS (128 bytes a clock) keeps up with the matrix cores.
+// MFMAs: RB decides how far LDS keeps up with the matrix cores.
 //
 // All 32-token tiles of all items (slice, sequence, row block) are laid end to end and cut into equal ranges, one per workgroup;
 // an item that lies in one range is written at once, the others leave partial results for the merge (tree.hip).

@@ -142,3 +142,17 @@ def test_tree_masks():
     for bad in ([0], [-1, 1], [-1, -2]):
         with pytest.raises(ValueError):
             pl.tree_masks(bad)
+
+
+def test_rotary_of_no_tokens_does_nothing():
+    """Empty tensors have no address: that is not a missing pointer."""
+    import torch
+    s = shape()
+    freq, pos = torch.zeros(s.d_r // 2, dtype=torch.float64), torch.zeros(0, dtype=torch.int32)
+    st = torch.bfloat16 if s.dtype == tp.TPLA_BF16 else torch.float32
+    q, k = torch.zeros((0, s.H, s.d_r), dtype=st), torch.zeros((0, s.d_r), dtype=st)
+    assert q.data_ptr() == 0 and pos.data_ptr() == 0
+    tp.tpla_apply_rotary(s, tp.TPLA_ROTARY_HALF, 0, s.d_r, freq, 1.0, pos, 0, q, q.clone(), k, k.clone(), stream=0)
+    tp.tpla_apply_rotary(s, tp.TPLA_ROTARY_HALF, 0, s.d_r, freq, 1.0, pos, 0, None, None, k, k, stream=0)
+    with pytest.raises(tp.TplaError):
+        tp.tpla_apply_rotary(s, 7, 0, s.d_r, freq, 1.0, pos, 0, q, q, None, None, stream=0)
