@@ -288,3 +288,48 @@ def test_masked_infinities_where_blocks_have_one_or_two_waves(T):
         assert np.isnan(o[:, :, 0]).all() and np.isnan(lse[:, :, 0]).all()
         o[:, :, 0], lse[:, :, 0] = clean[0][:, :, 0], clean[1][:, :, 0]
         assert_close(p, o, lse, clean)
+
+
+@pytest.mark.parametrize("H,T", [(16, 3), (16, 7), (64, 3)])
+def test_long_tables_in_pools_beyond_32_bit_offsets(H, T):
+    p = TreeProblem([300, 30], [T, T], T, H=H, g=1, spare_pages=0, seed=19 + T, max_pages=WIDE)
+    d = p.device()
+    used, n_pool = p.pools[0].shape[0], 120000
+    big = torch.empty((n_pool, 64, 320), dtype=torch.bfloat16, device="cuda")
+    ids = np.array([n_pool - 1 - 7001 * k for k in range(used)], dtype=np.int32)
+    assert ids.min() >= 0
+    for k in range(used):
+        big[int(ids[k])] = d["pools"][0][k]
+    table = torch.from_numpy(ids[np.clip(p.bt, 0, used - 1)]).cuda()
+    o, lse = out_buffers(p)
+    ws, n = workspace(p)
+    tp.tpla_decode_shards_tree(p.shape, p.T, d["q_lat"], d["q_pe"], [big], table, p.max_pages, d["lens"], d["drafts"], d["masks"], ws, n, o, lse)
+    torch.cuda.synchronize()
+    assert_close(p, o.cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.parametrize("H,T,wide", [(16, 3, WIDE), (16, 7, WIDE), (64, 3, WIDE), (64, 4, None)])
+def test_two_graphs_that_share_a_workspace(H, T, wide):
+    """Replayed one after the other on a stream, with other work in between: each has the eager call's bits every time."""
+    problems = [TreeProblem([2100, 65, 500], [T, 1, T], T, H=H, seed=23, max_pages=wide or 64),
+                TreeProblem([90, 1333, 4000], [1, T, T - 1], T, H=H, seed=24, max_pages=wide or 64)]
+    devs = [p.device() for p in problems]
+    want = [run_all(p, d) for p, d in zip(problems, devs)]
+    ws, n = workspace(problems[0])
+    assert n >= workspace(problems[1])[1]
+    outs, graphs = [out_buffers(p) for p in problems], []
+    for p, d, (o, lse) in zip(problems, devs, outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            tp.tpla_decode_shards_tree(p.shape, p.T, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"], d["drafts"],
+                                       d["masks"], ws, n, o, lse)
+        graphs.append(graph)
+    for it in range(4):
+        for k in ((0, 1), (1, 0), (0, 0), (1, 1))[it]:
+            o, lse = outs[k]
+            o.fill_(float("nan"))
+            lse.fill_(float("nan"))
+            graphs[k].replay()
+            graphs[1 - k].replay()                           # the other one uses the workspace right behind it
+            torch.cuda.synchronize()
+            assert np.array_equal(o.cpu().numpy(), want[k][0].astype(np.float32)) and np.array_equal(lse.cpu().numpy(), want[k][1].astype(np.float32))
