@@ -11,43 +11,55 @@ namespace tpla {
 constexpr int RO_THREADS = 256;
 constexpr int RO_BATCH = 4;        // rows per thread on their way together
 
-template <typename T>
-struct alignas(16) Eight {
-  T v[8];
+template <int BYTES>
+struct Word;
+template <>
+struct Word<2> { typedef unsigned short type; };
+template <>
+struct Word<4> { typedef unsigned type; };
+template <>
+struct Word<8> { typedef unsigned long long type; };
+template <>
+struct Word<16> { typedef f32x4 type; };
+
+template <typename T, int W>
+struct alignas(W * sizeof(T) < 16 ? W * sizeof(T) : 16) Columns {
+  T v[W];
   // Past the caches: what a call writes is read by another kernel, on other compute units, and lines kept for it push out what this
   // one still reads (20011 tokens, 64 heads: 80 us with ordinary stores, 62 so, 5.3 TB/s read and written; 2048 tokens 10.8 and 7.8).
   __device__ __forceinline__ void stream_to(T* dst) const {
-    f32x4 piece[sizeof(T) / 2];
+    constexpr int BYTES = alignof(Columns), N = sizeof(v) / BYTES;
+    typedef typename Word<BYTES>::type Piece;
+    Piece piece[N];
     __builtin_memcpy(piece, v, sizeof(v));
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) __builtin_nontemporal_store(piece[i], reinterpret_cast<f32x4*>(dst) + i);
+    for (int i = 0; i < N; ++i) __builtin_nontemporal_store(piece[i], reinterpret_cast<Piece*>(dst) + i);
   }
 };
 
-// What a thread does to one row.  VEC: 8 columns (of halves' rotated columns 8 and their 8 partners), otherwise one pair or one copied column.
-template <typename T, bool VEC>
-struct RowPart;
-template <typename T>
-struct RowPart<T, true> {
-  Eight<T> p, q;
+// What a thread does to one row: W columns, and of halves' rotated columns their W partners.  Pairs side by side and halves of whole eights: W = 8;
+// halves of an even number of columns 2, of an odd number 1 (64 heads, 4096 tokens, 60 of 64 columns rotated, bf16: 25.2 us with 1, 16.1 with 2).
+template <typename T, int W>
+struct RowPart {
+  Columns<T, W> p, q;
   __device__ __forceinline__ void load(const RotaryArgs& a, const T* src, int at, bool two) {
-    p = *reinterpret_cast<const Eight<T>*>(src + at);
-    if (two) q = *reinterpret_cast<const Eight<T>*>(src + at + a.rot / 2);
+    p = *reinterpret_cast<const Columns<T, W>*>(src + at);
+    if (two) q = *reinterpret_cast<const Columns<T, W>*>(src + at + a.rot / 2);
   }
   // turn: (cos, sin) of this token's pairs
   __device__ __forceinline__ void store(const RotaryArgs& a, T* dst, int at, bool two, const float2* turn) {
     if (two) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < W; ++e) {
         const float2 cs = turn[at + e];
         const float x = (float)p.v[e], y = (float)q.v[e];
         p.v[e] = (T)(x * cs.x - y * cs.y);
         q.v[e] = (T)(x * cs.y + y * cs.x);
       }
       q.stream_to(dst + at + a.rot / 2);
-    } else if (a.layout == TPLA_ROTARY_INTERLEAVED) {
+    } else if (W == 8 && a.layout == TPLA_ROTARY_INTERLEAVED) {
 #pragma unroll
-      for (int e = 0; e < 8; e += 2)
+      for (int e = 0; e + 1 < W; e += 2)
         if (at + e < a.rot) {
           const float2 cs = turn[(at + e) / 2];
           const float x = (float)p.v[e], y = (float)p.v[e + 1];
@@ -58,28 +70,10 @@ struct RowPart<T, true> {
     p.stream_to(dst + at);
   }
 };
-template <typename T>
-struct RowPart<T, false> {
-  T p, q;
-  __device__ __forceinline__ void load(const RotaryArgs& a, const T* src, int at, bool two) {
-    p = src[at];
-    if (two) q = src[at + (a.layout == TPLA_ROTARY_HALF ? a.rot / 2 : 1)];
-  }
-  __device__ __forceinline__ void store(const RotaryArgs& a, T* dst, int at, bool two, const float2* turn) {
-    const bool half = a.layout == TPLA_ROTARY_HALF;
-    if (two) {
-      const float2 cs = turn[half ? at : at / 2];
-      const float x = (float)p, y = (float)q;
-      p = (T)(x * cs.x - y * cs.y);
-      dst[at + (half ? a.rot / 2 : 1)] = (T)(x * cs.y + y * cs.x);
-    }
-    dst[at] = p;
-  }
-};
 
 // grid: (blocks of tokens, blocks of heads).  LDS: [tokens][rot / 2] pairs of (cos, sin), amplitude included.  A thread keeps its part of a row and
 // takes rows lanes_per_row threads apart, RO_BATCH of them on their way together; the keys are one more head.
-template <typename T, bool VEC>
+template <typename T, int W>
 __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a) {
   extern __shared__ float2 turns[];
   const int pairs = a.rot / 2, tid = threadIdx.x;
@@ -95,21 +89,20 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a) {
   __syncthreads();
   const bool half = a.layout == TPLA_ROTARY_HALF;
   // parts of a row: rotated ones (halves: of the first half), then what is copied
-  const int lead = VEC ? (half ? pairs / 8 : a.d_r / 8) : pairs;
-  const int parts = VEC ? (half ? lead + (a.d_r - a.rot) / 8 : lead) : pairs + (a.d_r - a.rot);
+  const int lead = half ? pairs / W : a.d_r / W, parts = half ? lead + (a.d_r - a.rot) / W : lead;
   const int at_once = max(1, RO_THREADS / parts);
   const int heads = (a.q ? a.H : 0) + (a.k ? 1 : 0);
   const int h0 = blockIdx.y * a.block_heads, nh = min(a.block_heads, heads - h0), rows = nt * nh;
   for (int part = tid % parts; part < parts; part += RO_THREADS) {       // (once, unless a row has more parts than there are threads)
     const int first = tid / parts;
     if (first >= at_once) continue;
-    const bool two = VEC ? half && part < lead : part < lead;
-    const int at = VEC ? (part < lead ? 8 * part : a.rot + 8 * (part - lead)) : part < lead ? (half ? part : 2 * part) : a.rot + part - lead;
+    const bool two = half && part < lead;
+    const int at = part < lead ? W * part : a.rot + W * (part - lead);
     // row = token * nh + head, walked without divisions
     const int dt = at_once / nh, dh = at_once % nh;
     int tt = first / nh, h = first % nh;
     for (int row = first; row < rows; row += RO_BATCH * at_once) {
-      RowPart<T, VEC> x[RO_BATCH];
+      RowPart<T, W> x[RO_BATCH];
       T* dst[RO_BATCH];
       int tok[RO_BATCH];
 #pragma unroll
@@ -139,7 +132,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a) {
 
 int launch_rotary(RotaryArgs a, int dtype, hipStream_t st) {
   const bool half = a.layout == TPLA_ROTARY_HALF;
-  const bool vec = !half || a.rot % 16 == 0;
+  const int w = !half || a.rot % 16 == 0 ? 8 : a.rot % 4 == 0 ? 2 : 1;
   const int heads = (a.q ? a.H : 0) + (a.k ? 1 : 0);
   // sines shared by the heads of a token; two tokens in a workgroup fill its threads, more leave some compute units behind
   // (4 tokens: 63 us for 20011 tokens and 9.0 for 2048; 2: 62 and 7.8; 1: 69 and 8.1)
@@ -147,8 +140,11 @@ int launch_rotary(RotaryArgs a, int dtype, hipStream_t st) {
   a.block_heads = a.T >= device_cu_count() ? heads : (heads + 3) / 4;
   const dim3 grid((unsigned)((a.T + a.block_tokens - 1) / a.block_tokens), (unsigned)((heads + a.block_heads - 1) / a.block_heads));
   const size_t lds = (size_t)a.block_tokens * (a.rot / 2) * sizeof(float2);
-  void (*fn)(RotaryArgs) = dtype == TPLA_F32 ? (vec ? rotary_kernel<float, true> : rotary_kernel<float, false>)
-                                             : (vec ? rotary_kernel<bf16_t, true> : rotary_kernel<bf16_t, false>);
+  void (*fn)(RotaryArgs);
+  if (dtype == TPLA_F32)
+    fn = w == 8 ? rotary_kernel<float, 8> : w == 2 ? rotary_kernel<float, 2> : rotary_kernel<float, 1>;
+  else
+    fn = w == 8 ? rotary_kernel<bf16_t, 8> : w == 2 ? rotary_kernel<bf16_t, 2> : rotary_kernel<bf16_t, 1>;
   hipLaunchKernelGGL(fn, grid, dim3(RO_THREADS), lds, st, a);
   return check_launch("rotary_kernel");
 }

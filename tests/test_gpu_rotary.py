@@ -159,3 +159,23 @@ def test_strides_of_single_tokens_and_heads_mean_nothing(T, H):
     for got, x in ((qo, before), (ko, kb), (q, before), (k, kb)):
         want, size = rotate64(x.double().cpu(), pos.cpu(), freq, 64, 0)
         assert_close(got, want, size, st)
+
+
+@pytest.mark.parametrize("T,H,d_r,rot,st", [
+    (33, 5, 64, 62, torch.bfloat16), (1100, 3, 64, 60, torch.bfloat16), (700, 9, 16, 6, torch.bfloat16), (5, 2, 128, 124, torch.float32),
+    (1031, 4, 64, 28, torch.float32), (50, 3, 24, 2, torch.float32), (50, 3, 24, 12, torch.float32), (7, 1, 1024, 1022, torch.bfloat16),
+])
+def test_halves_of_odd_and_even_numbers_of_columns(T, H, d_r, rot, st):
+    g = torch.Generator().manual_seed(T + rot)
+    wide = torch.randn((T, H, d_r + 8), generator=g).to(st)
+    q, k = wide[:, :, 8:], torch.randn((T, d_r), generator=g).to(st)
+    pos = torch.randint(0, 90000, (T,), generator=g).to(torch.int32)
+    freq = tp.tpla_rotary_frequencies(rot)
+    wd, kd = wide.cuda(), k.cuda()
+    tp.tpla_apply_rotary(shape(H, d_r, st), tp.TPLA_ROTARY_HALF, 0, rot, torch.from_numpy(freq).cuda(), 0.5, pos.cuda(), T, wd[:, :, 8:], wd[:, :, 8:], kd, kd)
+    torch.cuda.synchronize()
+    for got, x in ((wd[:, :, 8:], q), (kd, k)):
+        want, size = rotate64(x.double(), pos, freq, rot, tp.TPLA_ROTARY_HALF, 0.5)
+        assert_close(got, want, size, st)
+        assert torch.equal(got.cpu()[..., rot:], x[..., rot:])
+    assert torch.equal(wd.cpu()[:, :, :8], wide[:, :, :8])
