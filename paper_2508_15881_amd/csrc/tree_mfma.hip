@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
   constexpr int RC = Tile::RC, CPT = Tile::CPT, NSTAGE = Tile::NSTAGE;
   constexpr int KS = (DL + 64) / 32, DB = DL / 16;
   constexpr int KRING = 6, VRING = 4;
-  // streaming, not kept in L2 (32 x 32768 tokens, 64 rows: 284 -> 271 us with merge and combine; 64 x 8192, 80 rows: 204 -> 198; sixteen blocks of
+  // streaming, not kept in L2 (32 x 32768 tokens, 64 rows: 284 -> 271 us with merge and combine; 64 x 8192, 80 rows: 204 -> 198; eight blocks of
   // 128 rows, which find the rows of each other in the last-level cache, lose nothing)
   constexpr int STREAM = 2;
   extern __shared__ u32x4 smem[];
