@@ -435,8 +435,8 @@ int tpla_validate_block_table(const tpla_shape_t* shape, const int32_t* block_ta
  * rest of a row gets slot -1 and position 0, n_tokens = B * row_tokens.  cu_tokens int32 [B + 1] is the prefix sum of
  * add_lens either way, clipped to n_tokens.  counts int32 [2]: pages taken from the front of free_pages (the caller's next
  * list begins behind them), pages that were missing.  A sequence keeps the pages of rejected drafts and uses them first.
- * Where pages were missing, table entries behind pages_held_out[b] are as they were: before anything reads such tokens, call
- * again with pages_held_out for pages_held and more free pages, which places them all, or shorten the lengths.
+ * Where pages were missing, the entries of those that b wanted and was not given, pages_held_out[b] .. want_b - 1, become -1 (the entries behind
+ * want_b are as they were).  Another call with pages_held_out for pages_held and more free pages places all of the tokens.
  * Negative lengths count as 0, lengths beyond the row as the row's; a negative table entry gives slot
  * -1.  pages_held_out may be pages_held (for more than 1024 tokens a separate array saves a launch); no other
  * overlap.  All pointers are int32 DEVICE arrays; depths [B, row_tokens] or NULL; free_pages may be NULL with n_free =

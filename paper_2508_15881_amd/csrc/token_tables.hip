@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(EX_THREADS) extend_sequences_kernel(ExtendArgs
       if (b == 0) a.cu[0] = 0;
       a.cu[b + 1] = clip_int(end, a.n_tokens);
       a.held_out[b] = held + (int)given;
+      for (long long k = given; k < need; ++k) a.block_table[(size_t)b * a.max_pages + held + k] = -1;      // no page: see extend_together_kernel
     }
     first_of[tid] = from;
     held_of[tid] = held;
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(256) place_tokens_kernel(ExtendArgs a) {
 constexpr int EX_ROOM = 1024, EX_ONE = 256, EX_TOKENS = 1024;
 __global__ void __launch_bounds__(EX_ONE) extend_together_kernel(ExtendArgs a) {
   __shared__ long long part[EX_ONE / 64];
-  __shared__ int cu_of[EX_ROOM + 1], from_of[EX_ROOM], held_of[EX_ROOM], length_of[EX_ROOM], given_of[EX_ROOM];
+  __shared__ int cu_of[EX_ROOM + 1], from_of[EX_ROOM], held_of[EX_ROOM], length_of[EX_ROOM], given_of[EX_ROOM], need_of[EX_ROOM];
   const int tid = threadIdx.x;
   const unsigned cap = (unsigned)a.max_pages * (unsigned)a.page_tokens, pt = a.page_tokens;       // below 2^31
   long long tokens = 0, pages = 0;
@@ -173,6 +174,7 @@ __global__ void __launch_bounds__(EX_ONE) extend_together_kernel(ExtendArgs a) {
       cu_of[b + 1] = clip_int(end, a.n_tokens);
       from_of[b] = (int)min(first, (long long)a.n_free);
       given_of[b] = (int)min((long long)need, max(a.n_free - first, 0LL));
+      need_of[b] = need;
       held_of[b] = held;
       length_of[b] = L;
     }
@@ -181,7 +183,11 @@ __global__ void __launch_bounds__(EX_ONE) extend_together_kernel(ExtendArgs a) {
   if (blockIdx.x == 0) {
     for (int b = tid; b <= a.B; b += EX_ONE) {
       a.cu[b] = cu_of[b];
-      if (b < a.B) a.held_out[b] = held_of[b] + given_of[b];
+      if (b < a.B) {
+        a.held_out[b] = held_of[b] + given_of[b];
+        // A page that was not there is -1 and not whatever the row held: what reads the row knows that these tokens have no place.
+        for (int k = given_of[b]; k < need_of[b]; ++k) a.block_table[(size_t)b * a.max_pages + held_of[b] + k] = -1;
+      }
     }
     const long long taken = min(pages, (long long)a.n_free);
     if (tid == 0) a.counts[0] = (int)taken;
