@@ -490,7 +490,8 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
  * device; lse float [g,B,T,H] or NULL.  The other arguments as in tpla_decode_shards; any page size.  Bit-reproducible for
  * fixed arguments.  bf16 with d_r = 64 and d_c/g of 64, 128, 256 or 512 runs on the matrix cores, with the softmax weights
  * rounded to bf16 for the product with the values as in tpla_decode_shards; everything else in float
- * (TPLA_ERR_UNSUPPORTED beyond d_c/g = 1024 or d_c/g + d_r = 1984).
+ * (TPLA_ERR_UNSUPPORTED beyond d_c/g = 1024 or d_c/g + d_r = 1984).  max_pages_per_seq * page_tokens is at most 2^31 - 2^17
+ * (TPLA_ERR_UNSUPPORTED).
  */
 size_t tpla_workspace_bytes_tree(const tpla_shape_t* shape, int32_t T, int32_t max_pages_per_seq);
 int tpla_decode_shard_tree(const tpla_shape_t* shape, int32_t T, const void* q_lat_i, const void* q_pe, const void* shard_pool,

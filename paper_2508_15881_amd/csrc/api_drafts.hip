@@ -58,6 +58,9 @@ static int check_tree(const tpla_shape_t* sh, int n_shards, int32_t T, int32_t m
     return fail(TPLA_ERR_UNSUPPORTED, "B * T * H (or n_shards * B) too large");
   if (!tree_mfma_supported(*sh) && (dl > 1024 || dl + sh->d_r > 1984))
     return fail(TPLA_ERR_UNSUPPORTED, "d_c/g=%d above 1024, or d_c/g + d_r=%d above 1984", dl, dl + sh->d_r);
+  // token and page numbers stay int in the kernels: a split, a tile, the lanes of a wave or two chunks of page ids past the end included
+  if ((int64_t)max_pages * sh->page_tokens > ((int64_t)1 << 31) - (1 << 17))
+    return fail(TPLA_ERR_UNSUPPORTED, "max_pages_per_seq * page_tokens above 2^31 - 2^17");
   *p = plan_tree(*sh, n_shards, T, max_pages);
   const double tiles = ((double)max_pages * sh->page_tokens + 31) / 32, items = (double)n_shards * sh->B * p->blocks;
   if (p->mfma ? items * (tiles + 8) >= 2147483647.0 : items * p->n_splits >= 2147483647.0 || p->n_splits > 65535)
