@@ -376,6 +376,12 @@ __device__ __forceinline__ TreeLens tree_lens(const TreeArgs& a, int b) {
   return r;
 }
 
+// Drafts whose page the block table names, bit j for draft j: the others (negative entries) have no row in the cache and are seen by nobody.
+// Where a tile holds such tokens the kernels read page 0 in their place.  All lanes of a wave take part, each with the entry of draft `lane`; page:
+// that of token L + lane, clipped here (what lies beyond the row is not below TreeLens::keys).
+__device__ __forceinline__ int draft_entry(const TreeArgs& a, int b, int page) { return a.block_table[(size_t)b * a.max_pages + min(page, a.max_pages - 1)]; }
+__device__ __forceinline__ unsigned long long drafts_there(int entry) { return __ballot(entry >= 0); }
+
 int launch_stream_read(const void* buf, size_t bytes, void* sink, hipStream_t st);
 
 // PCA calibration: see pca.hip.

@@ -59,9 +59,10 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
 #pragma unroll
       for (int e = 0; e < 8; ++e) sm[8 * x + e] = q.v[e];
     }
+    const unsigned long long there = drafts_there(draft_entry(a, b, (len.L + lane) / a.page_tokens));
     unsigned long long bits[RW];
 #pragma unroll
-    for (int e = 0; e < RW; ++e) bits[e] = a.mask[(size_t)b * a.T + min(rw + e, rows - 1) / a.H];
+    for (int e = 0; e < RW; ++e) bits[e] = a.mask[(size_t)b * a.T + min(rw + e, rows - 1) / a.H] & there;
     const float* q = sm + RW * wave * w;
     float* mine = weights + wave * tokens * RW;     // [tokens][RW]
     const int parts = 64 / tokens, tok = lane % tokens, part = lane / tokens;
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
         for (int e = 0; e < TG_BATCH; ++e) {
           const int x = min(x0 + 256 * e, all - 1), k = x / pieces, t = min(s0 + k, k1 - 1), p = t / a.page_tokens;
           at[e] = k * (w + 4) + 8 * (x - k * pieces);
-          row[e] = ((size_t)a.block_table[(size_t)b * a.max_pages + p] * a.page_tokens + (t - p * a.page_tokens)) * w + 8 * (x - k * pieces);
+          row[e] = ((size_t)max(a.block_table[(size_t)b * a.max_pages + p], 0) * a.page_tokens + (t - p * a.page_tokens)) * w + 8 * (x - k * pieces);
         }
         Vec8 r[TG_BATCH];
 #pragma unroll

@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       const int k0 = t * TR_TOK, p0 = __builtin_amdgcn_readfirstlane(page_of(k0));
       char* dst = lds + (t % NSTAGE) * Tile::BYTES + wave * 1024;
       if (one_page && k0 + TR_TOK <= keys) {
-        const int page = __builtin_amdgcn_readfirstlane(id);
+        const int page = max(__builtin_amdgcn_readfirstlane(id), 0);
         const char* src = pool + ((size_t)page * pt + (k0 - p0 * pt)) * (RC * 16);
 #pragma unroll
         for (int j = 0; j < CPT; ++j)
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
 #pragma unroll 1
         for (int j = 0; j < CPT; ++j) {
           const int x = (wave + j * TR_NW) * 64 + here(lane), tok = x / RC, k = min(k0 + tok, keys - 1), p = page_of(k);
-          const int row_id = (int)lds_read_id(id_at(p));
+          const int row_id = max((int)lds_read_id(id_at(p)), 0);
           const char* src = pool + ((size_t)row_id * pt + (k - p * pt)) * (RC * 16) + ((x % RC) ^ swz(tok)) * 16;
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                            (__attribute__((address_space(3))) void*)(dst + j * TR_NW * 1024), 16, 0, 0);
@@ -400,6 +400,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       continue;
     }
 
+    int entry = draft_entry(a, b, page_of(L + lane));
     // ---- queries as B operands: block r, lane holds row row0 + 16 r + j16 ----
     bf16x8 q[RB][KS - QL];
 #pragma unroll
@@ -418,6 +419,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       });
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));        // complete before the loop: nothing there waits for them
+    asm volatile("" : "+v"(entry));
     first_tiles();
 
     f32x4 s[RB][2], next[RB][2];
@@ -491,10 +493,11 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       constexpr bool LAST = decltype(last_tile)::value;
       if ((t + 1) * TR_TOK > L) {                    // drafts, or past the end: masked here, and looked at again
         over = 0;
+        const unsigned long long there = drafts_there(here(entry));
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
           const int row = min(row0 + 16 * r + here(j16), rows - 1);
-          const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H];
+          const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H] & there;
 #pragma unroll
           for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -706,7 +709,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
       const int k0 = t * TP_TOK, p0 = __builtin_amdgcn_readfirstlane(page_of(k0));
       char* dst = lds + (t % NSTAGE) * Tile::BYTES + wave * 1024;
       if (one_page && k0 + TP_TOK <= keys) {
-        const int page = __builtin_amdgcn_readfirstlane(lds_read_id(id_at(p0)));
+        const int page = max(__builtin_amdgcn_readfirstlane(lds_read_id(id_at(p0))), 0);
         const char* src = pool + ((size_t)page * pt + (k0 - p0 * pt)) * (RC * 16);
 #pragma unroll
         for (int j = 0; j < CPT; ++j)
@@ -717,7 +720,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
 #pragma unroll 1
         for (int j = 0; j < CPT; ++j) {
           const int x = (wave + j * TP_NW) * 64 + here(lane), tok = x / RC, k = min(k0 + tok, keys - 1), p = page_of(k);
-          const int row_id = (int)lds_read_id(id_at(p));
+          const int row_id = max((int)lds_read_id(id_at(p)), 0);
           const char* src = pool + ((size_t)row_id * pt + (k - p * pt)) * (RC * 16) + ((x % RC) ^ swz(tok)) * 16;
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                            (__attribute__((address_space(3))) void*)(dst + j * TP_NW * 1024), 16, 0, STREAM);
@@ -737,6 +740,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
     for (int t = t0; t < t1 && t < t0 + NSTAGE - 1; ++t) issue(t);
     walk.note(a);
 
+    const int entry = draft_entry(a, b, page_of(L + lane));
     bf16x8 q[KS];
     {
       const int row = min(row0 + j16, rows - 1);
@@ -747,6 +751,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[ks]));   // complete before the loop
     }
+    const unsigned long long there = drafts_there(entry);
     f32x4 acc[DB];
     float m_run = -FLT_MAX, l_run = 0.f;             // see the kernel above
 #pragma unroll
@@ -805,7 +810,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
       };
       if (tail) {
         const int row = min(row0 + here(j16), rows - 1);
-        const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H];
+        const unsigned long long bits = a.mask[(size_t)b * a.T + row / a.H] & there;
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
