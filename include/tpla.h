@@ -517,9 +517,10 @@ int tpla_decode_shards_tree_combine(const tpla_shape_t* shape, int32_t T, const 
 /*
  * The accepted drafts of every sequence behind its committed tokens: for k < n_accepted[b], in all g pools,
  *     row of token seq_lens[b] + k  =  row of token seq_lens[b] + accepted[b, k]   (as it was before the call)
- * and new_lens[b] = seq_lens[b] + n_accepted[b].  accepted int32 [B, T]: indices into the drafts, strictly ascending (a
+ * and new_lens[b] = seq_lens[b] + n_accepted[b], clipped as below.  accepted int32 [B, T]: indices into the drafts, strictly ascending (a
  * path of a tree whose parents come before their children); n_accepted int32 [B], clipped to [0, T] and to the
- * block-table row. Entries outside [0, T) are clipped; another order gives wrong rows, never an access outside the
+ * block-table row, and to the drafts before the first accepted one whose page (or the page it moves to) is a negative table entry: that
+ * one has no row.  Entries outside [0, T) are clipped; another order gives wrong rows, never an access outside the
  * pages that the block-table row lists.  new_lens may be seq_lens.  No two sequences may share the pages that hold their
  * drafts.  Rows are copied bit for bit.  d_n, d_v, H of shape are not used.
  */

@@ -264,19 +264,31 @@ int launch_extend_sequences(const ExtendArgs& a, hipStream_t st) {
 constexpr int CM_THREADS = 1024, CM_BATCH = 8;
 __global__ void __launch_bounds__(CM_THREADS) commit_drafts_kernel(CommitArgs a) {
   __shared__ long long src_of[TPLA_MAX_DRAFTS], dst_of[TPLA_MAX_DRAFTS];      // byte offsets in a pool; -1: stays where it is
+  __shared__ int n_of;
   const int b = blockIdx.x, tid = threadIdx.x;
   const unsigned cap = (unsigned)a.max_pages * (unsigned)a.page_tokens, pt = a.page_tokens;       // below 2^31
   const int picked = tid < a.T ? a.accepted[(size_t)b * a.T + tid] : 0;
-  const int L = clip_int(a.seq_lens[b], cap), n = min(clip_int(a.n_accepted[b], a.T), (int)min(cap - L, (unsigned)a.T));
-  if (tid < n) {
-    const int j = min(max(picked, 0), a.T - 1);
-    const unsigned from = (unsigned)L + j, to = (unsigned)L + tid;
-    const int32_t* table = a.block_table + (size_t)b * a.max_pages;
-    const bool moves = j != tid && from < cap;
-    src_of[tid] = moves ? ((long long)table[from / pt] * pt + from % pt) * a.row_bytes : -1;
-    dst_of[tid] = ((long long)table[to / pt] * pt + to % pt) * a.row_bytes;
+  const int L = clip_int(a.seq_lens[b], cap);
+  if (tid < 64) {                                    // (one wave: a draft each)
+    int n = min(clip_int(a.n_accepted[b], a.T), (int)min(cap - L, (unsigned)a.T));
+    bool placed = true;
+    if (tid < n) {
+      const int j = min(max(picked, 0), a.T - 1);
+      const unsigned from = (unsigned)L + j, to = (unsigned)L + tid;
+      const int32_t* table = a.block_table + (size_t)b * a.max_pages;
+      const bool there = from < cap, moves = j != tid && there;
+      const int to_page = table[to / pt], from_page = there ? table[from / pt] : to_page;
+      placed = (to_page | from_page) >= 0;
+      src_of[tid] = moves ? ((long long)from_page * pt + from % pt) * a.row_bytes : -1;
+      dst_of[tid] = ((long long)to_page * pt + to % pt) * a.row_bytes;
+    }
+    // a draft without a page was never written: the path ends before it
+    const unsigned long long absent = __ballot(!placed);
+    if (absent) n = __builtin_ctzll(absent);
+    if (tid == 0) n_of = n;
   }
   __syncthreads();
+  const int n = n_of;
   if (tid == 0) a.new_lens[b] = L + n;               // (every wave has read the length that it may replace)
   const unsigned pieces = a.row_bytes / 16, per_row = pieces * a.n_shards;
   // whole rows per step, so that no row is written while another thread has yet to read it; a row wider than a step goes in parts, whose
