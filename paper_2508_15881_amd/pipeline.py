@@ -159,7 +159,8 @@ class DraftStep:
 
     def place(self, seq_lens, draft_lens, depths, free_pages, n_free, pages_held, block_table):
         """Pages, slots and positions of the drafts (once per step, for all layers); pages_held is updated, counts are the pages
-        taken from free_pages and those that were missing (which the caller provides in another call, or drafts less)."""
+        taken from free_pages and those that were missing.  Drafts of missing pages have slot -1 and a negative table entry: run
+        writes no row for them and no draft sees them, commit ends a path before them, so a step may go on without a look at counts."""
         B.tpla_extend_sequences(self.shape, seq_lens, draft_lens, self.T, depths, free_pages, n_free, pages_held, pages_held, block_table,
                                 self.max_pages, self.cu, self.slots, self.positions, self.slots.numel(), self.counts)
 
@@ -177,7 +178,8 @@ class DraftStep:
         return self.o
 
     def commit(self, accepted, n_accepted, seq_lens, new_lens, block_table, shard_pools):
-        """Accepted drafts' rows behind the committed ones (per layer); new_lens may be seq_lens where one layer is all."""
+        """Accepted drafts' rows behind the committed ones (per layer); new_lens, which counts the drafts that had a page, may be seq_lens
+        where one layer is all."""
         B.tpla_commit_drafts(self.shape, self.T, accepted, n_accepted, seq_lens, block_table, self.max_pages, shard_pools, new_lens)
 
 
