@@ -484,7 +484,8 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
  *     o_lat_i[b,t,h,:] = sum_k softmax(s)_k row_k[:d_c/g]       lse_i[b,t,h] = log sum_k exp(s_k)
  * A row that sees nothing, and rows t >= draft_lens[b], get o = 0, lse = -inf.  A draft whose page is a negative entry of the block table (the
  * free pages ran out) is seen by no row; the rows of such drafts are computed like others.  What a draft's row holds (infinities and NaN
- * too) does not reach rows that do not see it; bits at or beyond draft_lens[b] are ignored; slots at or beyond seq_lens[b] +
+ * too) does not reach rows that do not see it; for those that do the formulas hold, 0 * inf (a score of -inf) included, as for a committed
+ * token.  Bits at or beyond draft_lens[b] are ignored; slots at or beyond seq_lens[b] +
  * draft_lens[b] are never read.  Lengths out of range are clipped as in tpla_decode_shard (drafts beyond the block-table row
  * are not seen).  q_lat [g,B,T,H,d_c/g], q_pe [B,T,H,d_r] in shape->dtype: the layout of tpla_absorb_query, and o_lat float
  * [g,B,T,H,d_c/g] that of tpla_combine_shards, called with B T rows.  tree_mask uint64 [B,T] and draft_lens int32 [B] on the

@@ -381,6 +381,11 @@ __device__ __forceinline__ TreeLens tree_lens(const TreeArgs& a, int b) {
 // that of token L + lane, clipped here (what lies beyond the row is not below TreeLens::keys).
 __device__ __forceinline__ int draft_entry(const TreeArgs& a, int b, int page) { return a.block_table[(size_t)b * a.max_pages + min(page, a.max_pages - 1)]; }
 __device__ __forceinline__ unsigned long long drafts_there(int entry) { return __ballot(entry >= 0); }
+// The drafts that draft t sees.  (A sum of weights that is 0 is that of a row that sees no token, or of one whose scores are all -inf: 0 / 0.)
+__device__ __forceinline__ unsigned long long drafts_seen(const TreeArgs& a, int b, int t, int L, int keys, unsigned long long there) {
+  const int n = keys - L;                            // drafts within the row
+  return a.mask[(size_t)b * a.T + t] & there & (n < 64 ? (1ull << n) - 1 : ~0ull);
+}
 
 int launch_stream_read(const void* buf, size_t bytes, void* sink, hipStream_t st);
 

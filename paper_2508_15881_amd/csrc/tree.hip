@@ -19,6 +19,10 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
+__device__ __forceinline__ unsigned long long tree_seen(const TreeArgs& a, const TreeLens& len, int b, int t) {      // (all lanes of the wave)
+  return drafts_seen(a, b, t, len.L, len.keys, drafts_there(draft_entry(a, b, (len.L + (int)(threadIdx.x & 63)) / a.page_tokens)));
+}
+
 // LDS of the general kernel, in floats: queries [rows][w], weights [tokens][rows], rows [stage][w + 4] (an odd number of 16-byte pieces: the
 // lanes of a column spread over the banks).
 __host__ __device__ constexpr int tg_floats(int w, int rows, int tokens, int stage) { return rows * w + tokens * rows + stage * (w + 4); }
@@ -164,6 +168,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
     if (r >= all_rows) continue;
     const size_t out = (size_t)v * all_rows + r;
     if (a.p.n_splits == 1) {
+      if (l[e] == 0.f && r < rows && (len.L > 0 || tree_seen(a, len, b, r / a.H) != 0)) l[e] = __builtin_nanf("");
       const float inv = l[e] != 0.f ? 1.0f / l[e] : 0.f;
 #pragma unroll
       for (int d = 0; d < DC; ++d)
@@ -202,7 +207,9 @@ int launch_tree_generic(const TreeArgs& a, int dtype, hipStream_t st) {
 
 // Merge: a wave takes one row after another of an item, MERGE_LOADS slots' rows on their way together, the first of them requested with their references
 // (each is a round trip to memory); the lanes hold the references and weights of 64 slots at a time, and the rows are added in ascending order.  Rows of
-// drafts that do not exist get zeros and -inf here.  grid: (groups of `group` rows, a multiple of 4 that divides 16, of a (slice, sequence), (slice, sequence)).
+// drafts that do not exist get zeros and -inf here.  grid: (groups of `group` rows, a multiple of 4 that divides 16, of a (slice, sequence), (slice,
+// sequence)).  Where the matrix kernels put zeros in the place of drafts' values that are not finite (a negative sum, or -1 partial results of an
+// item that one workgroup had whole), rows that see such a draft get NaN in its column, whatever its weight: 0 * inf where its score is -inf.
 constexpr int MERGE_LOADS = 8;
 __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int group) {
   const int v = blockIdx.y, b = v % a.B, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -222,6 +229,7 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int group) 
     n = a.p.n_splits;
   }
   const int rows = tree_lens(a, b).n * a.H;
+  unsigned cleaned = 0, empty = 0;                              // rows of the group
   for (int e = wave; e < group; e += 4) {
     const int r = r0 + e;
     if (r >= all_rows) break;
@@ -231,7 +239,10 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int group) 
       if (a.lse && lane == 0) a.lse[(size_t)v * all_rows + r] = -INFINITY;
       continue;
     }
-    if (n == 1 && a.p.mfma) continue;                           // written by the workgroup that had it whole
+    if (n <= 1 && a.p.mfma) {                                   // written by the workgroup that had it whole
+      if (n < 0) cleaned |= 1u << e;
+      continue;
+    }
     const size_t local = r % a.p.block;
     auto slot = [&](int s) { return (size_t)(s == 0 ? first : next + (s - 1) * step) * a.p.block + local; };
     auto request = [&](f32x4 (&p)[MERGE_LOADS], int s0, int c) {
@@ -256,7 +267,10 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int group) 
           if (s0 + lane < n) q = *reinterpret_cast<const float2*>(a.part_ml + 2 * slot(s0 + lane));
         }
         const float w = exp2f(q.x - ref);
-        if (c0 == 0) l += wave_sum(q.y * w);
+        if (c0 == 0) {
+          l += wave_sum(fabsf(q.y) * w);
+          if (__any(__float_as_int(q.y) < 0)) cleaned |= 1u << e;
+        }
         const int here = min(64, n - s0);
         for (int s = 0; s < here; s += MERGE_LOADS) {
           if (c0 + s0 + s > 0) request(p, s0 + s, c);
@@ -269,6 +283,30 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int group) 
       if (c0 + 4 * lane < a.dl) *reinterpret_cast<f32x4*>(out + c) = x * inv;
     }
     if (a.lse && lane == 0) a.lse[(size_t)v * all_rows + r] = merge_lse(M, l);
+    if (l == 0.f) empty |= 1u << e;
+  }
+  // ---- rare: rows of the matrix kernels whose drafts' values were cleaned, and rows without a weight ----
+  if (!a.p.mfma) cleaned = 0;
+  for (unsigned left = cleaned | empty; left; left &= left - 1) {
+    const int e = __builtin_ctz(left), r = r0 + e;
+    const TreeLens len = tree_lens(a, b);
+    unsigned long long seen = tree_seen(a, len, b, r / a.H);
+    float* out = a.o_lat + ((size_t)v * all_rows + r) * a.dl;   // (a lane's columns are those it wrote above)
+    const float nan = __builtin_nanf("");
+    if (((empty >> e) & 1) && (seen != 0 || len.L > 0)) {       // every score -inf: 0 / 0
+      for (int c = 4 * lane; c < a.dl; c += 256) *reinterpret_cast<f32x4*>(out + c) = f32x4{nan, nan, nan, nan};
+      if (a.lse && lane == 0) a.lse[(size_t)v * all_rows + r] = nan;
+    } else if ((cleaned >> e) & 1) {                            // a value that is not finite, whatever its weight (0 * inf where its score is -inf)
+      for (; seen; seen &= seen - 1) {
+        const int k = len.L + __builtin_ctzll(seen), p = k / a.page_tokens;
+        const unsigned short* row = static_cast<const unsigned short*>(tree_pool(a, v / a.B)) +
+                                    ((size_t)a.block_table[(size_t)b * a.max_pages + p] * a.page_tokens + (k - p * a.page_tokens)) * (a.dl + a.d_r);
+        for (int c = 4 * lane; c < a.dl; c += 256)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if ((row[c + x] & 0x7F80) == 0x7F80) out[c + x] = nan;
+      }
+    }
   }
 }
 

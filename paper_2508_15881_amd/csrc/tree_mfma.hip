@@ -34,7 +34,7 @@ struct TreeTile {
   static constexpr int Q_BYTES = TR_NW * RB * QL * 1024;
   static constexpr int FIT = (158 * 1024 - Q_BYTES - TR_ID_RING * 4) / BYTES;
   static constexpr int NSTAGE = FIT < 8 ? FIT : 8;      // tiles in flight or in use; at most 8 (see TR_IDS)
-  static constexpr int IDS = NSTAGE * BYTES, Q = IDS + TR_ID_RING * 4, LDS = Q + Q_BYTES;
+  static constexpr int IDS = NSTAGE * BYTES, Q = IDS + TR_ID_RING * 4, CLEANED = Q + Q_BYTES, LDS = CLEANED + 16;
   static_assert(TR_TOK * RC % (64 * TR_NW) == 0, "every wave issues the same number of loads");
   static_assert(NSTAGE >= 4, "a tile whose values are read, two whose scores are, and one on its way");
 };
@@ -262,6 +262,13 @@ __device__ __forceinline__ T here(T x) {
   return x;
 }
 
+// Zero for what is not finite among two bfloat16.
+__device__ __forceinline__ unsigned finite_pair(unsigned u) {
+  if ((u & 0x7F80u) == 0x7F80u) u &= 0xFFFF0000u;
+  if ((u & 0x7F800000u) == 0x7F800000u) u &= 0xFFFFu;
+  return u;
+}
+
 template <int DL, int RB, int QL>
 __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   using Tile = TreeTile<DL, RB, QL>;
@@ -272,6 +279,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
   using Reads = ScoreReads<KS, QL, RB, RING>;
   extern __shared__ u32x4 smem[];
   char* const lds = reinterpret_cast<char*>(smem);
+  volatile int* const cleaned = reinterpret_cast<volatile int*>(lds + Tile::CLEANED);      // some value of this item's tiles was
   const unsigned lds_base = lds_at(lds);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -344,6 +352,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       }
     };
     lds_barrier();                                   // the item before this one no longer reads LDS
+    if (tid == 0) *cleaned = 0;
     request_ids(chunk);
     request_ids(chunk + 1);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -363,7 +372,8 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       if (t + NSTAGE - 1 < t1) issue(t + NSTAGE - 1, id);
     };
     // Values of drafts are masked per row, and a weight of zero does not silence an infinity or a NaN: what is not finite in tile t becomes
-    // zero here, behind its scores and ahead of the product with its weights.  A row that sees such a draft has it in its score already.
+    // zero here, behind its scores and ahead of the product with its weights.  The merge makes it good for the rows that see such a draft; it is told
+    // by the sign of the partial sums, or by -1 workgroups of an item that one has whole.
     auto clean = [&](int t) {
       lds_barrier();
 #pragma unroll 1
@@ -371,13 +381,10 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
         const int tok = x / RC, c = (x % RC) ^ swz(tok);
         if (c >= DL / 8 || t * TR_TOK + tok < L) continue;
         u32x4* at = smem + (t % NSTAGE) * (TR_TOK * RC) + x;
-        u32x4 u = *at;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
-          if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
-        }
+        const u32x4 was = *at, u = {finite_pair(was[0]), finite_pair(was[1]), finite_pair(was[2]), finite_pair(was[3])};
+        if (((u[0] ^ was[0]) | (u[1] ^ was[1]) | (u[2] ^ was[2]) | (u[3] ^ was[3])) == 0) continue;
         *at = u;
+        *cleaned = 1;
       }
       lds_barrier();
     };
@@ -610,6 +617,8 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
 
     // ---- the item's result, or a partial one ----
     mm_settle_result();
+    const int was_cleaned = *cleaned;
+    if (was_cleaned && walk.whole && tid == 0) a.plan[3 * walk.item + 1] = -1;
     static_for<RB>([&](auto rc) {
       constexpr int r = decltype(rc)::value;
       const int local = wave * (16 * RB) + 16 * r + here(j16), row = rb * a.p.block + local;
@@ -617,6 +626,10 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
       const bool there = row < rows;
+      if (walk.whole && __any(l == 0.f)) {
+        const unsigned long long drafts = drafts_there(here(entry));
+        if (there && l == 0.f && (L > 0 || drafts_seen(a, b, row / a.H, L, keys, drafts) != 0)) l = __builtin_nanf("");
+      }
       const float inv = walk.whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
       float* out = walk.whole ? a.o_lat + ((size_t)v * all_rows + row) * DL : a.part_acc + ((size_t)walk.slot * a.p.block + local) * DL;
       static_for<DB>([&](auto dc) {
@@ -627,7 +640,7 @@ __global__ void __launch_bounds__(TR_NW * 64, 1) tree_mfma_kernel(TreeArgs a) {
       acc_keep();
       if (there && q4 == 0) {
         if (!walk.whole)
-          *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)walk.slot * a.p.block + local)) = make_float2(m_run[r], l);
+          *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)walk.slot * a.p.block + local)) = make_float2(m_run[r], was_cleaned ? -l : l);
         else if (a.lse)
           a.lse[(size_t)v * all_rows + row] = l != 0.f ? (m_run[r] + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
@@ -650,7 +663,7 @@ struct PairTile {
   static constexpr int BYTES = TP_TOK * RC * 16;       // a round
   static constexpr int CPT = TP_TOK * RC / 64 / TP_NW;
   static constexpr int NSTAGE = 3;
-  static constexpr int IDS = NSTAGE * BYTES, LDS = IDS + TR_ID_RING * 4;
+  static constexpr int IDS = NSTAGE * BYTES, CLEANED = IDS + TR_ID_RING * 4, LDS = CLEANED + 16;
   static_assert(TP_TOK * RC % (64 * TP_NW) == 0, "every wave issues the same number of loads");
   static_assert(4 * (DL / 16 + 1) * 1024 <= NSTAGE * BYTES, "the join of two teams fits the ring");
 };
@@ -666,6 +679,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
   constexpr int STREAM = 2;
   extern __shared__ u32x4 smem[];
   char* const lds = reinterpret_cast<char*>(smem);
+  volatile int* const cleaned = reinterpret_cast<volatile int*>(lds + Tile::CLEANED);      // some value of this item's tiles was
   const unsigned lds_base = lds_at(lds);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -733,6 +747,7 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
       }
     };
     lds_barrier();                                   // the item before this one no longer reads LDS
+    if (tid == 0) *cleaned = 0;
     request_ids(chunk);
     request_ids(chunk + 1);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -764,13 +779,10 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
         const int tok = x / RC, c = (x % RC) ^ swz(tok);
         if (c >= DL / 8 || t * TP_TOK + tok < L) continue;
         u32x4* at = smem + (t % NSTAGE) * (TP_TOK * RC) + x;
-        u32x4 u = *at;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
-          if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
-        }
+        const u32x4 was = *at, u = {finite_pair(was[0]), finite_pair(was[1]), finite_pair(was[2]), finite_pair(was[3])};
+        if (((u[0] ^ was[0]) | (u[1] ^ was[1]) | (u[2] ^ was[2]) | (u[3] ^ was[3])) == 0) continue;
         *at = u;
+        *cleaned = 1;
       }
       lds_barrier();
     };
@@ -886,18 +898,21 @@ __global__ void __launch_bounds__(TP_NW * 64, 2) tree_pair_kernel(TreeArgs a) {
         for (int d = 0; d < DB; ++d) acc[d] = acc[d] * mine + *reinterpret_cast<const f32x4*>(at + d * 1024) * theirs;
       }
     }
+    const int was_cleaned = *cleaned;
+    if (was_cleaned && walk.whole && tid == 0) a.plan[3 * walk.item + 1] = -1;
     float l = l_run;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     const int local = member * 16 + j16, row = row0 + j16;
     if (!alive || row >= rows) continue;
+    if (walk.whole && l == 0.f && (L > 0 || drafts_seen(a, b, row / a.H, L, keys, there) != 0)) l = __builtin_nanf("");
     const float inv = walk.whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
     float* out = walk.whole ? a.o_lat + ((size_t)v * all_rows + row) * DL : a.part_acc + ((size_t)walk.slot * a.p.block + local) * DL;
 #pragma unroll
     for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(out + 16 * d + 4 * q4) = acc[d] * inv;
     if (q4 == 0) {
       if (!walk.whole)
-        *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)walk.slot * a.p.block + local)) = make_float2(m_run, l);
+        *reinterpret_cast<float2*>(a.part_ml + 2 * ((size_t)walk.slot * a.p.block + local)) = make_float2(m_run, was_cleaned ? -l : l);
       else if (a.lse)
         a.lse[(size_t)v * all_rows + row] = l != 0.f ? (m_run + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }
