@@ -30,7 +30,7 @@ __host__ __device__ constexpr int tg_floats(int w, int rows, int tokens, int sta
 // grid: (items of 4 RW rows, splits).  The rows of `stage` tokens are staged as floats, as many as LDS holds: short contexts are two round trips to
 // memory and not two for every 64 tokens.  Of these a wave scores `tokens` (a power of two up to 64 that divides stage) at a time for its RW rows,
 // 64 / tokens lanes per token, then its lanes hold columns.  Masked tokens are not multiplied by zero but left out: their rows
-// may hold anything.  DC: columns per lane.
+// may hold anything (a token that is seen with weight 0 is not: 0 * inf).  DC: columns per lane.
 template <typename T, int DC, int RW>
 __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int tokens, int stage) {
   extern __shared__ __align__(16) float sm[];
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
           const float x = sees ? s[e] * a.scale_log2 : -INFINITY;
           const float m_new = fmaxf(m[e], wave_max(x));
           const float ref = m_new == -INFINITY ? 0.f : m_new;
-          const float alpha = exp2f(m[e] - ref), p = exp2f(x - ref);
+          const float alpha = exp2f(m[e] - ref), p = sees ? exp2f(x - ref) : -0.f;       // -0: not seen, which 0 (a score of -inf) is
           l[e] = fmaf(l[e], alpha, wave_sum(part == 0 ? p : 0.f));
           m[e] = m_new;
 #pragma unroll
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
           if (part == 0) mine[tok * RW + e] = p;
         }
         wave_lds_order();
-        // (tokens past the end have weight 0; of committed ones nothing is masked)
+        // (tokens past the end are not seen; of committed ones nothing is masked)
         const int plain = min(len.L, k1) - t0;
         for (int k = 0; k < tokens; k += TG_TOKENS * groups) {
           Weights p[TG_TOKENS];
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(256) tree_generic_kernel(TreeArgs a, int token
 #pragma unroll
               for (int d = 0; d < DC; ++d)
 #pragma unroll
-                for (int e = 0; e < RW; ++e) acc[e][d] = p[u][e] != 0.f ? fmaf(p[u][e], x[u][d], acc[e][d]) : acc[e][d];
+                for (int e = 0; e < RW; ++e) acc[e][d] = __float_as_uint(p[u][e]) != 0x80000000u ? fmaf(p[u][e], x[u][d], acc[e][d]) : acc[e][d];
           }
         }
         wave_lds_order();

@@ -90,3 +90,58 @@ def test_committing_the_draft_changes_nothing(dtype, H, L):
     tp.tpla_decode_shards(p.shape, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"] + 1, 0, ws, n, o2, lse2)
     torch.cuda.synchronize()
     assert np.array_equal(np.isnan(o), np.isnan(o2.cpu().numpy())) and np.array_equal(np.isnan(lse), np.isnan(lse2.cpu().numpy()))
+
+
+GENERAL = [("f32", 32, 2, 4, 5, [126, 0]), ("f32", 256, 1, 3, 6, [900, 13]), ("f32", 8, 2, 3, 3, [70, 1]), ("f32", 64, 8, 64, 16, [90, 32]), ("f32", 32, 1, 4, 5, [3001, 0]),
+           ("bf16", 72, 2, 6, 5, [70, 3])]
+
+
+@pytest.mark.parametrize("negative", [False, True])
+@pytest.mark.parametrize("dtype,dl,g,H,T,lens", GENERAL)
+def test_an_infinity_in_one_column_of_the_general_kernel(dtype, dl, g, H, T, lens, negative):
+    masks = np.array([[(2 << t) - 1 for t in range(T)]] * 2, dtype=np.uint64)
+    masks[:, T - 1] = 1 << (T - 1)
+    both = set()
+    for b, j, column in ((0, 1, 5), (1, 0, dl - 1), (0, T - 2, 0)):
+        print("infinity, general", dtype, dl, g, H, T, lens, negative, b, j, column, flush=True)
+        p = TreeProblem(lens, [T, T], T, H=H, g=g, dl=dl, d_r=16, dtype=dtype, seed=dl + H + T + j, masks=masks)
+        ref, kinds = with_infinity(p, b, j, column, negative)
+        both |= kinds
+        o, lse = run_all(p)
+        assert_close(p, o, lse, ref)
+        assert np.array_equal(np.isnan(lse), np.isnan(ref[1]))
+    assert both == {True, False}
+
+
+@pytest.mark.parametrize("dtype,dl,H,L", [("f32", 32, 4, 71), ("f32", 256, 3, 71), ("bf16", 72, 6, 71), ("f32", 64, 4, 301), ("bf16", 256, 16, 71), ("bf16", 64, 16, 301)])
+def test_an_infinity_of_a_committed_token_wherever_it_stands(dtype, dl, H, L):
+    """In a group of tokens of its own kind, beside drafts, last before them."""
+    T = 3
+    for k in (0, L // 2, L - 3, L - 2, L - 1):
+        print("infinity, committed", dtype, dl, H, L, k, flush=True)
+        p = TreeProblem([L], [T], T, H=H, g=1, dl=dl, d_r=64 if dl in (64, 256) and dtype == "bf16" else 16, dtype=dtype, seed=dl + L)
+        page, off = p.row_of(0, k)
+        p.pools[0][page, off, 2] = INF[dtype]
+        o, _ = run_all(p)
+        q = wl.as_f64(p.q_lat, dtype)[0, 0, :, :, 2]
+        want = np.zeros(o.shape, dtype=bool)
+        want[0, 0][q >= 0] = True
+        want[0, 0, ..., 2] = True
+        assert (q < 0).any() and (q > 0).any() and np.array_equal(np.isnan(o), want)
+
+
+@pytest.mark.parametrize("L", [0, 63, 600])
+def test_committing_a_float_draft_changes_nothing(L):
+    p = TreeProblem([L, 40], [1, 1], 1, H=4, dl=64, d_r=16, masks=[[1], [1]], dtype="f32", seed=6)
+    ref, kinds = with_infinity(p, 0, 0, 9)
+    assert kinds == {True, False}
+    d = p.device()
+    o, lse = run_all(p, d)
+    assert_close(p, o, lse, ref)
+    o2, lse2 = out_buffers(p)
+    n = tp.tpla_workspace_bytes_all(p.shape, p.max_pages, 0)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    tp.tpla_decode_shards(p.shape, d["q_lat"], d["q_pe"], d["pools"], d["bt"], p.max_pages, d["lens"] + 1, 0, ws, n, o2, lse2)
+    torch.cuda.synchronize()
+    print(np.isnan(o).sum(), np.isnan(o2.cpu().numpy()).sum(), lse[0, 0], lse2[0, 0])
+    assert np.array_equal(np.isnan(o), np.isnan(o2.cpu().numpy())) and np.array_equal(np.isnan(lse), np.isnan(lse2.cpu().numpy()))
