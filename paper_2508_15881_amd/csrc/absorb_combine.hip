@@ -331,6 +331,12 @@ __global__ void __launch_bounds__(256) combine_shards_vec_kernel(const float* __
   }
 }
 
+// Whether launch_combine_shards has a launch for so many rows and columns (its fastest kernel's is smaller, and the general kernel steps in).
+int check_combine_grid(const tpla_shape_t& sh) {
+  if ((sh.d_v + 127) / 128 > 65535 || ((int64_t)sh.B + BT - 1) / BT > 65535) return fail(TPLA_ERR_UNSUPPORTED, "grid too large");
+  return TPLA_OK;
+}
+
 template <typename OT>
 static int launch_combine_shards_to(const tpla_shape_t& sh, const float* o_lat, const void* W_UV_t, OT* o,
                                     hipStream_t st) {
@@ -347,8 +353,9 @@ static int launch_combine_shards_to(const tpla_shape_t& sh, const float* o_lat, 
       return check_launch("combine_shards_vec_kernel");
     }
   }
+  const int rc = check_combine_grid(sh);
+  if (rc) return rc;
   const dim3 grid((unsigned)sh.H, (unsigned)((sh.d_v + 127) / 128), (unsigned)((sh.B + BT - 1) / BT));
-  if (grid.y > 65535 || grid.z > 65535) return fail(TPLA_ERR_UNSUPPORTED, "grid too large");
   if (sh.dtype == TPLA_F32)
     hipLaunchKernelGGL((combine_shards_kernel<float, OT>), grid, dim3(128), 0, st, o_lat,
                        static_cast<const float*>(W_UV_t), o, sh.B, sh.H, sh.d_c, sh.d_v, sh.g);

@@ -270,11 +270,14 @@ int tpla_decode_shards_tree_combine(const tpla_shape_t* shape, int32_t T, const 
   if (!W_UV_t || !o) return fail(TPLA_ERR_NULL, "W_UV_t/o is NULL");
   if (o_dtype != TPLA_F32 && o_dtype != TPLA_BF16) return fail(TPLA_ERR_DTYPE, "o_dtype %d is neither TPLA_F32 nor TPLA_BF16", o_dtype);
   if (!aligned16(W_UV_t) || !aligned16(o)) return fail(TPLA_ERR_ALIGN, "pointers must be 16-byte aligned");
+  TreePlan p;
+  if ((rc = check_tree(shape, shape->g, T, max_pages_per_seq, &p))) return rc;
+  tpla_shape_t rows = *shape;
+  rows.B = shape->B * T;                             // (check_tree: no overflow)
+  if (!combine_mfma_supported(rows) && (rc = check_combine_grid(rows))) return rc;
   rc = tree_common(shape, shape->g, T, q_lat, q_pe, shard_pools, block_table, max_pages_per_seq, seq_lens, draft_lens, tree_mask,
                    workspace, workspace_bytes, o_lat, lse, stream);
   if (rc) return rc;
-  tpla_shape_t rows = *shape;
-  rows.B = shape->B * T;
   return tpla_combine_shards_to(&rows, o_lat, W_UV_t, o, o_dtype, stream);
 }
 

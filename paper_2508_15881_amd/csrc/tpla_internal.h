@@ -409,6 +409,7 @@ int launch_combine_shards(const tpla_shape_t& sh, const float* o_lat, const void
 bool absorb_mfma_supported(const tpla_shape_t& sh);
 int launch_absorb_query_mfma(const tpla_shape_t& sh, const void* q_nope, const void* W_UK_t,
                              const MuFactors& mu, void* q_lat, hipStream_t st);
+int check_combine_grid(const tpla_shape_t& sh);
 bool combine_mfma_supported(const tpla_shape_t& sh);
 int launch_combine_shards_mfma(const tpla_shape_t& sh, const float* o_lat, const void* W_UV_t, void* o, int o_dtype,
                                hipStream_t st);

@@ -17,3 +17,13 @@ def test_rows_whose_token_numbers_pass_31_bits(dtype, g, pt, max_pages):
         assert code(tp.tpla_decode_shards_tree, *args) == -7
         assert code(tp.tpla_decode_shard_tree, *(args[:4] + [A] + args[5:])) == -7
     assert tp.tpla_workspace_bytes_tree(s, 4, most // pt) > 0
+
+
+@pytest.mark.parametrize("dtype,d_v", [(tp.TPLA_F32, 32), (tp.TPLA_BF16, 12), (tp.TPLA_BF16, 128)])
+def test_rows_that_the_combine_has_no_launch_for(dtype, d_v):
+    """Refused ahead of the attention: the workspace is enough, so the only thing wrong is what follows."""
+    s = shape(B=32768, H=1, d_c=64, g=1, d_v=d_v, d_r=64, dtype=dtype)
+    need = tp.tpla_workspace_bytes_tree(s, 64, 4)
+    assert need > 0
+    both = [s, 64, A, A, [A], A, 4, A, A, A, A, need, A, A, dtype, A, A]
+    assert code(tp.tpla_decode_shards_tree_combine, *both) == -7 and "grid" in tp.tpla_last_error()
