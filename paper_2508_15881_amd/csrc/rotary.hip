@@ -6,6 +6,8 @@
 // tokens once, for all their heads.
 #include "tpla_internal.h"
 
+#include <algorithm>
+
 namespace tpla {
 
 constexpr int RO_THREADS = 256;
@@ -130,7 +132,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a) {
   }
 }
 
-int launch_rotary(RotaryArgs a, int dtype, hipStream_t st) {
+static int launch_rotary_tokens(RotaryArgs a, int dtype, hipStream_t st) {
   const bool half = a.layout == TPLA_ROTARY_HALF;
   const int w = !half || a.rot % 16 == 0 ? 8 : a.rot % 4 == 0 ? 2 : 1;
   const int heads = (a.q ? a.H : 0) + (a.k ? 1 : 0);
@@ -147,6 +149,26 @@ int launch_rotary(RotaryArgs a, int dtype, hipStream_t st) {
     fn = w == 8 ? rotary_kernel<bf16_t, 8> : w == 2 ? rotary_kernel<bf16_t, 2> : rotary_kernel<bf16_t, 1>;
   hipLaunchKernelGGL(fn, grid, dim3(RO_THREADS), lds, st, a);
   return check_launch("rotary_kernel");
+}
+
+// A launch holds fewer than 2^32 threads along a dimension, and a workgroup of 256 may have one token: longer calls go in parts.
+int launch_rotary(RotaryArgs a, int dtype, hipStream_t st) {
+  constexpr int64_t MOST = (int64_t)1 << 23;
+  const int64_t T = a.T, esz = dtype == TPLA_F32 ? 4 : 2;
+  const auto ahead = [](const void* p, int64_t bytes) { return p ? static_cast<const char*>(p) + bytes : nullptr; };
+  const auto out_ahead = [](void* p, int64_t bytes) { return p ? static_cast<char*>(p) + bytes : nullptr; };
+  for (int64_t t = 0; t < T; t += MOST) {
+    RotaryArgs part = a;
+    part.T = std::min(MOST, T - t);
+    part.positions = a.positions + t;
+    part.q = ahead(a.q, t * a.q_ts * esz);
+    part.k = ahead(a.k, t * a.k_ts * esz);
+    part.q_out = out_ahead(a.q_out, t * a.qo_ts * esz);
+    part.k_out = out_ahead(a.k_out, t * a.ko_ts * esz);
+    const int rc = launch_rotary_tokens(part, dtype, st);
+    if (rc) return rc;
+  }
+  return TPLA_OK;
 }
 
 }  // namespace tpla
