@@ -54,8 +54,8 @@ static int check_tree(const tpla_shape_t* sh, int n_shards, int32_t T, int32_t m
   int rc = check_shape(sh);
   if (rc || (rc = check_drafts(T)) || (rc = check_table(sh, max_pages))) return rc;
   const int dl = sh->d_c / sh->g;
-  if ((int64_t)sh->B * T * sh->H > (int64_t)2147483647 / 2 || (int64_t)n_shards * sh->B > 65535)
-    return fail(TPLA_ERR_UNSUPPORTED, "B * T * H (or n_shards * B) too large");
+  if ((int64_t)sh->B * T * sh->H > (int64_t)2147483647 / 2 || (int64_t)n_shards * sh->B > 65535 || sh->H > 65535)
+    return fail(TPLA_ERR_UNSUPPORTED, "B * T * H (or n_shards * B, or H) too large");
   if (!tree_mfma_supported(*sh) && (dl > 1024 || dl + sh->d_r > 1984))
     return fail(TPLA_ERR_UNSUPPORTED, "d_c/g=%d above 1024, or d_c/g + d_r=%d above 1984", dl, dl + sh->d_r);
   // token and page numbers stay int in the kernels: a split, a tile, the lanes of a wave or two chunks of page ids past the end included
@@ -63,7 +63,8 @@ static int check_tree(const tpla_shape_t* sh, int n_shards, int32_t T, int32_t m
     return fail(TPLA_ERR_UNSUPPORTED, "max_pages_per_seq * page_tokens above 2^31 - 2^17");
   *p = plan_tree(*sh, n_shards, T, max_pages);
   const double tiles = ((double)max_pages * sh->page_tokens + 31) / 32, items = (double)n_shards * sh->B * p->blocks;
-  if (p->mfma ? items * (tiles + 8) >= 2147483647.0 : items * p->n_splits >= 2147483647.0 || p->n_splits > 65535)
+  // (general: a workgroup of 256 threads per item, fewer than 2^32 in a launch)
+  if (p->mfma ? items * (tiles + 8) >= 2147483647.0 : items >= 16777216.0 || items * p->n_splits >= 2147483647.0 || p->n_splits > 65535)
     return fail(TPLA_ERR_UNSUPPORTED, "n_shards * B * row blocks * max_pages_per_seq too large");
   return TPLA_OK;
 }
@@ -286,6 +287,7 @@ int tpla_commit_drafts(const tpla_shape_t* shape, int32_t T, const int32_t* acce
                        void* const* shard_pools, int32_t* new_lens, void* stream) {
   int rc = check_shape(shape);
   if (rc || (rc = check_drafts(T)) || (rc = check_table(shape, max_pages_per_seq))) return rc;
+  if (shape->B >= 1 << 22) return fail(TPLA_ERR_UNSUPPORTED, "B=%d above 2^22 - 1", shape->B);       // (1024 threads each, fewer than 2^32 in a launch)
   if (!accepted || !n_accepted || !seq_lens || !block_table || !shard_pools || !new_lens)
     return fail(TPLA_ERR_NULL, "a required pointer is NULL");
   CommitArgs a;

@@ -27,3 +27,18 @@ def test_rows_that_the_combine_has_no_launch_for(dtype, d_v):
     assert need > 0
     both = [s, 64, A, A, [A], A, 4, A, A, A, A, need, A, A, dtype, A, A]
     assert code(tp.tpla_decode_shards_tree_combine, *both) == -7 and "grid" in tp.tpla_last_error()
+
+
+def test_grids_of_more_threads_than_a_launch_has():
+    # 2^24 items of 16 rows of the general kernel
+    s = shape(B=65535, H=65, d_c=8, g=1, d_r=8, dtype=tp.TPLA_F32)
+    assert tp.tpla_workspace_bytes_tree(s, 63, 4) > 0
+    assert tp.tpla_workspace_bytes_tree(s, 64, 4) == 0
+    assert code(tp.tpla_decode_shards_tree, s, 64, A, A, [A], A, 4, A, A, A, A, BIG, A, A) == -7
+    # rows of one sequence
+    for dtype in (tp.TPLA_BF16, tp.TPLA_F32):
+        s = shape(B=1, H=65536, d_c=64, g=1, dtype=dtype)
+        assert tp.tpla_workspace_bytes_tree(s, 64, 4) == 0
+        assert code(tp.tpla_decode_shards_tree, s, 64, A, A, [A], A, 4, A, A, A, A, BIG, A, A) == -7
+        assert tp.tpla_workspace_bytes_tree(shape(B=1, H=65535, d_c=64, g=1, dtype=dtype), 64, 4) > 0
+    assert code(tp.tpla_commit_drafts, shape(B=1 << 22), 4, A, A, A, A, 8, [A, A], A) == -7
