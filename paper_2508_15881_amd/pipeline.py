@@ -117,10 +117,12 @@ class DecodeStep:
 
 
 def tree_masks(parents):
-    """Masks and depths of draft trees on the host: parents int [.., T], parents[.., t] < t the draft that t continues,
+    """Masks and depths of draft trees on the host: parents int [.., T], T up to 64, parents[.., t] < t the draft that t continues,
     -1 where it continues the committed tokens.  Returns (masks uint64, depths int32) of the same shape: a draft sees what
     its parent sees, and itself."""
     parents = np.asarray(parents)
+    if parents.shape[-1] > B.TPLA_MAX_DRAFTS:
+        raise ValueError("%d drafts, a mask has %d bits" % (parents.shape[-1], B.TPLA_MAX_DRAFTS))
     masks, depths = np.zeros(parents.shape, dtype=np.uint64), np.zeros(parents.shape, dtype=np.int32)
     for t in range(parents.shape[-1]):
         p = parents[..., t]

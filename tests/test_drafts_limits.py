@@ -1,8 +1,10 @@
 """Host side of the speculative step's entry points: sizes that the kernels' launches and index arithmetic do not hold are refused
 before anything is launched."""
+import numpy as np
 import pytest
 
 import paper_2508_15881_amd as tp
+from paper_2508_15881_amd import pipeline as pl
 from test_drafts_host import A, BIG, code, shape
 
 
@@ -42,3 +44,12 @@ def test_grids_of_more_threads_than_a_launch_has():
         assert code(tp.tpla_decode_shards_tree, s, 64, A, A, [A], A, 4, A, A, A, A, BIG, A, A) == -7
         assert tp.tpla_workspace_bytes_tree(shape(B=1, H=65535, d_c=64, g=1, dtype=dtype), 64, 4) > 0
     assert code(tp.tpla_commit_drafts, shape(B=1 << 22), 4, A, A, A, A, 8, [A, A], A) == -7
+
+
+@pytest.mark.parametrize("parents", [np.arange(-1, 64), np.full((3, 65), -1), np.full(100, -1)])
+def test_more_drafts_than_a_mask_has_bits(parents):
+    """The 65th draft's own bit was lost, and with it what it sees of itself."""
+    with pytest.raises(ValueError):
+        pl.tree_masks(parents)
+    masks, _ = pl.tree_masks(parents[..., :64])
+    assert (masks[..., 63] >> np.uint64(63) == 1).all()
