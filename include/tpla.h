@@ -453,7 +453,7 @@ int tpla_extend_sequences(const tpla_shape_t* shape, const int32_t* seq_lens, co
  * factor > 1 stretches them for contexts that many times as long.  original_positions = 0: every f_j / factor.  Otherwise by
  * how often a pair turns over the original_positions the model was trained on: pairs that turn at least beta_fast times stay,
  * those that turn at most beta_slow times are divided by factor, between them linearly in j, the ends of that ramp rounded
- * outwards to whole pairs.  (The factor on sine and cosine that goes with it is tpla_apply_rotary's amplitude.)
+ * outwards to whole pairs and kept within 0 .. rot_dim - 1.  (The factor on sine and cosine that goes with it is tpla_apply_rotary's amplitude.)
  */
 int tpla_rotary_frequencies(int32_t rot_dim, double base, double factor, int32_t original_positions, double beta_fast,
                             double beta_slow, double* freq);

@@ -172,7 +172,8 @@ int tpla_rotary_frequencies(int32_t rot_dim, double base, double factor, int32_t
   for (int j = 0; j < rot_dim / 2; ++j) {
     const double f = pow(base, -2.0 * j / rot_dim);
     double slow = 1.0;
-    if (original_positions > 0) slow = fmin(fmax((j - low) / fmax(high - low, 1e-3), 0.0), 1.0);
+    // (pair 0 turns most: where it does so at most beta_slow times, the ramp ends ahead of it)
+    if (original_positions > two_pi * beta_slow) slow = fmin(fmax((j - low) / fmax(high - low, 1e-3), 0.0), 1.0);
     freq[j] = f * (1.0 - slow) + f / factor * slow;
   }
   return TPLA_OK;

@@ -53,3 +53,15 @@ def test_more_drafts_than_a_mask_has_bits(parents):
         pl.tree_masks(parents)
     masks, _ = pl.tree_masks(parents[..., :64])
     assert (masks[..., 63] >> np.uint64(63) == 1).all()
+
+
+@pytest.mark.parametrize("original,base,fast,slow", [(4, 10000.0, 32.0, 1.0), (1, 10000.0, 32.0, 1.0), (6, 500.0, 32.0, 1.0), (7, 10000.0, 32.0, 1.0), (100, 1e6, 32.0, 16.0),
+                                                     (64, 10000.0, 32.0, 1.0), (4096, 10000.0, 32.0, 1.0), (8192, 12.0, 4.0, 1.0), (2 ** 31 - 1, 1e4, 32.0, 1.0)])
+def test_frequencies_of_pairs_that_turn_seldom_or_often(original, base, fast, slow):
+    for rot in (2, 8, 64, 128):
+        f = tp.tpla_rotary_frequencies(rot, base=base, factor=40.0, original_positions=original, beta_fast=fast, beta_slow=slow)
+        want = base ** (-2.0 * np.arange(rot // 2) / rot)
+        turns = original * want / (2 * np.pi)
+        seldom, often = turns <= slow * (1 - 1e-12), turns >= fast * (1 + 1e-12)
+        assert np.allclose(f[seldom], want[seldom] / 40, rtol=1e-14, atol=0) and np.allclose(f[often], want[often], rtol=1e-14, atol=0)
+        assert (f <= want * (1 + 1e-14)).all() and (f >= want / 40 * (1 - 1e-14)).all()
