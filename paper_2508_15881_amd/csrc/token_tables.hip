@@ -87,7 +87,6 @@ __global__ void __launch_bounds__(EX_THREADS) extend_sequences_kernel(ExtendArgs
   __shared__ long long first_of[EX_THREADS];         // pages wanted before a sequence of this step, and of those given
   __shared__ int held_of[EX_THREADS];
   const int tid = threadIdx.x, n_thr = blockDim.x;
-  const long long cap = (long long)a.max_pages * a.page_tokens;
   long long tokens = 0, pages = 0;
   for (int b0 = 0; b0 < a.B; b0 += n_thr) {
     const int b = b0 + tid, here = min(n_thr, a.B - b0);
