@@ -187,7 +187,8 @@ struct TreeWalk {
 // the accumulators are written out, with the wait states that the compiler then does not insert: 2 between an ordinary write and a
 // matrix instruction that reads it, 11 (here 18) between a matrix instruction and an ordinary one that reads its result.
 // acc_keep() stands at every step of the loop: nothing of the compiler's may live in these registers across it.  That it puts nothing
-// there in between either is checked on the assembly (tests/test_isa_tree_waits.py).
+// there in between either is checked on the assembly (tests/test_isa_tree_waits.py), and so are the wait states on every path
+// (tests/test_isa_tree_results.py).
 #define TR_ACC_REGS \
   "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", "a10", "a11", "a12", "a13", "a14", "a15", "a16", "a17", "a18", "a19", "a20", "a21", "a22", \
   "a23", "a24", "a25", "a26", "a27", "a28", "a29", "a30", "a31", "a32", "a33", "a34", "a35", "a36", "a37", "a38", "a39", "a40", "a41", "a42", "a43", \
