@@ -259,7 +259,8 @@ int launch_extend_sequences(const ExtendArgs& a, hipStream_t st) {
 // One workgroup per sequence.  Row k goes behind the committed ones from draft accepted[k] >= k, so a row that is written was
 // read before, in this step or an earlier one: a step reads its rows of all slices (CM_BATCH pieces of 16 bytes per thread, on their way
 // together), waits for all of the workgroup, and writes them.  Where every row lies is found once, by a thread each.
-// (kernel alone, 240 sequences with up to 60 rows of four slices: 256 threads of 16 pieces 12.7 us, 512 of 8 8.5, 1024 of 8 7.1)
+// (kernel alone, 240 sequences with up to 60 rows of four slices: 256 threads of 16 pieces 12.7 us, 512 of 8 8.5, 1024 of 8 7.1; with the
+// check of the pages 7.3)
 constexpr int CM_THREADS = 1024, CM_BATCH = 8;
 __global__ void __launch_bounds__(CM_THREADS) commit_drafts_kernel(CommitArgs a) {
   __shared__ long long src_of[TPLA_MAX_DRAFTS], dst_of[TPLA_MAX_DRAFTS];      // byte offsets in a pool; -1: stays where it is
@@ -276,8 +277,8 @@ __global__ void __launch_bounds__(CM_THREADS) commit_drafts_kernel(CommitArgs a)
       const unsigned from = (unsigned)L + j, to = (unsigned)L + tid;
       const int32_t* table = a.block_table + (size_t)b * a.max_pages;
       const bool there = from < cap, moves = j != tid && there;
-      const int to_page = table[to / pt], from_page = there ? table[from / pt] : to_page;
-      placed = (to_page | from_page) >= 0;
+      const int to_page = table[to / pt], from_page = table[min(from, cap - 1) / pt];
+      placed = to_page >= 0 && (from_page >= 0 || !there);
       src_of[tid] = moves ? ((long long)from_page * pt + from % pt) * a.row_bytes : -1;
       dst_of[tid] = ((long long)to_page * pt + to % pt) * a.row_bytes;
     }
