@@ -438,7 +438,7 @@ int tpla_validate_block_table(const tpla_shape_t* shape, const int32_t* block_ta
  * Where pages were missing, the entries of those that b wanted and was not given, pages_held_out[b] .. want_b - 1, become -1 (the entries behind
  * want_b are as they were).  Another call with pages_held_out for pages_held and more free pages places all of the tokens.
  * Negative lengths count as 0, lengths beyond the row as the row's; a negative table entry gives slot
- * -1.  pages_held_out may be pages_held (for more than 1024 tokens a separate array saves a launch); no other
+ * -1.  Slots are int32: (page id + 1) * page_tokens stays below 2^31.  pages_held_out may be pages_held (for more than 1024 tokens a separate array saves a launch); no other
  * overlap.  All pointers are int32 DEVICE arrays; depths [B, row_tokens] or NULL; free_pages may be NULL with n_free =
  * 0.  Only shape->B and page_tokens are read (the shape is checked whole).
  */
