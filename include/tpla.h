@@ -529,6 +529,85 @@ int tpla_commit_drafts(const tpla_shape_t* shape, int32_t T, const int32_t* acce
                        const int32_t* seq_lens, const int32_t* block_table, int32_t max_pages_per_seq,
                        void* const* shard_pools, int32_t* new_lens, void* stream);
 
+/*
+ * ---- Grouped heads: layers with a key and a value per group of query heads, beside the latent ones ----
+ * The cache of such a layer is a pair of paged pools, k_pool [P, H_kv, page_tokens, d_k] and v_pool [P, H_kv, page_tokens, d_v]: the
+ * tokens of a page that belong to one head lie together.  Block tables, slots and positions are those of the latent caches: one call of
+ * tpla_extend_sequences serves both kinds of layers.  Query head h reads the keys and values of head h / (H / H_kv).
+ */
+typedef struct tpla_heads {
+  int32_t B;           /* sequences                                                  */
+  int32_t H;           /* query heads, a multiple of H_kv                            */
+  int32_t H_kv;        /* heads of keys and values                                   */
+  int32_t d_k;         /* width of a query and a key, a multiple of 8, at most 256   */
+  int32_t d_v;         /* width of a value, likewise                                 */
+  int32_t page_tokens; /* tokens per cache page                                      */
+  int32_t dtype;       /* TPLA_F32 or TPLA_BF16                                      */
+  float sm_scale;      /* softmax scale, 1/sqrt(d_k) as a rule                       */
+} tpla_heads_t;
+
+/*
+ * Norm and position of every head of queries and keys in one pass.  A row x of d_k columns (token t, one head) becomes
+ *     y = x / sqrt(mean(x^2) + norm_eps) * weight,   then the pairs of its first rot_dim columns turned as by tpla_apply_rotary
+ * with layout, freq, amplitude and positions as there; columns rot_dim .. d_k - 1 stay y.  norm_eps < 0: no norm, y = x, and the weights
+ * are NULL.  rot_dim = 0: no rotation, and freq and positions may be NULL.  q [T, H, d_k] and k [T, H_kv, d_k], q_out and k_out likewise,
+ * in shape->dtype with strides in elements (innermost dense): they may be columns of a wider projection; pointers and strides in whole
+ * 16 bytes (TPLA_ERR_ALIGN; the stride of a single token or head means nothing).  q_weight and k_weight [d_k] in shape->dtype or NULL for
+ * all ones.  An output may be its input, with the same strides; no other overlap.  q with q_out, or k with k_out, may be NULL; T = 0 does
+ * nothing.  Mean, norm, angles' sines and products in float (angles in double), one rounding on the way out.
+ */
+int tpla_norm_rotary_heads(const tpla_heads_t* shape, int32_t layout, int32_t rot_dim, const double* freq, float amplitude,
+                           const void* q_weight, const void* k_weight, float norm_eps, const int32_t* positions, int64_t T,
+                           const void* q, int64_t q_token_stride, int64_t q_head_stride, void* q_out, int64_t q_out_token_stride,
+                           int64_t q_out_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
+                           int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/*
+ * New tokens into the cache, norm and position on the way: q (with q_out; both may be NULL) and k as in tpla_norm_rotary_heads, but the
+ * keys of token t go to slot slots[t] = page * page_tokens + offset of k_pool, and v [T, H_kv, d_v] (strides as k's) unchanged to the same
+ * slot of v_pool.  A negative slot skips the token's key and value (its queries are written).  slots int32 [T], no slot twice.
+ */
+int tpla_append_heads(const tpla_heads_t* shape, int32_t layout, int32_t rot_dim, const double* freq, float amplitude,
+                      const void* q_weight, const void* k_weight, float norm_eps, const int32_t* positions, int64_t T,
+                      const void* q, int64_t q_token_stride, int64_t q_head_stride, void* q_out, int64_t q_out_token_stride,
+                      int64_t q_out_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                      int64_t v_token_stride, int64_t v_head_stride, const int32_t* slots, void* k_pool, void* v_pool, void* stream);
+
+/*
+ * One new token per sequence over the paged keys and values.  For sequence b, query head h, over tokens t < seq_lens[b]:
+ *     s_t = sm_scale * (q[b,h] . k_t),   o[b,h,:] = sum_t softmax(s)_t v_t,   lse[b,h] = log sum_t exp(s_t)
+ * with the key and value of token t in page block_table[b, t / page_tokens], slot t % page_tokens.  seq_lens counts the new token, as in
+ * tpla_decode_shard.  Tokens whose page is a negative entry are not seen; a row that sees nothing gets o = 0, lse = -inf; slots at or
+ * beyond seq_lens[b] are never read; lengths out of range are clipped to the block-table row.  A row that sees scores of -inf alone, or
+ * one that is not finite otherwise, gets o that is not a number.  q [B, H, d_k] in shape->dtype, dense; o [B, H, d_v] float (o_dtype =
+ * TPLA_F32) or bfloat16 (TPLA_BF16); lse float [B, H] or NULL.  workspace: tpla_workspace_bytes_heads() bytes; nothing in it has to be
+ * cleared.  The token axis is split over workgroups and joined in a fixed order: bit-reproducible for fixed arguments.  bf16 with d_k =
+ * d_v = 64 or 128 and pages of a multiple of 16 tokens runs on the bf16 matrix instructions, with the softmax weights rounded to bf16 for
+ * the product with the values; everything else in float.  max_pages_per_seq * page_tokens is at most 2^31 - 2^17, B * H below 2^28
+ * (TPLA_ERR_UNSUPPORTED).
+ */
+size_t tpla_workspace_bytes_heads(const tpla_heads_t* shape, int32_t max_pages_per_seq);
+int tpla_decode_heads(const tpla_heads_t* shape, const void* q, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                      int32_t max_pages_per_seq, const int32_t* seq_lens, void* workspace, size_t workspace_bytes, void* o,
+                      int32_t o_dtype, float* lse, void* stream);
+
+/*
+ * Prompts, or parts of prompts behind cached tokens: causal attention of the new tokens of every sequence over the cache, which holds them
+ * already (tpla_append_heads).  seq_lens[b] counts the tokens before the new ones, as in tpla_extend_sequences (NULL: none anywhere); new
+ * token i of b is row cu_seqlens[b] + i of q and o and token seq_lens[b] + i of its sequence, and sees the tokens up to itself:
+ *     s_t = sm_scale * (q[row,h] . k_t) for t <= seq_lens[b] + i,   o and lse as in tpla_decode_heads.
+ * cu_seqlens int32 [B + 1], non-decreasing, on the device (row ranges are clipped to [0, T)); max_new: an upper bound of the new tokens of
+ * a sequence (rows beyond it are not computed).  Rows behind cu_seqlens[B] are left as they were.  What a token's key or value holds
+ * (infinities and NaN too) does not reach rows that do not see it.  Tokens beyond the block-table row do not exist: they are not seen.
+ * q [T, H, d_k] in shape->dtype, dense; o [T, H, d_v] in o_dtype; lse float [T, H] or NULL.  T = 0 does nothing.  workspace:
+ * tpla_workspace_bytes_prefill_heads() bytes (the work of few rows is split over their tokens); it may be NULL where that is 0.  Kernels,
+ * pages of negative entries, lengths, limits (T in the place of B) and reproducibility as in tpla_decode_heads.
+ */
+size_t tpla_workspace_bytes_prefill_heads(const tpla_heads_t* shape, int64_t T, int32_t max_new, int32_t max_pages_per_seq);
+int tpla_prefill_heads(const tpla_heads_t* shape, const void* q, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                       int32_t max_pages_per_seq, const int32_t* seq_lens, const int32_t* cu_seqlens, int64_t T, int32_t max_new,
+                       void* workspace, size_t workspace_bytes, void* o, int32_t o_dtype, float* lse, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,4 +18,6 @@ from .binding import (  # noqa: F401
     TPLA_MAX_DRAFTS, TPLA_ROTARY_HALF, TPLA_ROTARY_INTERLEAVED,
     tpla_extend_sequences, tpla_rotary_frequencies, tpla_apply_rotary, tpla_workspace_bytes_tree, tpla_decode_shard_tree,
     tpla_decode_shards_tree, tpla_decode_shards_tree_combine, tpla_commit_drafts,
+    TplaHeads, tpla_norm_rotary_heads, tpla_append_heads, tpla_workspace_bytes_heads, tpla_decode_heads,
+    tpla_workspace_bytes_prefill_heads, tpla_prefill_heads,
 )

@@ -31,6 +31,8 @@ EXPORTS = (
     "tpla_attention_block_workspace_bytes", "tpla_decode_shards_project",
     "tpla_extend_sequences", "tpla_rotary_frequencies", "tpla_apply_rotary", "tpla_workspace_bytes_tree",
     "tpla_decode_shard_tree", "tpla_decode_shards_tree", "tpla_decode_shards_tree_combine", "tpla_commit_drafts",
+    "tpla_norm_rotary_heads", "tpla_append_heads", "tpla_workspace_bytes_heads", "tpla_decode_heads",
+    "tpla_workspace_bytes_prefill_heads", "tpla_prefill_heads",
 )
 
 
@@ -51,6 +53,14 @@ class TplaShape(ctypes.Structure):
     @property
     def dl(self):
         return self.d_c // self.g
+
+
+class TplaHeads(ctypes.Structure):
+    """Mirror of tpla_heads_t."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float),
+    ]
 
 
 _lib = None
@@ -152,6 +162,20 @@ def load_library():
     lib.tpla_commit_drafts.argtypes = [shp, i32, vp, vp, vp, vp, i32, ctypes.POINTER(vp), vp, vp]
     lib.tpla_pca_basis.restype = ctypes.c_int
     lib.tpla_pca_basis.argtypes = [i32, i32, i64, vp, vp, vp, vp, vp]
+    hds, rows = ctypes.POINTER(TplaHeads), [vp, i64, i64]
+    prepared = [hds, i32, i32, vp, ctypes.c_float, vp, vp, ctypes.c_float, vp, i64]
+    lib.tpla_norm_rotary_heads.restype = ctypes.c_int
+    lib.tpla_norm_rotary_heads.argtypes = prepared + 4 * rows + [vp]
+    lib.tpla_append_heads.restype = ctypes.c_int
+    lib.tpla_append_heads.argtypes = prepared + 4 * rows + [vp, vp, vp, vp]
+    lib.tpla_workspace_bytes_heads.restype = ctypes.c_size_t
+    lib.tpla_workspace_bytes_heads.argtypes = [hds, i32]
+    lib.tpla_decode_heads.restype = ctypes.c_int
+    lib.tpla_decode_heads.argtypes = [hds, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp, i32, vp, vp]
+    lib.tpla_workspace_bytes_prefill_heads.restype = ctypes.c_size_t
+    lib.tpla_workspace_bytes_prefill_heads.argtypes = [hds, i64, i32, i32]
+    lib.tpla_prefill_heads.restype = ctypes.c_int
+    lib.tpla_prefill_heads.argtypes = [hds, vp, vp, vp, vp, i32, vp, vp, i64, i32, vp, ctypes.c_size_t, vp, i32, vp, vp]
     _lib = lib
     return lib
 
@@ -434,6 +458,60 @@ def tpla_commit_drafts(shape, T, accepted, n_accepted, seq_lens, block_table, ma
     _check(load_library().tpla_commit_drafts(
         ctypes.byref(shape), T, _ptr(accepted), _ptr(n_accepted), _ptr(seq_lens), _ptr(block_table), max_pages_per_seq,
         _pool_array(shard_pools), _ptr(new_lens), _stream(stream)))
+
+
+def _rows(x, shape):
+    """_view of a tensor that may be missing: address and strides of tokens and heads."""
+    if x is None:
+        return None, (0, 0)
+    return _view(x, shape)
+
+
+def tpla_norm_rotary_heads(shape, layout, rot_dim, freq, amplitude, q_weight, k_weight, norm_eps, positions, T, q, q_out, k, k_out,
+                           stream=None):
+    """q, q_out [T, H, d_k] and k, k_out [T, H_kv, d_k] may be views: their strides, which the C call takes after each pointer, are
+    read off the tensors.  q (with q_out) or k (with k_out) may be None."""
+    args = []
+    for x, heads in ((q, shape.H), (q_out, shape.H), (k, shape.H_kv), (k_out, shape.H_kv)):
+        p, s = _rows(x, (T, heads, shape.d_k))
+        args += [p, s[0], s[1]]
+    _check(load_library().tpla_norm_rotary_heads(
+        ctypes.byref(shape), layout, rot_dim, _ptr(freq), amplitude, _ptr(q_weight), _ptr(k_weight), norm_eps, _ptr(positions), T, *args,
+        _stream(stream)))
+
+
+def tpla_append_heads(shape, layout, rot_dim, freq, amplitude, q_weight, k_weight, norm_eps, positions, T, q, q_out, k, v, slots, k_pool,
+                      v_pool, stream=None):
+    """q, q_out [T, H, d_k] (or both None), k [T, H_kv, d_k] and v [T, H_kv, d_v] may be views, as in tpla_norm_rotary_heads."""
+    args = []
+    for x, heads, d in ((q, shape.H, shape.d_k), (q_out, shape.H, shape.d_k), (k, shape.H_kv, shape.d_k), (v, shape.H_kv, shape.d_v)):
+        p, s = _rows(x, (T, heads, d))
+        args += [p, s[0], s[1]]
+    _check(load_library().tpla_append_heads(
+        ctypes.byref(shape), layout, rot_dim, _ptr(freq), amplitude, _ptr(q_weight), _ptr(k_weight), norm_eps, _ptr(positions), T, *args,
+        _ptr(slots), _ptr(k_pool), _ptr(v_pool), _stream(stream)))
+
+
+def tpla_workspace_bytes_heads(shape, max_pages_per_seq):
+    return int(load_library().tpla_workspace_bytes_heads(ctypes.byref(shape), max_pages_per_seq))
+
+
+def tpla_decode_heads(shape, q, k_pool, v_pool, block_table, max_pages_per_seq, seq_lens, workspace, workspace_bytes, o, o_dtype, lse,
+                      stream=None):
+    _check(load_library().tpla_decode_heads(
+        ctypes.byref(shape), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_table), max_pages_per_seq, _ptr(seq_lens), _ptr(workspace),
+        workspace_bytes, _ptr(o), o_dtype, _ptr(lse), _stream(stream)))
+
+
+def tpla_workspace_bytes_prefill_heads(shape, T, max_new, max_pages_per_seq):
+    return int(load_library().tpla_workspace_bytes_prefill_heads(ctypes.byref(shape), T, max_new, max_pages_per_seq))
+
+
+def tpla_prefill_heads(shape, q, k_pool, v_pool, block_table, max_pages_per_seq, seq_lens, cu_seqlens, T, max_new, workspace,
+                       workspace_bytes, o, o_dtype, lse, stream=None):
+    _check(load_library().tpla_prefill_heads(
+        ctypes.byref(shape), _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_table), max_pages_per_seq, _ptr(seq_lens), _ptr(cu_seqlens),
+        T, max_new, _ptr(workspace), workspace_bytes, _ptr(o), o_dtype, _ptr(lse), _stream(stream)))
 
 
 def tpla_pca_basis(d_c, g, n_rows, sum_host, gram_host):
