@@ -89,6 +89,7 @@ static HeadRowsArgs rows_args(const tpla_heads_t* sh, int32_t layout, int32_t ro
 
 // ---- attention ----
 static HeadsPlan plan_heads(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages) {
+  if (heads_mfma_supported(sh) && heads_ranges_fit(sh, max_new)) return heads_ranges_plan(sh, max_new, max_pages);
   return general_heads_plan(sh, T, max_new, max_pages);
 }
 
@@ -101,6 +102,8 @@ static int check_attention(const tpla_heads_t* sh, int64_t rows, int32_t* max_ne
   if (rows * sh->H >= (int64_t)1 << 28) return fail(TPLA_ERR_UNSUPPORTED, "rows * H = %lld above 2^28 - 1", (long long)rows * sh->H);
   if (sh->B >= 1 << 22) return fail(TPLA_ERR_UNSUPPORTED, "B=%d above 2^22 - 1", sh->B);
   *p = plan_heads(*sh, rows, *max_new, max_pages);
+  if (p->kernel == HEADS_RANGES && (double)p->items * (((double)max_pages * sh->page_tokens + 31) / 32) >= 2147483647.0)
+    return fail(TPLA_ERR_UNSUPPORTED, "sequences * heads of keys * max_pages_per_seq too large");
   if (p->items >= (int64_t)1 << 23) return fail(TPLA_ERR_UNSUPPORTED, "%lld work items are more than a launch has", (long long)p->items);
   return TPLA_OK;
 }
@@ -124,7 +127,9 @@ static int attention(const tpla_heads_t* sh, const HeadsPlan& p, const void* q, 
   a.o = o;
   a.lse = lse;
   a.part_acc = static_cast<float*>(workspace);
-  a.part_ml = a.part_acc ? a.part_acc + (size_t)p.items * p.n_splits * p.rows * sh->d_v : nullptr;
+  a.part_ml = a.part_acc ? a.part_acc + (size_t)p.slots * p.rows * sh->d_v : nullptr;
+  a.plan = a.part_acc ? reinterpret_cast<int32_t*>(a.part_ml + (size_t)p.slots * p.rows * 2) : nullptr;
+  a.n_wg = p.n_wg;
   a.B = sh->B;
   a.H = sh->H;
   a.H_kv = sh->H_kv;
@@ -139,6 +144,7 @@ static int attention(const tpla_heads_t* sh, const HeadsPlan& p, const void* q, 
   a.n_splits = p.n_splits;
   a.tiles = p.tiles;
   a.scale_log2 = sh->sm_scale * 1.4426950408889634f;
+  if (p.kernel == HEADS_RANGES) return launch_heads_ranges(a, p, (hipStream_t)stream);
   return launch_general_heads(a, p, sh->dtype, (hipStream_t)stream);
 }
 

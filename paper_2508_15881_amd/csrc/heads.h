@@ -28,10 +28,16 @@ struct HeadsArgs {
   int B, H, H_kv, G, d_k, d_v, page_tokens, max_pages, o_dtype;
   int T, max_new, n_splits;
   int tiles;                             // of rows: decode per (sequence, head of keys), prefill an upper bound for all sequences, per head of keys
+  int32_t* plan;                         // ranges: where the merge finds an item's parts, three ints per item
+  int n_wg;                              // ranges: workgroups
   float scale_log2;
 };
 
+enum HeadsKernel { HEADS_GENERAL, HEADS_RANGES };
 struct HeadsPlan {
+  HeadsKernel kernel;
+  int n_wg;                    // HEADS_RANGES: workgroups, each with an equal range of all tiles
+  int64_t slots;               // partial results, of `rows` rows each
   int rows;                    // rows of an item
   int tiles;                   // HeadsArgs::tiles
   int64_t items;               // work items (upper bound), each of n_splits parts of its tokens
@@ -41,6 +47,11 @@ struct HeadsPlan {
 // max_new = 0: decode
 HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages);
 int launch_general_heads(const HeadsArgs& a, const HeadsPlan& p, int dtype, hipStream_t st);
+// bf16, d_k = d_v of 64 or 128, pages of a multiple of 16 tokens, at most 64 rows per head of keys: see heads_ranges.hip
+bool heads_mfma_supported(const tpla_heads_t& sh);
+bool heads_ranges_fit(const tpla_heads_t& sh, int32_t max_new);
+HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages);
+int launch_heads_ranges(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st);
 
 // A work item: `rows` rows of one head of keys of one sequence.  Row r of a (sequence, head) is its new token r / G, query head r % G of the group.
 struct HeadsItem {

@@ -255,6 +255,8 @@ static bool general_joins(const tpla_heads_t& sh, int32_t max_new) {
 
 HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages) {
   HeadsPlan p;
+  p.kernel = HEADS_GENERAL;
+  p.n_wg = 0;
   const int G = sh.H / sh.H_kv;
   p.rows = general_joins(sh, max_new) ? 16 : 64;
   const int64_t tiles = max_new > 0 ? T * G / p.rows + sh.B : (G + p.rows - 1) / p.rows;
@@ -263,7 +265,8 @@ HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
   const int64_t tokens = (int64_t)max_pages * sh.page_tokens, want = (4 * (int64_t)device_cu_count() + p.items - 1) / p.items;
   const int64_t most = (tokens + 255) / 256;
   p.n_splits = (int)(want < 1 ? 1 : want < most ? want : most);
-  p.workspace = p.n_splits > 1 ? (size_t)p.items * p.n_splits * p.rows * (sh.d_v + 2) * sizeof(float) : 0;
+  p.slots = p.n_splits > 1 ? p.items * p.n_splits : 0;
+  p.workspace = (size_t)p.slots * p.rows * (sh.d_v + 2) * sizeof(float);
   return p;
 }
 
