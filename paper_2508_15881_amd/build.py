@@ -25,7 +25,7 @@ if LIB_NAME != "libtpla.so":
 SOURCES = ["api.hip", "decode_mfma.hip", "decode_generic.hip", "transform.hip", "transform_mfma.hip", "transform_weights.hip",
            "absorb_combine.hip", "absorb_combine_mfma.hip", "pca.hip", "prefill_mfma.hip",
            "api_drafts.hip", "token_tables.hip", "rotary.hip", "tree.hip", "tree_mfma.hip",
-           "api_heads.hip", "heads_rows.hip", "heads_general.hip", "heads_ranges.hip"]
+           "api_heads.hip", "heads_rows.hip", "heads_general.hip", "heads_ranges.hip", "heads_prompts.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

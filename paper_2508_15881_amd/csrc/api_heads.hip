@@ -89,7 +89,7 @@ static HeadRowsArgs rows_args(const tpla_heads_t* sh, int32_t layout, int32_t ro
 
 // ---- attention ----
 static HeadsPlan plan_heads(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages) {
-  if (heads_mfma_supported(sh) && heads_ranges_fit(sh, max_new)) return heads_ranges_plan(sh, max_new, max_pages);
+  if (heads_mfma_supported(sh)) return heads_ranges_fit(sh, max_new) ? heads_ranges_plan(sh, max_new, max_pages) : heads_prompts_plan(sh, T, max_new, max_pages);
   return general_heads_plan(sh, T, max_new, max_pages);
 }
 
@@ -144,6 +144,7 @@ static int attention(const tpla_heads_t* sh, const HeadsPlan& p, const void* q, 
   a.n_splits = p.n_splits;
   a.tiles = p.tiles;
   a.scale_log2 = sh->sm_scale * 1.4426950408889634f;
+  if (p.kernel == HEADS_PROMPTS) return launch_heads_prompts(a, p, (hipStream_t)stream);
   if (p.kernel == HEADS_RANGES) return launch_heads_ranges(a, p, (hipStream_t)stream);
   return launch_general_heads(a, p, sh->dtype, (hipStream_t)stream);
 }

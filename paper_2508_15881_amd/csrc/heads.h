@@ -33,7 +33,7 @@ struct HeadsArgs {
   float scale_log2;
 };
 
-enum HeadsKernel { HEADS_GENERAL, HEADS_RANGES };
+enum HeadsKernel { HEADS_GENERAL, HEADS_RANGES, HEADS_PROMPTS };
 struct HeadsPlan {
   HeadsKernel kernel;
   int n_wg;                    // HEADS_RANGES: workgroups, each with an equal range of all tiles
@@ -52,6 +52,9 @@ bool heads_mfma_supported(const tpla_heads_t& sh);
 bool heads_ranges_fit(const tpla_heads_t& sh, int32_t max_new);
 HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages);
 int launch_heads_ranges(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st);
+// the same types, any number of rows: see heads_prompts.hip
+HeadsPlan heads_prompts_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages);
+int launch_heads_prompts(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st);
 
 // A work item: `rows` rows of one head of keys of one sequence.  Row r of a (sequence, head) is its new token r / G, query head r % G of the group.
 struct HeadsItem {

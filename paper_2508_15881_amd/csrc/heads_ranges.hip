@@ -7,8 +7,7 @@
 // the tiles of an item in turn, each with a place of its own in LDS that direct loads fill: no barrier within an item, the next keys are
 // requested once the scores have read the last ones, the next values after the output product, and eight waves on a compute unit keep some
 // 100 KB on their way.  An item that lies in one range is written at once, the parts of the others are merged by a second kernel.
-#include "lds_tile.h"
-#include "heads.h"
+#include "heads_tile.h"
 
 #include <algorithm>
 
@@ -20,15 +19,6 @@ constexpr int HN_LOADS = HN_TILE / 1024; // direct-to-LDS loads each
 constexpr int HN_IDS = 1024;             // page ids held at once
 constexpr int HN_MIN_UNITS = 4;          // tiles of a range at least: one per wave
 constexpr int HN_LDS = HN_NW * 2 * HN_TILE + HN_IDS * 4;
-
-// Place of the 16-byte pieces of row `tok` within the row: piece c lies at c ^ heads_swz(tok).  Rows of 256 bytes begin at the same bank, so
-// that the four rows of a transposing read must differ by two pieces at least, and the eight of a row-wise one by one; rows of 128 bytes
-// alternate between the halves of the banks.
-template <int RC>
-__device__ __forceinline__ int heads_swz(int tok) {
-  if constexpr (RC == 16) return ((tok & 3) << 1) | ((tok >> 2) & 1) | (tok & 8);
-  return tok & 7;
-}
 
 __host__ __device__ __forceinline__ int range_start(int n_wg, int units, int w) { return (int)((long long)w * units / n_wg); }
 // The last workgroup whose range begins at or before unit u.
@@ -118,17 +108,6 @@ struct HeadsWalk {
     a.plan[3 * item + 2] = slot & 1;
   }
 };
-
-// Read and waited for here: left to the compiler, a read of LDS waits for the direct loads on their way.
-__device__ __forceinline__ int lds_read_page(const int* at) {
-  int id;
-  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(id) : "v"(lds_at(reinterpret_cast<const char*>(at))) : "memory");
-  return id;
-}
-template <int N>
-__device__ __forceinline__ void loads_wait() {
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
 
 // D: width.  RB: blocks of 16 rows.
 template <int D, int RB>
@@ -325,7 +304,7 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
             } else if (tok0 + at >= least) {
               const u32x4 v = *piece;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) odd = odd || (v[e] & 0x7F80u) == 0x7F80u || (v[e] & 0x7F800000u) == 0x7F800000u;
+              for (int e = 0; e < 4; ++e) odd = odd || not_finite_pair(v[e]);
             }
           }
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -356,12 +335,8 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
           // A weight of zero does not silence what is not finite: one token at a time, kept by the rows that see it.
 #pragma unroll 1
           for (int tok = 0; tok < TOK; ++tok) {
-            // token 32 h + 16 g + 4 c + i is element 4 g + i of the lanes with q4 = c
-            const int h = tok >> 5, e = 4 * ((tok >> 4) & 1) + (tok & 3);
-            const bool holds = q4 == ((tok >> 2) & 3);
-            u32x4 keep;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) keep[x] = holds && x == (e >> 1) ? ((e & 1) ? 0xFFFF0000u : 0xFFFFu) : 0u;
+            const int h = tok >> 5;
+            const u32x4 keep = keep_token(tok, q4);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
               u32x2 lo, hi;
