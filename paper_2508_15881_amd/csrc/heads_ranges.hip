@@ -18,6 +18,9 @@ constexpr int HN_TILE = 8192;            // bytes of keys, and of values, of a t
 constexpr int HN_LOADS = HN_TILE / 1024; // direct-to-LDS loads each
 constexpr int HN_IDS = 1024;             // page ids held at once
 constexpr int HN_MIN_UNITS = 4;          // tiles of a range at least: one per wave
+// Units of an item ahead of its tiles, for what it costs besides them (page ids, queries, the way of the first tiles, the join): many short items
+// are spread over the workgroups, and ranges with several of them end with the others.
+constexpr int HN_START = 4;
 constexpr int HN_LDS = HN_NW * 2 * HN_TILE + HN_IDS * 4;
 
 __host__ __device__ __forceinline__ int range_start(int n_wg, int units, int w) { return (int)((long long)w * units / n_wg); }
@@ -52,7 +55,7 @@ struct HeadsWalk {
     u.tiles = max((u.it.keys + TOK - 1) / TOK, 1);
     return u;
   }
-  __device__ __forceinline__ int count(const HeadsArgs& a, const Units& u) const { return u.blocks * u.tiles * a.H_kv; }
+  __device__ __forceinline__ int count(const HeadsArgs& a, const Units& u) const { return u.blocks * (u.tiles + HN_START) * a.H_kv; }
   __device__ __forceinline__ bool begin(const HeadsArgs& a) {
     const int lane = threadIdx.x & 63;
     front = units_of(a, lane);
@@ -66,39 +69,44 @@ struct HeadsWalk {
     end = range_start(n_wg, units, w + 1);
     return true;
   }
-  // The next item of the range; false: there is none.  a.tiles: items per (sequence, head of keys) that the plan has room for.
+  // The next item with tiles in the range; false: there is none.  a.tiles: items per (sequence, head of keys) that the plan has room for.
   __device__ __forceinline__ bool find(const HeadsArgs& a) {
-    if (pos >= end) return false;
     const int lane = threadIdx.x & 63;
-    int b0 = 0, incl = front_incl;
-    Units u = front;
-    unsigned long long past = __ballot(incl > pos);
-    while (past == 0) {                                // ends: pos lies below the sum over all sequences
-      b0 += 64;
-      const int base = __builtin_amdgcn_readlane(incl, 63);
-      u = units_of(a, b0 + lane);
-      incl = wave_prefix(count(a, u)) + base;
-      past = __ballot(incl > pos);
+    while (pos < end) {
+      int b0 = 0, incl = front_incl;
+      Units u = front;
+      unsigned long long past = __ballot(incl > pos);
+      while (past == 0) {                              // ends: pos lies below the sum over all sequences
+        b0 += 64;
+        const int base = __builtin_amdgcn_readlane(incl, 63);
+        u = units_of(a, b0 + lane);
+        incl = wave_prefix(count(a, u)) + base;
+        past = __ballot(incl > pos);
+      }
+      const int src = __builtin_ctzll(past), rem = pos - __builtin_amdgcn_readlane(incl - count(a, u), src);
+      tiles = __builtin_amdgcn_readlane(u.tiles, src);
+      const int span = tiles + HN_START, which = rem / span, at = rem - which * span, stop = min(span, at + (end - pos));
+      const bool first = pos == range0;
+      last = pos - at + span - 1;
+      pos += stop - at;
+      t0 = max(at - HN_START, 0);
+      t1 = stop - HN_START;
+      if (t1 <= t0) continue;                          // the range ends before the item's first tile
+      it.b = b0 + src;
+      it.first = __builtin_amdgcn_readlane(u.it.first, src);
+      it.rows = __builtin_amdgcn_readlane(u.it.rows, src);
+      it.L = __builtin_amdgcn_readlane(u.it.L, src);
+      it.keys = __builtin_amdgcn_readlane(u.it.keys, src);
+      const int blocks = __builtin_amdgcn_readlane(u.blocks, src);
+      it.kvh = which / blocks;
+      const int block = which - it.kvh * blocks;
+      it.row0 = block * ROWS;
+      item = (it.b * a.H_kv + it.kvh) * a.tiles + block;
+      whole = t0 == 0 && t1 == tiles;
+      slot = 2 * w + (first ? 0 : 1);
+      return true;
     }
-    const int src = __builtin_ctzll(past), rem = pos - __builtin_amdgcn_readlane(incl - count(a, u), src);
-    it.b = b0 + src;
-    it.first = __builtin_amdgcn_readlane(u.it.first, src);
-    it.rows = __builtin_amdgcn_readlane(u.it.rows, src);
-    it.L = __builtin_amdgcn_readlane(u.it.L, src);
-    it.keys = __builtin_amdgcn_readlane(u.it.keys, src);
-    tiles = __builtin_amdgcn_readlane(u.tiles, src);
-    const int blocks = __builtin_amdgcn_readlane(u.blocks, src), which = rem / tiles;
-    it.kvh = which / blocks;
-    const int block = which - it.kvh * blocks;
-    it.row0 = block * ROWS;
-    item = (it.b * a.H_kv + it.kvh) * a.tiles + block;
-    t0 = rem - which * tiles;
-    t1 = min(tiles, t0 + (end - pos));
-    whole = t0 == 0 && t1 == tiles;
-    slot = 2 * w + (pos == range0 ? 0 : 1);
-    last = pos - t0 + tiles - 1;
-    pos += t1 - t0;
-    return true;
+    return false;
   }
   // Where the merge finds the item's parts: whoever has its first tile says so.
   __device__ __forceinline__ void note(const HeadsArgs& a) const {
@@ -480,7 +488,7 @@ HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max
   p.items = (int64_t)sh.B * sh.H_kv * p.tiles;
   p.n_splits = 1;
   const int tok = HN_TILE / (2 * sh.d_k);
-  const double tiles = (double)p.items * (((double)max_pages * sh.page_tokens + tok - 1) / tok);
+  const double tiles = (double)p.items * (((double)max_pages * sh.page_tokens + tok - 1) / tok + HN_START);
   const int most = device_cu_count() * (rb == 1 ? 2 : 1);
   p.n_wg = (int)std::max(1.0, std::min((double)most, tiles / HN_MIN_UNITS));
   p.slots = 2 * (int64_t)p.n_wg;

@@ -64,9 +64,15 @@ struct Piece8<bf16_t> {
   }
 };
 
+// What a row's columns are multiplied with: y' = y cos + z sin, z the partner's column (the sign of sin is the place in the pair).
+struct Turn8 {
+  float c[8], s[8];
+};
+
 // grid: (tokens, blocks of rows).  The rows of a token are its H heads of queries, its H_kv of keys and, with slots, its H_kv of values.  LDS: (cos,
-// sin) of the token's rot / 2 pairs, amplitude included.  LPR: lanes per row.
-template <typename T, int LPR>
+// sin) of the token's rot / 2 pairs, amplitude included.  LPR: lanes per row.  WHOLE: columns in eights are turned alike: rot / 2 a multiple of 8, or
+// pairs side by side with rot one.
+template <typename T, int LPR, bool WHOLE>
 __global__ void __launch_bounds__(HR_THREADS) head_rows_kernel(HeadRowsArgs a, int block_rows) {
   extern __shared__ float2 turns[];
   constexpr int AT_ONCE = HR_THREADS / LPR;
@@ -75,9 +81,9 @@ __global__ void __launch_bounds__(HR_THREADS) head_rows_kernel(HeadRowsArgs a, i
   const int nq = a.q ? a.H : 0, nk = a.k ? a.H_kv : 0, nv = a.slots ? a.H_kv : 0;
   const int r0 = blockIdx.y * block_rows, r1 = min(r0 + block_rows, nq + nk + nv);
   const int slot = a.slots ? a.slots[t] : 0;
-  const int page = a.slots && slot >= 0 ? slot / a.page_tokens : 0, at = slot - page * a.page_tokens;
+  const bool half = a.layout == TPLA_ROTARY_HALF;
 
-  Piece8<T> x[HR_BATCH];
+  Piece8<T> x[HR_BATCH], wq, wk;
   auto request = [&](int first) {
 #pragma unroll
     for (int k = 0; k < HR_BATCH; ++k) {
@@ -93,6 +99,15 @@ __global__ void __launch_bounds__(HR_THREADS) head_rows_kernel(HeadRowsArgs a, i
   };
   int first = r0 + tid / LPR;
   request(first);
+  {
+    float one[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) one[e] = 1.f;
+    wq.set(one);
+    wk.set(one);
+  }
+  if (a.q_weight && c < a.d_k) wq.load(static_cast<const T*>(a.q_weight) + c);
+  if (a.k_weight && c < a.d_k) wk.load(static_cast<const T*>(a.k_weight) + c);
   for (int p = tid; p < pairs; p += HR_THREADS) {
     const double turn = (double)a.positions[t] * (a.freq[p] * 0.15915494309189533577);
     float s, co;
@@ -100,13 +115,27 @@ __global__ void __launch_bounds__(HR_THREADS) head_rows_kernel(HeadRowsArgs a, i
     turns[p] = make_float2(co * a.amplitude, s * a.amplitude);
   }
   __syncthreads();
-  const bool half = a.layout == TPLA_ROTARY_HALF;
+  const int page = a.slots && slot >= 0 ? slot / a.page_tokens : 0, at = slot - page * a.page_tokens;
+  Turn8 turn;
+  if constexpr (WHOLE) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool low = half ? c < pairs : (e & 1) == 0;
+      const float2 cs = c < a.rot ? turns[half ? (low ? c + e : c + e - pairs) : (c + e) / 2] : make_float2(1.f, 0.f);
+      turn.c[e] = cs.x;
+      turn.s[e] = low ? -cs.y : cs.y;
+    }
+  }
+  const int partner = (c < pairs ? lane + pairs / 8 : lane - pairs / 8) & 63;
+  const bool opposite = pairs == 4 * LPR;              // halves of whole rows: the partner is lane ^ LPR / 2
+  const float inv_d = 1.0f / (float)a.d_k;
   for (; first - tid / LPR < r1; first += HR_BATCH * AT_ONCE) {        // (whole waves stay together: lanes exchange columns)
 #pragma unroll
     for (int k = 0; k < HR_BATCH; ++k) {
       const int r = first + k * AT_ONCE;
       const bool is_q = r < nq, is_k = !is_q && r < nq + nk;
       const bool turned = (is_q || is_k) && r < r1, inside = r < r1 && c < (turned ? a.d_k : a.d_v);
+      if (first - tid / LPR + k * AT_ONCE >= r1) continue;             // (no row for any thread)
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = 0.f;
@@ -120,35 +149,40 @@ __global__ void __launch_bounds__(HR_THREADS) head_rows_kernel(HeadRowsArgs a, i
         if constexpr (LPR > 4) sum += lane_xor<4>(sum, lane);
         if constexpr (LPR > 8) sum += lane_xor<8>(sum, lane);
         if constexpr (LPR > 16) sum += lane_xor<16>(sum, lane);
-        const float by = 1.0f / sqrtf(sum / (float)a.d_k + a.eps);
-        const T* w = static_cast<const T*>(is_q ? a.q_weight : a.k_weight);
+        const float by = __builtin_amdgcn_rsqf(fmaf(sum, inv_d, a.eps));
+        float w[8];
+        Piece8<T> mine = wk;
+        if (is_q) mine = wq;
+        mine.get(w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= by;
-        if (w && inside && turned) {
-          Piece8<T> wp;
-          wp.load(w + c);
-          float wf[8];
-          wp.get(wf);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] *= wf[e];
-        }
+        for (int e = 0; e < 8; ++e) y[e] *= by * w[e];
       }
-      if (half && pairs > 0) {
+      if constexpr (WHOLE) {
         float z[8];
-        if (pairs % 8 == 0) {                          // the partners lie in one lane
-          const int other = (c < pairs ? lane + pairs / 8 : lane - pairs / 8) & 63;
+        if (!half) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], other);
+          for (int e = 0; e < 8; ++e) z[e] = y[e ^ 1];
+        } else if (opposite) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[e] = lane_xor<LPR / 2>(y[e], lane);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {                // columns c + e -+ pairs: one of 8 values of some lane
-            const int col = c + e < pairs ? c + e + pairs : c + e - pairs, other = (lane - part + (col >> 3)) & 63;
-            z[e] = 0.f;
+          for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], partner);
+        }
+        if (c < a.rot) {
 #pragma unroll
-            for (int f = 0; f < 8; ++f) {
-              const float v = __shfl(y[f], other);
-              z[e] = (col & 7) == f ? v : z[e];
-            }
+          for (int e = 0; e < 8; ++e) y[e] = fmaf(z[e], turn.s[e], y[e] * turn.c[e]);
+        }
+      } else if (half) {
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {                  // columns c + e -+ pairs: one of 8 values of some lane
+          const int col = c + e < pairs ? c + e + pairs : c + e - pairs, other = (lane - part + (col >> 3)) & 63;
+          z[e] = 0.f;
+#pragma unroll
+          for (int f = 0; f < 8; ++f) {
+            const float v = __shfl(y[f], other);
+            z[e] = (col & 7) == f ? v : z[e];
           }
         }
 #pragma unroll
@@ -187,6 +221,11 @@ __global__ void __launch_bounds__(HR_THREADS) head_rows_kernel(HeadRowsArgs a, i
   }
 }
 
+template <typename T, bool WHOLE>
+static auto head_rows_kernel_of(int lpr) -> void (*)(HeadRowsArgs, int) {
+  return lpr == 4 ? head_rows_kernel<T, 4, WHOLE> : lpr == 8 ? head_rows_kernel<T, 8, WHOLE> : lpr == 16 ? head_rows_kernel<T, 16, WHOLE> : head_rows_kernel<T, 32, WHOLE>;
+}
+
 static int launch_head_rows_tokens(const HeadRowsArgs& a, int dtype, hipStream_t st) {
   const int widest = a.slots && a.d_v > a.d_k ? a.d_v : a.d_k, lpr = widest <= 32 ? 4 : widest <= 64 ? 8 : widest <= 128 ? 16 : 32;
   const int rows = (a.q ? a.H : 0) + (a.k ? a.H_kv : 0) + (a.slots ? a.H_kv : 0);
@@ -194,11 +233,9 @@ static int launch_head_rows_tokens(const HeadRowsArgs& a, int dtype, hipStream_t
   const int step = HR_BATCH * (HR_THREADS / lpr);
   const int block_rows = a.T >= 2 * device_cu_count() ? rows : std::min(rows, step);
   const dim3 grid((unsigned)a.T, (unsigned)((rows + block_rows - 1) / block_rows));
-  void (*fn)(HeadRowsArgs, int);
-  if (dtype == TPLA_F32)
-    fn = lpr == 4 ? head_rows_kernel<float, 4> : lpr == 8 ? head_rows_kernel<float, 8> : lpr == 16 ? head_rows_kernel<float, 16> : head_rows_kernel<float, 32>;
-  else
-    fn = lpr == 4 ? head_rows_kernel<bf16_t, 4> : lpr == 8 ? head_rows_kernel<bf16_t, 8> : lpr == 16 ? head_rows_kernel<bf16_t, 16> : head_rows_kernel<bf16_t, 32>;
+  const bool whole = a.rot % (a.layout == TPLA_ROTARY_HALF ? 16 : 8) == 0;
+  void (*fn)(HeadRowsArgs, int) = dtype == TPLA_F32 ? (whole ? head_rows_kernel_of<float, true>(lpr) : head_rows_kernel_of<float, false>(lpr))
+                                                    : (whole ? head_rows_kernel_of<bf16_t, true>(lpr) : head_rows_kernel_of<bf16_t, false>(lpr));
   hipLaunchKernelGGL(fn, grid, dim3(HR_THREADS), std::max(1, a.rot / 2) * sizeof(float2), st, a, block_rows);
   return check_launch("head_rows_kernel");
 }
