@@ -600,8 +600,8 @@ int tpla_decode_heads(const tpla_heads_t* shape, const void* q, const void* k_po
  * a sequence (rows beyond it are not computed).  Rows behind cu_seqlens[B] are left as they were.  What a token's key or value holds
  * (infinities and NaN too) does not reach rows that do not see it.  Tokens beyond the block-table row do not exist: they are not seen.
  * q [T, H, d_k] in shape->dtype, dense; o [T, H, d_v] in o_dtype; lse float [T, H] or NULL.  T = 0 does nothing.  workspace:
- * tpla_workspace_bytes_prefill_heads() bytes (the work of few rows is split over their tokens); it may be NULL where that is 0.  Kernels,
- * pages of negative entries, lengths, limits (T in the place of B) and reproducibility as in tpla_decode_heads.
+ * tpla_workspace_bytes_prefill_heads() bytes (the work of few rows is split over their tokens), which serve calls of fewer tokens and fewer
+ * new ones too; it may be NULL where that is 0.  Kernels, pages of negative entries, lengths, limits (T in the place of B) and reproducibility as in tpla_decode_heads.
  */
 size_t tpla_workspace_bytes_prefill_heads(const tpla_heads_t* shape, int64_t T, int32_t max_new, int32_t max_pages_per_seq);
 int tpla_prefill_heads(const tpla_heads_t* shape, const void* q, const void* k_pool, const void* v_pool, const int32_t* block_table,

@@ -93,6 +93,13 @@ static HeadsPlan plan_heads(const tpla_heads_t& sh, int64_t T, int32_t max_new, 
   return general_heads_plan(sh, T, max_new, max_pages);
 }
 
+// What a prefill of up to T tokens, up to max_new of a sequence, needs at most, whichever kernel and split its own numbers lead to.
+static size_t prefill_room(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages) {
+  if (!heads_mfma_supported(sh)) return general_heads_room(sh, T, max_pages);
+  const size_t few = heads_ranges_room(sh, max_new, max_pages), many = heads_prompts_room(sh, T, max_pages);
+  return few > many ? few : many;
+}
+
 // rows: of q (decode: B, prefill: T); max_new: 0 for decode, cut to T
 static int check_attention(const tpla_heads_t* sh, int64_t rows, int32_t* max_new, int32_t max_pages, HeadsPlan* p) {
   int rc = check_heads(sh);
@@ -246,7 +253,7 @@ int tpla_decode_heads(const tpla_heads_t* shape, const void* q, const void* k_po
 size_t tpla_workspace_bytes_prefill_heads(const tpla_heads_t* shape, int64_t T, int32_t max_new, int32_t max_pages_per_seq) {
   HeadsPlan p;
   if (T < 1 || max_new < 1 || check_attention(shape, T, &max_new, max_pages_per_seq, &p)) return 0;
-  return p.workspace;
+  return prefill_room(*shape, T, max_new, max_pages_per_seq);
 }
 
 int tpla_prefill_heads(const tpla_heads_t* shape, const void* q, const void* k_pool, const void* v_pool, const int32_t* block_table,

@@ -46,14 +46,17 @@ struct HeadsPlan {
 };
 // max_new = 0: decode
 HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages);
+size_t general_heads_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages);      // the most that a prefill of up to T tokens needs
 int launch_general_heads(const HeadsArgs& a, const HeadsPlan& p, int dtype, hipStream_t st);
 // bf16, d_k = d_v of 64 or 128, pages of a multiple of 16 tokens, at most 64 rows per head of keys: see heads_ranges.hip
 bool heads_mfma_supported(const tpla_heads_t& sh);
 bool heads_ranges_fit(const tpla_heads_t& sh, int32_t max_new);
 HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages);
+size_t heads_ranges_room(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages);
 int launch_heads_ranges(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st);
 // the same types, any number of rows: see heads_prompts.hip
 HeadsPlan heads_prompts_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages);
+size_t heads_prompts_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages);
 int launch_heads_prompts(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st);
 
 // A work item: `rows` rows of one head of keys of one sequence.  Row r of a (sequence, head) is its new token r / G, query head r % G of the group.

@@ -270,6 +270,19 @@ HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
   return p;
 }
 
+// items * n_splits is below 4 compute units' worth of items and one more split of each, and there are fewer items than that wherever they are split.
+size_t general_heads_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages) {
+  if ((int64_t)max_pages * sh.page_tokens <= 256) return 0;
+  const int64_t fill = 4 * (int64_t)device_cu_count();
+  size_t most = 0;
+  for (int rows = 16; rows <= 64; rows *= 4) {
+    const int64_t items = (T * (sh.H / sh.H_kv) / rows + sh.B) * sh.H_kv, slots = (items < fill ? items : fill) + fill;
+    const size_t bytes = (size_t)slots * rows * (sh.d_v + 2) * sizeof(float);
+    most = bytes > most ? bytes : most;
+  }
+  return most;
+}
+
 template <typename T, bool JOIN>
 static int launch_general(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st) {
   const int nb = ((a.d_k > a.d_v ? a.d_k : a.d_v) + 15) / 16;

@@ -434,19 +434,26 @@ __global__ void __launch_bounds__(256) heads_prompts_merge_kernel(HeadsArgs a) {
   if (a.lse && c == 0) a.lse[out] = heads_lse(M, sum);
 }
 
+static int64_t prompts_items(const tpla_heads_t& sh, int64_t T) { return (T * (sh.H / sh.H_kv) / HP_ROWS + sh.B) * sh.H_kv; }
+
 HeadsPlan heads_prompts_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages) {
   HeadsPlan p;
   p.kernel = HEADS_PROMPTS;
   p.rows = HP_ROWS;
-  const int64_t tiles = T * (sh.H / sh.H_kv) / HP_ROWS + sh.B;
-  p.tiles = (int)tiles;
-  p.items = tiles * sh.H_kv;
+  p.items = prompts_items(sh, T);
+  p.tiles = (int)(p.items / sh.H_kv);
   p.n_wg = 2 * device_cu_count();                      // workgroups that the chip holds
   // Split where the items do not fill it twice and there are tokens to split.
   p.n_splits = p.items < 2 * p.n_wg && (int64_t)max_pages * sh.page_tokens > HP_CHUNK_MIN ? 2 : 1;
   p.slots = p.n_splits > 1 ? p.items + p.n_wg : 0;     // (the parts of an item: what it reads over the chunk's length, rounded up)
   p.workspace = (size_t)p.slots * p.rows * (sh.d_v + 2) * sizeof(float);
   return p;
+}
+
+size_t heads_prompts_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages) {
+  if ((int64_t)max_pages * sh.page_tokens <= HP_CHUNK_MIN) return 0;
+  const int64_t n_wg = 2 * device_cu_count();
+  return (size_t)(std::min(prompts_items(sh, T), 2 * n_wg) + n_wg) * HP_ROWS * (sh.d_v + 2) * sizeof(float);
 }
 
 int launch_heads_prompts(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st) {

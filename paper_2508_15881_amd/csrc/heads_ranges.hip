@@ -496,6 +496,12 @@ HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max
   return p;
 }
 
+size_t heads_ranges_room(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages) {
+  size_t most = 0;
+  for (int32_t n = 1; n <= max_new && heads_ranges_fit(sh, n); ++n) most = std::max(most, heads_ranges_plan(sh, n, max_pages).workspace);
+  return most;
+}
+
 int launch_heads_ranges(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st) {
   void (*fn)(HeadsArgs);
   void (*merge)(HeadsArgs);

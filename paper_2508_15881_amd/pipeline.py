@@ -185,6 +185,52 @@ class DraftStep:
         B.tpla_commit_drafts(self.shape, self.T, accepted, n_accepted, seq_lens, block_table, self.max_pages, shard_pools, new_lens)
 
 
+class HeadsStep:
+    """Buffers and call order of layers with grouped heads, for the tokens that a serving step adds to each of B sequences: one (decode) or
+    up to max_new (prompts, or parts of prompts behind cached tokens).  The pages, slots and positions are those of the latent layers."""
+
+    def __init__(self, shape, max_pages_per_seq, frequencies, max_tokens=None, max_new=1, layout=B.TPLA_ROTARY_HALF, amplitude=1.0, norm_eps=1e-6,
+                 device="cuda"):
+        """max_tokens: room for new tokens of all sequences together (B of them by default)."""
+        self.shape, self.max_pages, self.max_new = shape, int(max_pages_per_seq), int(max_new)
+        self.T = int(max_tokens or shape.B)
+        self.layout, self.amplitude, self.norm_eps = layout, float(amplitude), float(norm_eps)
+        self.freq = torch.as_tensor(frequencies, dtype=torch.float64).to(device)
+        self.tables = B.TplaShape(shape.B, 1, 8, 1, 8, 1, 1, shape.page_tokens, shape.dtype, 1.0)      # B and page_tokens are what counts
+        st = torch_dtype(shape.dtype)
+        ints = lambda n: torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
+        self.slots, self.positions, self.cu, self.counts = ints(self.T), ints(self.T), ints(shape.B + 1), ints(2)
+        self.q = torch.empty((self.T, shape.H, shape.d_k), dtype=st, device=device)
+        self.o = torch.empty((self.T, shape.H, shape.d_v), dtype=st, device=device)
+        self.lse = torch.empty((self.T, shape.H), dtype=torch.float32, device=device)
+        n = B.tpla_workspace_bytes_heads(shape, self.max_pages)
+        if n == 0:
+            raise B.TplaError(-2, B.tpla_last_error())
+        self.ws_bytes = max(n, B.tpla_workspace_bytes_prefill_heads(shape, self.T, self.max_new, self.max_pages))
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+
+    def place(self, seq_lens, add_lens, free_pages, n_free, pages_held, block_table):
+        """Pages, slots and positions of the new tokens, packed (once per step, for all layers).  counts: pages taken, pages that were missing;
+        tokens without a page are neither written nor seen."""
+        B.tpla_extend_sequences(self.tables, seq_lens, add_lens, 0, None, free_pages, n_free, pages_held, pages_held, block_table, self.max_pages,
+                                self.cu, self.slots, self.positions, self.T, self.counts)
+
+    def run(self, q, k, v, q_weight, k_weight, k_pool, v_pool, block_table, seq_lens, decode=False):
+        """One layer: q [T, H, d_k], k [T, H_kv, d_k], v [T, H_kv, d_v] of the step's T new tokens (views of a projection will do), written to
+        the cache and attended to.  seq_lens: as for place, before the new tokens; decode: one new token for every sequence, seq_lens with it.
+        Returns o [T, H, d_v] in the storage type."""
+        T = q.shape[0]
+        B.tpla_append_heads(self.shape, self.layout, 2 * self.freq.numel(), self.freq, self.amplitude, q_weight, k_weight, self.norm_eps,
+                            self.positions[:T], T, q, self.q[:T], k, v, self.slots[:T], k_pool, v_pool)
+        if decode:
+            B.tpla_decode_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.workspace, self.ws_bytes,
+                                self.o[:T], self.shape.dtype, self.lse[:T])
+        else:
+            B.tpla_prefill_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.cu, T, min(self.max_new, T),
+                                 self.workspace, self.ws_bytes, self.o[:T], self.shape.dtype, self.lse[:T])
+        return self.o[:T]
+
+
 def transform_weights(shape, mode, signs, U, W_UK, W_UV):
     """W_UK [H,d_n,d_c] -> W_UK U (last axis); W_UV [H,d_c,d_v] -> U^T W_UV (middle axis)."""
     W_UK_t = torch.empty_like(W_UK)

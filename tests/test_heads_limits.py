@@ -90,7 +90,10 @@ def test_prefill():
     assert prefill(T=-1) == -2 and prefill(most=0) == -2 and prefill(most=-1) == -2 and prefill(pages=0) == -2 and prefill(pages=0, T=0) == -2
     assert prefill(o_dtype=9) == -5 and prefill(T=1 << 25, most=5) == -7 and prefill(pages=1 << 25) == -7 and prefill(T=1 << 40, most=5) == -7
     need = tp.tpla_workspace_bytes_prefill_heads(shape(), 9, 9, 1024)
-    assert need > 0 and prefill(pages=1024, n=need - 1) == -4 and prefill(pages=1024, ws=None, n=need) == -1
+    assert need > 0 and prefill(pages=1024, n=1024) == -4 and prefill(pages=1024, ws=None, n=need) == -1
+    for s in (shape(), shape(H_kv=8), shape(dtype=F), shape(B=1, H=1, H_kv=1, d_k=64, d_v=64), shape(d_v=64)):         # room for fewer tokens too
+        sizes = [tp.tpla_workspace_bytes_prefill_heads(s, t, min(t, 100), 1024) for t in (1, 5, 9, 64, 200, 1000, 4000, 20000)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
     assert tp.tpla_workspace_bytes_prefill_heads(shape(), 9, 50, 1024) == need              # no more new tokens than there are rows
     assert tp.tpla_workspace_bytes_prefill_heads(shape(), 0, 9, 4) == 0 and tp.tpla_workspace_bytes_prefill_heads(shape(), 9, 0, 4) == 0
     assert prefill(T=0, most=0, q=None, cu=None, o=None) == 0
