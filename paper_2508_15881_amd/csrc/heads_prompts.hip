@@ -19,7 +19,7 @@ constexpr int HP_TILE = 8192;            // bytes of keys, and of values, of a t
 constexpr int HP_CPT = HP_TILE / 1024 / HP_NW;   // direct loads per wave, of keys and of values
 constexpr int HP_IDS = 1024;             // page ids held at once
 constexpr int HP_ODD = HP_NSTAGE * 2 * HP_TILE + HP_IDS * 4;
-constexpr int HP_LDS = HP_ODD + 16;
+constexpr int HP_LDS = HP_ODD + (HP_NSTAGE + 1) * 4;
 constexpr int HP_CHUNK_MIN = 512;        // tokens of a part of an item at least
 
 // One part of an item: tokens [k0, k1).
@@ -65,7 +65,7 @@ __device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, bool it
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
     const double per = ceil(work * a.H_kv / a.n_wg);       // (whole numbers below 2^53)
-    chunk = per < 1073741824.0 ? max(((int)per + 63) / 64 * 64, HP_CHUNK_MIN) : 0x7fffffff;
+    chunk = __builtin_amdgcn_readfirstlane(per < 1073741824.0 ? max(((int)per + 63) / 64 * 64, HP_CHUNK_MIN) : 0x7fffffff);
   }
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     const PromptSeq s = b0 == 0 ? front : prompt_seq(a, b0 + lane);
@@ -107,10 +107,12 @@ template <int D, bool PARTS>
 __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs a) {
   constexpr int RC = D / 8, TOK = HP_TILE / (2 * D), TB = TOK / 16, KS = D / 32, DB = D / 16, QB = HP_QB;
   constexpr int LOAD_TOK = 64 / RC;
+  static_assert(QB * DB <= 16, "the accumulators are a0 to a63");
   extern __shared__ u32x4 smem[];
   char* const lds = reinterpret_cast<char*>(smem);
   int* const ids = reinterpret_cast<int*>(lds + HP_NSTAGE * 2 * HP_TILE);
   int* const odd_tile = reinterpret_cast<int*>(lds + HP_ODD);      // 1 + the last tile of each place that holds values that are not finite
+  int* const first_hole = odd_tile + HP_NSTAGE;                     // first page of those in ids that is missing
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j16 = lane & 15, q4 = lane >> 4;
   PromptUnit u;
   if (!prompt_unit<PARTS>(a, blockIdx.x, false, u)) return;
@@ -122,8 +124,8 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   unsigned ld_at[HP_CPT], k_at[KS], v_at[DB];
 #pragma unroll
   for (int j = 0; j < HP_CPT; ++j) {
-    const int tok = (wave + j * HP_NW) * LOAD_TOK + lane / RC;
-    ld_at[j] = (unsigned)(tok * (2 * D) + ((lane % RC) ^ heads_swz<RC>(tok)) * 16);
+    const int tok = (wave + j * HP_NW) * LOAD_TOK + lane / RC;      // the piece of the row that this lane loads, and the row within the load
+    ld_at[j] = (unsigned)((lane / RC) * (2 * D) + ((lane % RC) ^ heads_swz<RC>(tok)) * 16);
   }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) k_at[ks] = (j16 * RC + ((4 * ks + q4) ^ heads_swz<RC>(j16))) * 16;
@@ -134,71 +136,76 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
 
   const int pt = a.page_tokens, shift = (pt & (pt - 1)) == 0 ? __builtin_ctz(pt) : -1;
   auto page_of = [&](int t) { return shift >= 0 ? t >> shift : t / pt; };
-  const bool one_page = pt % TOK == 0;
   const size_t page_bytes = (size_t)a.H_kv * pt * (2 * D);
   const int32_t* table = a.table + (size_t)it.b * a.max_pages;
   const char* k_head = static_cast<const char*>(a.k_pool) + (size_t)it.kvh * pt * (2 * D);
   const char* v_head = static_cast<const char*>(a.v_pool) + (size_t)it.kvh * pt * (2 * D);
   int id0 = 0;
-  auto id_of = [&](int p) { return lds_read_page(ids + (p - id0)); };
 
-  // Tile t on its way.  Tokens past the end repeat the last one, those of missing pages are page 0's; they are masked, and their values zeroed.
-  auto issue = [&](int t) {
-    const int tok0 = t * TOK;
+  // Tile t on its way.  A load's tokens lie in one page (of a multiple of 16 tokens); ids: their pages.
+  auto load_tok = [&](int t, int j) { return t * TOK + (wave + j * HP_NW) * LOAD_TOK; };
+  auto issue_whole = [&](int t, const int (&id)[HP_CPT]) {
     char* dst = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + wave * 1024;
-    if (one_page && tok0 + TOK <= keys) {
-      const int p = page_of(tok0), id = max(__builtin_amdgcn_readfirstlane(id_of(p)), 0);
-      const size_t at = (size_t)id * page_bytes + (size_t)(tok0 - p * pt) * (2 * D);
+    size_t at[HP_CPT];
 #pragma unroll
-      for (int j = 0; j < HP_CPT; ++j)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k_head + at + ld_at[j]),
-                                         (__attribute__((address_space(3))) void*)(dst + j * HP_NW * 1024), 16, 0, 0);
+    for (int j = 0; j < HP_CPT; ++j) {
+      const int tok = load_tok(t, j);
+      at[j] = (size_t)(unsigned)max(__builtin_amdgcn_readfirstlane(id[j]), 0) * page_bytes + (size_t)(tok - page_of(tok) * pt) * (2 * D);
+    }
 #pragma unroll
-      for (int j = 0; j < HP_CPT; ++j)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v_head + at + ld_at[j]),
-                                         (__attribute__((address_space(3))) void*)(dst + HP_TILE + j * HP_NW * 1024), 16, 0, 0);
-    } else {
+    for (int j = 0; j < HP_CPT; ++j)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k_head + at[j] + ld_at[j]),
+                                       (__attribute__((address_space(3))) void*)(dst + j * HP_NW * 1024), 16, 0, 0);
 #pragma unroll
-      for (int j = 0; j < HP_CPT; ++j) {
-        const int in_tile = (wave + j * HP_NW) * LOAD_TOK + lane / RC, tok = min(tok0 + in_tile, keys - 1), p = page_of(tok), id = max(id_of(p), 0);
-        const size_t at = (size_t)id * page_bytes + (size_t)(tok - p * pt) * (2 * D) + ((lane % RC) ^ heads_swz<RC>(in_tile)) * 16;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k_head + at),
-                                         (__attribute__((address_space(3))) void*)(dst + j * HP_NW * 1024), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v_head + at),
-                                         (__attribute__((address_space(3))) void*)(dst + HP_TILE + j * HP_NW * 1024), 16, 0, 0);
-      }
+    for (int j = 0; j < HP_CPT; ++j)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v_head + at[j] + ld_at[j]),
+                                       (__attribute__((address_space(3))) void*)(dst + HP_TILE + j * HP_NW * 1024), 16, 0, 0);
+  };
+  // Tokens past the end repeat the last one, those of missing pages are page 0's; they are masked, and their values zeroed.
+  auto issue = [&](int t) {
+    if ((t + 1) * TOK <= keys) {
+      int id[HP_CPT];
+#pragma unroll
+      for (int j = 0; j < HP_CPT; ++j) id[j] = lds_read_page(ids + (page_of(load_tok(t, j)) - id0));
+      issue_whole(t, id);
+      return;
+    }
+    char* dst = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + wave * 1024;
+#pragma unroll 1
+    for (int j = 0; j < HP_CPT; ++j) {
+      const int in_tile = (wave + j * HP_NW) * LOAD_TOK + lane / RC, tok = min(t * TOK + in_tile, keys - 1), p = page_of(tok);
+      const int id = max(lds_read_page(ids + (p - id0)), 0);
+      const size_t at = (size_t)id * page_bytes + (size_t)(tok - p * pt) * (2 * D) + ((lane % RC) ^ heads_swz<RC>(in_tile)) * 16;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k_head + at),
+                                       (__attribute__((address_space(3))) void*)(dst + j * HP_NW * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v_head + at),
+                                       (__attribute__((address_space(3))) void*)(dst + HP_TILE + j * HP_NW * 1024), 16, 0, 0);
     }
   };
-  // Which blocks of 16 tokens of a tile have a page.
-  auto blocks_there = [&](int t) {
-    int there = 0;
-    if (one_page) {
-      there = __builtin_amdgcn_readfirstlane(id_of(page_of(t * TOK))) >= 0 ? (1 << TB) - 1 : 0;
-    } else {
-#pragma unroll
-      for (int n = 0; n < TB; ++n)
-        if (t * TOK + 16 * n < keys && __builtin_amdgcn_readfirstlane(id_of(page_of(t * TOK + 16 * n))) >= 0) there |= 1 << n;
-    }
-    return there;
+  // The tile t is there, its own loads of the next two tiles may be on their way.
+  auto arrived = [&](int t, int c1) {
+    if (t + 2 < c1)
+      loads_wait<2 * 2 * HP_CPT>();
+    else if (t + 1 < c1)
+      loads_wait<2 * HP_CPT>();
+    else
+      loads_wait<0>();
   };
 
   // ---- this wave's rows ----
   const int row_w = it.row0 + wave * (16 * QB);
   int sees[QB];
-  size_t out_row[QB];
 #pragma unroll
   for (int r = 0; r < QB; ++r) {
-    const int row = row_w + 16 * r + j16, mine = min(row, it.rows - 1);
-    sees[r] = row < it.rows ? it.sees(mine, a.G) : 0;
-    out_row[r] = (size_t)(it.first + mine / a.G) * a.H + it.kvh * a.G + mine % a.G;
+    const int row = row_w + 16 * r + j16;
+    sees[r] = row < it.rows ? it.sees(row, a.G) : 0;
   }
+  auto out_row = [&](int row) { return (size_t)(it.first + row / a.G) * a.H + it.kvh * a.G + row % a.G; };
   const bool alive = row_w < it.rows;
-  const int most = alive ? it.sees(min(row_w + 16 * QB, it.rows) - 1, a.G) : 0;                       // tokens that some row of the wave sees,
-  const int least_w = row_w + 16 * QB <= it.rows ? it.sees(row_w, a.G) : 0;                           // and that all of its rows see
-  const int least = it.sees(it.row0, a.G);                                                            // that all rows of the workgroup see
+  const int most = alive ? it.sees(min(row_w + 16 * QB, it.rows) - 1, a.G) : 0;                       // tokens that some row of the wave sees
+  const int least = it.sees(it.row0, a.G);                                                            // and that all rows of the workgroup see
 
   bf16x8 q[QB][KS];
-  f32x4 acc[QB][DB];
   float m[QB], l[QB];
   int seen[QB];
 #pragma unroll
@@ -206,18 +213,18 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
     m[r] = -INFINITY;
     l[r] = 0.f;
     seen[r] = 0;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) acc[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  out_keep();
+  static_for<QB * DB>([&](auto ic) { out_write<decltype(ic)::value>(f32x4{0.f, 0.f, 0.f, 0.f}); });
 
-  // ---- one tile: CUT: some of its tokens are not seen by some rows ----
+  // ---- one tile.  CUT: some of its tokens are not seen by some rows; there: its blocks of 16 tokens that have a page ----
   auto tile_body = [&](int t, int there, auto cut_tag) {
     constexpr bool CUT = decltype(cut_tag)::value;
     const int tok0 = t * TOK;
     const unsigned base = lds_base + (unsigned)((t % HP_NSTAGE) * (2 * HP_TILE));
     f32x4 s[QB][TB];
     {
-      constexpr int N = KS * TB, AHEAD = 8;
+      constexpr int N = KS * TB, AHEAD = D == 128 ? 8 : 4;
       bf16x8 kf[AHEAD];
       static_for<AHEAD>([&](auto ic) {
         constexpr int x = decltype(ic)::value;
@@ -227,8 +234,12 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
         constexpr int x = decltype(ic)::value, ks = x / TB, n = x % TB;
         lds_wait<(N - 1 - x < AHEAD - 1 ? N - 1 - x : AHEAD - 1)>(kf[x % AHEAD]);
 #pragma unroll
-        for (int r = 0; r < QB; ++r)
-          s[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x % AHEAD], q[r][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[r][n], 0, 0, 0);
+        for (int r = 0; r < QB; ++r) {
+          if constexpr (ks == 0)
+            score_first(s[r][n], kf[x % AHEAD], q[r][ks]);
+          else
+            score_more(s[r][n], kf[x % AHEAD], q[r][ks]);
+        }
         if constexpr (x + AHEAD < N) lds_read_b128<((x + AHEAD) % TB) * (16 * RC * 16)>(kf[x % AHEAD], base + k_at[(x + AHEAD) / TB]);
       });
     }
@@ -241,10 +252,15 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
       lds_read_tr_b64<(y / DB) * (32 * RC * 16) + 16 * RC * 16>(hi[y % VA], base + v_at[y % DB]);
     };
     if constexpr (!CUT) static_for<VA>([&](auto ic) { value(ic); });
+    out_settle_result();
+#pragma unroll
+    for (int r = 0; r < QB; ++r)
+#pragma unroll
+      for (int n = 0; n < TB; ++n) settle_scores(s[r][n]);
 
     bf16x8 p[QB][TB / 2];
-#pragma unroll
-    for (int r = 0; r < QB; ++r) {
+    static_for<QB>([&](auto rc) {
+      constexpr int r = decltype(rc)::value;
       if constexpr (CUT) {
 #pragma unroll
         for (int n = 0; n < TB; ++n)
@@ -254,8 +270,6 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
             seen[r] |= vis;
             if (!vis) s[r][n][i] = -INFINITY;
           }
-      } else {
-        seen[r] = 1;
       }
       float top = s[r][0][0];
 #pragma unroll
@@ -270,8 +284,8 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[r] - m_new);
         l[r] *= alpha;
         m[r] = m_new;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[r][d] *= alpha;
+        out_settle_result();
+        static_for<DB>([&](auto dc) { out_scale<r * DB + decltype(dc)::value>(alpha); });
       }
       const float ref = m[r] == -INFINITY ? 0.f : m[r];
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -284,8 +298,12 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
           p[r][n / 2][4 * (n & 1) + i] = (bf16_t)e;
         }
       l[r] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    }
+    });
 
+#pragma unroll
+    for (int r = 0; r < QB; ++r)
+#pragma unroll
+      for (int h = 0; h < TB / 2; ++h) settle_weights(p[r][h]);
     bool odd = false;
     if constexpr (CUT) odd = __builtin_amdgcn_readfirstlane(lds_read_page(odd_tile + t % HP_NSTAGE)) == t + 1;
     if (!odd) {
@@ -294,34 +312,43 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
         constexpr int x = decltype(ic)::value, d = x % DB, h = x / DB, ahead = NV - 1 - x < VA - 1 ? NV - 1 - x : VA - 1;
         lds_wait<2 * ahead>(lo[x % VA], hi[x % VA]);
         const u32x4 v = {lo[x % VA][0], lo[x % VA][1], hi[x % VA][0], hi[x % VA][1]};
-#pragma unroll
-        for (int r = 0; r < QB; ++r)
-          acc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), p[r][h], acc[r][d], 0, 0, 0);
+        static_for<QB>([&](auto rc) { out_product<decltype(rc)::value * DB + d>(v, p[decltype(rc)::value][h]); });
         if constexpr (x + VA < NV) value(std::integral_constant<int, x + VA>{});
       });
     } else {
       // A weight of zero does not silence what is not finite: one token at a time, kept by the rows that see it.
+      out_settle_result();
 #pragma unroll 1
       for (int tok = 0; tok < TOK; ++tok) {
-        const int h = tok >> 5;
+        const unsigned h = tok >> 5;
         const u32x4 keep = keep_token(tok, q4);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
+        out_keep();
+        static_for<DB>([&](auto dc) {
+          constexpr int d = decltype(dc)::value;
           u32x2 vlo, vhi;
           lds_read_tr_b64<0>(vlo, base + v_at[d] + h * (32 * RC * 16));
           lds_read_tr_b64<16 * RC * 16>(vhi, base + v_at[d] + h * (32 * RC * 16));
           lds_wait<0>(vlo, vhi);
-          const u32x4 v = u32x4{vlo[0], vlo[1], vhi[0], vhi[1]} & keep;
-#pragma unroll
-          for (int r = 0; r < QB; ++r) {
+          bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{vlo[0], vlo[1], vhi[0], vhi[1]} & keep);
+          settle_weights(v);
+          static_for<QB>([&](auto rc) {
+            constexpr int r = decltype(rc)::value;
             u32x4 w = __builtin_bit_cast(u32x4, p[r][0]);
-            if constexpr (TB == 4) w = h ? __builtin_bit_cast(u32x4, p[r][1]) : w;
-            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w & keep), acc[r][d], 0, 0, 0);
+            if constexpr (TB == 4) w = (w & (h - 1u)) | (__builtin_bit_cast(u32x4, p[r][1]) & (0u - h));
+            const f32x4 was = out_read<r * DB + d>();
+            bf16x8 one = __builtin_bit_cast(bf16x8, w & keep);
+            f32x4 x = was;
+            settle_scores(x);
+            settle_weights(one);
+            score_more(x, v, one);
+            out_settle_result();
+            settle_scores(x);
             const bool vis = ((there >> (tok >> 4)) & 1) && tok0 + tok < sees[r];
-            acc[r][d] = vis ? x : acc[r][d];
-          }
-        }
+            out_write<r * DB + d>(vis ? x : was);
+          });
+        });
       }
+      out_settle_write();
     }
   };
 
@@ -331,81 +358,119 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
     const int c1 = min(t1, c0 + id_tiles);
     __syncthreads();
     id0 = page_of(c0 * TOK);
+    if (tid == 0) *first_hole = 0x7fffffff;
+    __syncthreads();
     for (int x = tid; x < HP_IDS; x += HP_NW * 64) {
       const int p = id0 + x;
-      if (p < a.max_pages && (long long)p * pt < (long long)min(keys, c1 * TOK)) ids[x] = table[p];
+      if (p < a.max_pages && (long long)p * pt < (long long)min(keys, c1 * TOK)) {
+        const int id = table[p];
+        ids[x] = id;
+        if (id < 0) atomicMin(first_hole, p);
+      }
     }
     __syncthreads();
+    // tiles that exist whole and that every row of the workgroup sees
+    const int hole = __builtin_amdgcn_readfirstlane(*first_hole), plain = hole == 0x7fffffff ? least : min(least, hole * pt);
+    const int whole = min(c1, max(c0, plain / TOK));
     for (int t = c0; t < min(c1, c0 + HP_NSTAGE - 1); ++t) issue(t);
     if (c0 == t0) {
 #pragma unroll
       for (int r = 0; r < QB; ++r)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[r][ks] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.q) + out_row[r] * D + 32 * ks + 8 * q4);
+        for (int ks = 0; ks < KS; ++ks)
+          q[r][ks] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.q) + out_row(min(row_w + 16 * r + j16, it.rows - 1)) * D + 32 * ks + 8 * q4);
 #pragma unroll
       for (int r = 0; r < QB; ++r)
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[r][ks]));       // complete before the loop
     }
-    for (int t = c0; t < c1; ++t) {
-      if (t + 2 < c1)
-        loads_wait<2 * 2 * HP_CPT>();
-      else if (t + 1 < c1)
-        loads_wait<2 * HP_CPT>();
-      else
-        loads_wait<0>();
-      const int tok0 = t * TOK, there = blocks_there(t);
-      const bool holes = tok0 + TOK > keys || there != (1 << TB) - 1;
-      if (holes || tok0 + TOK > least) {
-        // what this wave has loaded: rows that are no tokens become zeros; values that are not finite, which some rows may not see
-        char* mine = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + HP_TILE + wave * 1024 + lane * 16;
+    int t = c0;
+    // the page ids of the tile that is requested next, read a tile ahead
+    const int last_id = page_of(max(min(keys, c1 * TOK) - 1, 0)) - id0;
+    int id[HP_CPT];
 #pragma unroll
-        for (int j = 0; j < HP_CPT; ++j) {
-          const int in_tile = (wave + j * HP_NW) * LOAD_TOK + lane / RC;
-          u32x4* piece = reinterpret_cast<u32x4*>(mine + j * HP_NW * 1024);
-          if (tok0 + in_tile >= keys || !((there >> (in_tile >> 4)) & 1)) {
-            *piece = u32x4{0u, 0u, 0u, 0u};
-          } else {
-            const u32x4 v = *piece;
-            if (not_finite_pair(v[0]) || not_finite_pair(v[1]) || not_finite_pair(v[2]) || not_finite_pair(v[3])) odd_tile[t % HP_NSTAGE] = t + 1;
-          }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
+    for (int j = 0; j < HP_CPT; ++j) id[j] = lds_read_page(ids + min(page_of(load_tok(t + HP_NSTAGE - 1, j)) - id0, last_id));
+    for (; t < whole; ++t) {
+      out_keep();
+      arrived(t, c1);
       __builtin_amdgcn_s_barrier();                    // tile t is there for all waves, tile t - 1 is no longer read
+      asm volatile("" ::: "memory");
+      const int next = t + HP_NSTAGE - 1;
+      if (next < c1) {
+        if ((next + 1) * TOK <= keys)
+          issue_whole(next, id);
+        else
+          issue(next);
+      }
+#pragma unroll
+      for (int j = 0; j < HP_CPT; ++j) lds_request_page(id[j], ids + min(page_of(load_tok(next + 1, j)) - id0, last_id));
+      if (alive) tile_body(t, 0, std::false_type{});
+#pragma unroll
+      for (int j = 0; j < HP_CPT; ++j) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(id[j]) : : "memory");      // (long there)
+    }
+    if (whole > t0) seen[0] = seen[1] = 1;
+    for (; t < c1; ++t) {
+      out_keep();
+      arrived(t, c1);
+      const int tok0 = t * TOK;
+      int there = 0;
+#pragma unroll
+      for (int n = 0; n < TB; ++n)
+        if (tok0 + 16 * n < keys && __builtin_amdgcn_readfirstlane(lds_read_page(ids + (page_of(tok0 + 16 * n) - id0))) >= 0) there |= 1 << n;
+      // what this wave has loaded: rows that are no tokens become zeros; values that are not finite, which some rows may not see
+      char* mine = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + HP_TILE + wave * 1024 + lane * 16;
+#pragma unroll
+      for (int j = 0; j < HP_CPT; ++j) {
+        const int in_tile = (wave + j * HP_NW) * LOAD_TOK + lane / RC;
+        u32x4* piece = reinterpret_cast<u32x4*>(mine + j * HP_NW * 1024);
+        if (tok0 + in_tile >= keys || !((there >> (in_tile >> 4)) & 1)) {
+          *piece = u32x4{0u, 0u, 0u, 0u};
+        } else {
+          const u32x4 v = *piece;
+          if (not_finite_pair(v[0]) || not_finite_pair(v[1]) || not_finite_pair(v[2]) || not_finite_pair(v[3])) odd_tile[t % HP_NSTAGE] = t + 1;
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       if (t + HP_NSTAGE - 1 < c1) issue(t + HP_NSTAGE - 1);
       if (tok0 >= most) continue;                      // (the wave's rows see none of it; the barriers above are still reached)
-      if (holes || tok0 + TOK > least_w)
-        tile_body(t, there, std::true_type{});
-      else
-        tile_body(t, there, std::false_type{});
+      tile_body(t, there, std::true_type{});
     }
   }
   if (!alive) return;
-#pragma unroll
-  for (int r = 0; r < QB; ++r) {
+  out_settle_result();
+  static_for<QB>([&](auto rc) {
+    constexpr int r = decltype(rc)::value;
     l[r] += lane_xor<16>(l[r], lane);
     l[r] += lane_xor<32>(l[r], lane);
     int any = seen[r];
     any |= __shfl_xor(any, 16);
     any |= __shfl_xor(any, 32);
     heads_close(m[r], l[r], any);
-    const int row = row_w + 16 * r + j16;
-    if (row >= it.rows) continue;
-    if (u.parts == 1) {
-      const float inv = heads_inverse(l[r]);
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-        store4(a.o, out_row[r] * D + 16 * d + 4 * q4, a.o_dtype, l[r] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[r][d] * inv);
-      if (a.lse && q4 == 0) a.lse[out_row[r]] = heads_lse(m[r], l[r]);
-    } else {
-      const size_t at = (size_t)u.slot * HP_ROWS + (row - it.row0);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(a.part_acc + at * D + 16 * d + 4 * q4) = acc[r][d];
-      if (q4 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m[r], l[r]);
+    int j = j16;
+    asm volatile("" : "+v"(j));                        // (made here: nothing of it is kept over the loops)
+    const int row = row_w + 16 * r + j;
+    const bool written = row < it.rows;
+    const float inv = heads_inverse(l[r]);
+    const size_t out = out_row(min(row, it.rows - 1));
+    const size_t at = (size_t)u.slot * HP_ROWS + (row - it.row0);
+    static_for<DB>([&](auto dc) {
+      constexpr int d = decltype(dc)::value;
+      const f32x4 x = out_read<r * DB + d>();
+      if (!written) return;
+      if (u.parts == 1)
+        store4(a.o, out * D + 16 * d + 4 * q4, a.o_dtype, l[r] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : x * inv);
+      else
+        *reinterpret_cast<f32x4*>(a.part_acc + at * D + 16 * d + 4 * q4) = x;
+    });
+    if (written && q4 == 0) {
+      if (u.parts > 1)
+        *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m[r], l[r]);
+      else if (a.lse)
+        a.lse[out] = heads_lse(m[r], l[r]);
     }
-  }
+  });
 }
 
 // grid: (items, groups of 256 / (D / 4) rows).  The parts of a row in their order, a thread for four columns.

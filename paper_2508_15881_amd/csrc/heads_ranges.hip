@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
           // A weight of zero does not silence what is not finite: one token at a time, kept by the rows that see it.
 #pragma unroll 1
           for (int tok = 0; tok < TOK; ++tok) {
-            const int h = tok >> 5;
+            const unsigned h = tok >> 5;
             const u32x4 keep = keep_token(tok, q4);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
 #pragma unroll
               for (int r = 0; r < RB; ++r) {
                 u32x4 w = __builtin_bit_cast(u32x4, p[r][0]);
-                if constexpr (TB == 4) w = h ? __builtin_bit_cast(u32x4, p[r][1]) : w;
+                if constexpr (TB == 4) w = (w & (h - 1u)) | (__builtin_bit_cast(u32x4, p[r][1]) & (0u - h));
                 const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w & keep), acc[r][d], 0, 0, 0);
                 const bool vis = ((there >> (tok >> 4)) & 1) && tok0 + tok < sees[r];
                 acc[r][d] = vis ? x : acc[r][d];

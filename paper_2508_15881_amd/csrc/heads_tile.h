@@ -5,12 +5,13 @@
 
 namespace tpla {
 
-// Place of the 16-byte pieces of row `tok` within the row: piece c lies at c ^ heads_swz(tok).  Rows of 256 bytes begin at the same bank, so
-// that the four rows of a transposing read must differ by two pieces at least, and the eight of a row-wise one by one; rows of 128 bytes
-// alternate between the halves of the banks.
+// Place of the 16-byte pieces of row `tok` within the row: piece c lies at c ^ heads_swz(tok).  Row-wise reads (ds_read_b128: 16 tokens at one piece) run in groups
+// of 16 lanes that take tokens 0-3 and 12-15 at one piece and 4-11 at the next one; transposing reads (ds_read_b64_tr_b16) in groups of 8 tokens
+// at a pair of pieces.  Rows of 128 bytes alternate between the halves of the banks, tok & 7 is right for both.  Rows of 256 bytes all begin at the
+// same bank: bits 1 to 3 of the swizzle have to tell 8 tokens apart, and all four, with the shift of the group above, 16.
 template <int RC>
 __device__ __forceinline__ int heads_swz(int tok) {
-  if constexpr (RC == 16) return ((tok & 3) << 1) | ((tok >> 2) & 1) | (tok & 8);
+  if constexpr (RC == 16) return ((tok & 3) << 1) | ((tok >> 2) & 1) | ((((tok >> 2) ^ (tok >> 3)) & 1) << 3);
   return tok & 7;
 }
 
@@ -23,6 +24,70 @@ __device__ __forceinline__ int lds_read_page(const int* at) {
 template <int N>
 __device__ __forceinline__ void loads_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// A page id on its way: wait with lds_wait_id before it is used.
+__device__ __forceinline__ void lds_request_page(int& id, const int* at) {
+  asm volatile("ds_read_b32 %0, %1" : "=v"(id) : "v"(lds_at(reinterpret_cast<const char*>(at))) : "memory");
+}
+
+// ---- output accumulators in registers of our choice ----
+// Quad N is a[4 N : 4 N + 3].  Left to the compiler the accumulators exist twice: a branch may rescale them, and it copies them for every tile so
+// that the branch finds them in other registers (16384 tokens, 64 of them: 2870 us).  So the output product and what else touches them are
+// written out, with the wait states that the compiler then does not insert: 2 between an ordinary write and a matrix instruction that reads
+// it, 11 (here 18) between a matrix instruction and an ordinary one that touches its result.  out_keep() stands at every step of a loop: nothing
+// of the compiler's may live in these registers across it.
+__device__ __forceinline__ void out_keep() {
+#ifdef __HIP_DEVICE_COMPILE__                         // (the host's compiler does not know the names)
+  asm volatile("" : : : "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", "a10", "a11", "a12", "a13", "a14", "a15", "a16", "a17", "a18", "a19", "a20",
+               "a21", "a22", "a23", "a24", "a25", "a26", "a27", "a28", "a29", "a30", "a31", "a32", "a33", "a34", "a35", "a36", "a37", "a38", "a39", "a40", "a41",
+               "a42", "a43", "a44", "a45", "a46", "a47", "a48", "a49", "a50", "a51", "a52", "a53", "a54", "a55", "a56", "a57", "a58", "a59", "a60", "a61", "a62",
+               "a63");
+#endif
+}
+// The scores' products too: the compiler would take accumulation registers for their results, these among them.
+__device__ __forceinline__ void score_first(f32x4& s, const bf16x8& k, const bf16x8& q) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+}
+__device__ __forceinline__ void score_more(f32x4& s, const bf16x8& k, const bf16x8& q) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+}
+template <int N>
+__device__ __forceinline__ void out_product(const u32x4& v, const bf16x8& p) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 a[%2:%3], %0, %1, a[%2:%3]" : : "v"(v), "v"(p), "n"(4 * N), "n"(4 * N + 3));
+}
+// The weights are in place: what follows multiplies with them.
+__device__ __forceinline__ void settle_weights(bf16x8& p) { asm volatile("s_nop 1" : "+v"(p) : : "memory"); }
+__device__ __forceinline__ void settle_scores(f32x4& s) { asm volatile("" : "+v"(s)); }
+__device__ __forceinline__ void out_settle_write() { asm volatile("s_nop 1" ::: "memory"); }
+__device__ __forceinline__ void out_settle_result() { asm volatile("s_nop 15\n\ts_nop 1" ::: "memory"); }
+template <int A>
+__device__ __forceinline__ float out_read_one() {
+  float x;
+  asm volatile("v_accvgpr_read_b32 %0, a[%1]" : "=v"(x) : "n"(A));
+  return x;
+}
+template <int N>
+__device__ __forceinline__ f32x4 out_read() {
+  const float x = out_read_one<4 * N>(), y = out_read_one<4 * N + 1>(), z = out_read_one<4 * N + 2>(), w = out_read_one<4 * N + 3>();
+  return f32x4{x, y, z, w};
+}
+template <int N>
+__device__ __forceinline__ void out_write(f32x4 x) {
+  asm volatile("v_accvgpr_write_b32 a[%4], %0\n\tv_accvgpr_write_b32 a[%5], %1\n\tv_accvgpr_write_b32 a[%6], %2\n\tv_accvgpr_write_b32 a[%7], %3"
+               : : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "n"(4 * N), "n"(4 * N + 1), "n"(4 * N + 2), "n"(4 * N + 3));
+}
+template <int A>
+__device__ __forceinline__ void out_scale_one(float by) {
+  float t;
+  asm volatile("v_accvgpr_read_b32 %0, a[%2]\n\tv_mul_f32 %0, %0, %1\n\tv_accvgpr_write_b32 a[%2], %0" : "=&v"(t) : "v"(by), "n"(A));
+}
+template <int N>
+__device__ __forceinline__ void out_scale(float by) {
+  out_scale_one<4 * N>(by);
+  out_scale_one<4 * N + 1>(by);
+  out_scale_one<4 * N + 2>(by);
+  out_scale_one<4 * N + 3>(by);
 }
 
 // Whether two bfloat16 hold an infinity or a NaN.
