@@ -14,12 +14,13 @@
 namespace tpla {
 
 constexpr int HP_NW = 4, HP_QB = 2, HP_ROWS = HP_NW * HP_QB * 16;
+constexpr int HP_PER_CU = 8 / HP_NW;
 constexpr int HP_NSTAGE = 4;
 constexpr int HP_TILE = 8192;            // bytes of keys, and of values, of a tile
 constexpr int HP_CPT = HP_TILE / 1024 / HP_NW;   // direct loads per wave, of keys and of values
 constexpr int HP_IDS = 1024;             // page ids held at once
 constexpr int HP_ODD = HP_NSTAGE * 2 * HP_TILE + HP_IDS * 4;
-constexpr int HP_LDS = HP_ODD + (HP_NSTAGE + 1) * 4;
+constexpr int HP_LDS = HP_ODD + (HP_NSTAGE + HP_NW) * 4;
 constexpr int HP_CHUNK_MIN = 512;        // tokens of a part of an item at least
 
 // One part of an item: tokens [k0, k1).
@@ -46,41 +47,91 @@ __device__ __forceinline__ PromptSeq prompt_seq(const HeadsArgs& a, int b) {
   s.tiles = (s.it.rows + HP_ROWS - 1) / HP_ROWS;
   return s;
 }
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  return __builtin_amdgcn_readfirstlane(v);
+}
+// Tokens of a part, so that the parts of all items are one round of the workgroups that the chip holds, or two where there are more items than that.
+// (A few more than a round would take as long as two: two sequences, 536 parts of 4352 tokens for 512 workgroups, 217 us; 480 of 5120 REPLACE.)
+__device__ __forceinline__ int prompt_chunk(const HeadsArgs& a, const PromptSeq& front) {
+  const int lane = threadIdx.x & 63;
+  double work = (double)front.tiles * front.it.keys;
+  int tiles = front.tiles;
+  for (int b0 = 64; b0 < a.B; b0 += 64) {
+    const PromptSeq s = prompt_seq(a, b0 + lane);
+    work += (double)s.tiles * s.it.keys;
+    tiles += s.tiles;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+  tiles = wave_total(tiles);
+  const int room = tiles * a.H_kv <= a.n_wg ? a.n_wg : 2 * a.n_wg;
+  const double per = work * a.H_kv / room;
+  if (per >= 1073741824.0) return 0x7fffffff;
+  int chunk = max(((int)per + 63) / 64 * 64, HP_CHUNK_MIN);
+  for (int k = 0; k < 32; ++k) {
+    int units = front.tiles * heads_parts(front.it.keys, chunk);
+    for (int b0 = 64; b0 < a.B; b0 += 64) {
+      const PromptSeq s = prompt_seq(a, b0 + lane);
+      units += s.tiles * heads_parts(s.it.keys, chunk);
+    }
+    if (wave_total(units) * a.H_kv <= room) return __builtin_amdgcn_readfirstlane(chunk);
+    chunk += max(chunk / 32 / 64 * 64, 64);
+  }
+  return 0x7fffffff;
+}
+
+// Lane k gets what the sequence with the k-th largest key has in this lane (ties by index): `from` its lane.  Bit by bit from the top: the sequences that
+// agree with this lane's so far, those of them that are larger by this bit.
+__device__ __forceinline__ int longest_first(int key, int& from) {
+  const int lane = threadIdx.x & 63;
+  int top = key;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = max(top, __shfl_xor(top, d));
+  unsigned long long same = ~0ull;
+  int rank = 0;
+  for (int bit = 31 - __builtin_clz(__builtin_amdgcn_readfirstlane(top) | 1); bit >= 0; --bit) {
+    const bool mine = (key >> bit) & 1;
+    const unsigned long long set = __ballot(mine);
+    rank += mine ? 0 : __popcll(same & set);
+    same &= mine ? set : ~set;
+  }
+  rank += __popcll(same & ((1ull << lane) - 1));
+  from = __builtin_amdgcn_ds_permute(4 * rank, lane);
+  return rank;
+}
+
 // Heads of keys are the fastest index: workgroups go to the XCDs in turn, so each XCD's L2 holds the keys and values of few heads.  PARTS: the work
-// of an item is split; then tiles follow, then parts.  Otherwise the tiles of a sequence go from its last (most keys) to its first.
-// `first_part`: the unit is an item's part 0 and idx counts items alone (the merge).
-template <bool PARTS>
-__device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, bool items_only, PromptUnit& u) {
+// of an item is split; then tiles follow, then parts.  Otherwise whole sequences follow, longest first (in groups of 64), and the tiles of a
+// sequence from its last (most keys) to its first: the grid ends on short items.
+// ITEMS: the unit is an item's part 0 and idx counts items alone (the merge, which finds the chunk in a.plan).
+template <bool PARTS, bool ITEMS>
+__device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, PromptUnit& u) {
   const int lane = threadIdx.x & 63;
   const int kvh = idx % a.H_kv;
   int at = idx / a.H_kv, before = 0;
   const PromptSeq front = prompt_seq(a, lane);
-  int chunk = 0x7fffffff;
-  if constexpr (PARTS) {
-    double work = (double)front.tiles * front.it.keys;
-    for (int b0 = 64; b0 < a.B; b0 += 64) {
-      const PromptSeq s = prompt_seq(a, b0 + lane);
-      work += (double)s.tiles * s.it.keys;
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
-    const double per = ceil(work * a.H_kv / a.n_wg);       // (whole numbers below 2^53)
-    chunk = __builtin_amdgcn_readfirstlane(per < 1073741824.0 ? max(((int)per + 63) / 64 * 64, HP_CHUNK_MIN) : 0x7fffffff);
-  }
+  const int chunk = ITEMS ? a.plan[0] : PARTS ? prompt_chunk(a, front) : 0x7fffffff;
+  if (PARTS && !ITEMS && blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = chunk;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     const PromptSeq s = b0 == 0 ? front : prompt_seq(a, b0 + lane);
     const int parts = PARTS ? heads_parts(s.it.keys, chunk) : 1;
-    const int units = s.tiles * parts, incl = wave_prefix(units);
-    const int count = items_only ? s.tiles : units, count_incl = items_only ? wave_prefix(count) : incl;
+    int units = s.tiles * parts, count = ITEMS ? s.tiles : units, from = lane;
+    if (!PARTS && a.B > 1) {
+      longest_first((s.it.keys >> 5) + (s.tiles > 0 ? 1 : 0), from);
+      units = count = __shfl(count, from);
+    }
+    const int incl = wave_prefix(units), count_incl = ITEMS ? wave_prefix(count) : incl;
     const unsigned long long past = __ballot(count_incl > at);
     if (past == 0) {
       at -= __builtin_amdgcn_readlane(count_incl, 63);
       before += __builtin_amdgcn_readlane(incl, 63);
       continue;
     }
-    const int src = __builtin_ctzll(past);
-    at -= __builtin_amdgcn_readlane(count_incl - count, src);
-    before += __builtin_amdgcn_readlane(incl - units, src);
+    const int place = __builtin_ctzll(past), src = __builtin_amdgcn_readlane(from, place);
+    at -= __builtin_amdgcn_readlane(count_incl - count, place);
+    before += __builtin_amdgcn_readlane(incl - units, place);
     const int tiles = __builtin_amdgcn_readlane(s.tiles, src);
     u.it.b = b0 + src;
     u.it.kvh = kvh;
@@ -103,35 +154,36 @@ __device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, bool it
   return false;
 }
 
-template <int D, bool PARTS>
+// ONE: pages of whole tiles.
+template <int D, bool PARTS, bool ONE>
 __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs a) {
   constexpr int RC = D / 8, TOK = HP_TILE / (2 * D), TB = TOK / 16, KS = D / 32, DB = D / 16, QB = HP_QB;
   constexpr int LOAD_TOK = 64 / RC;
-  static_assert(QB * DB <= 16, "the accumulators are a0 to a63");
+  static_assert(QB * DB <= 16, "accumulators of 64 registers");
   extern __shared__ u32x4 smem[];
   char* const lds = reinterpret_cast<char*>(smem);
   int* const ids = reinterpret_cast<int*>(lds + HP_NSTAGE * 2 * HP_TILE);
   int* const odd_tile = reinterpret_cast<int*>(lds + HP_ODD);      // 1 + the last tile of each place that holds values that are not finite
-  int* const first_hole = odd_tile + HP_NSTAGE;                     // first page of those in ids that is missing
+  int* const first_hole = odd_tile + HP_NSTAGE;                     // of the ids that each wave has read, the first page that is missing
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j16 = lane & 15, q4 = lane >> 4;
   PromptUnit u;
-  if (!prompt_unit<PARTS>(a, blockIdx.x, false, u)) return;
+  if (!prompt_unit<PARTS, false>(a, blockIdx.x, u)) return;
   const HeadsItem it = u.it;
   const int keys = it.keys;
   if (tid < HP_NSTAGE) odd_tile[tid] = 0;
 
   // ---- per-lane places ----
-  unsigned ld_at[HP_CPT], k_at[KS], v_at[DB];
+  unsigned ld_at[HP_CPT];
 #pragma unroll
   for (int j = 0; j < HP_CPT; ++j) {
     const int tok = (wave + j * HP_NW) * LOAD_TOK + lane / RC;      // the piece of the row that this lane loads, and the row within the load
-    ld_at[j] = (unsigned)((lane / RC) * (2 * D) + ((lane % RC) ^ heads_swz<RC>(tok)) * 16);
+    ld_at[j] = (unsigned)((ONE ? tok : lane / RC) * (2 * D) + ((lane % RC) ^ heads_swz<RC>(tok)) * 16);
   }
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) k_at[ks] = (j16 * RC + ((4 * ks + q4) ^ heads_swz<RC>(j16))) * 16;
+  // Rows begin at whole 128 bytes and places at whole 16 KB, so pieces of a row differ in a few address bits alone: k-step ks of the keys is at ks << 6,
+  // block d of the values at d << 5 of the first one's.
+  const unsigned k_at = (unsigned)((j16 * RC + (q4 ^ heads_swz<RC>(j16))) * 16);
   const int v_tok = 4 * q4 + (j16 >> 2);
-#pragma unroll
-  for (int d = 0; d < DB; ++d) v_at[d] = HP_TILE + (v_tok * RC + ((2 * d + ((j16 & 3) >> 1)) ^ heads_swz<RC>(v_tok))) * 16 + (j16 & 1) * 8;
+  const unsigned v_at = (unsigned)(HP_TILE + (v_tok * RC + (((j16 & 3) >> 1) ^ heads_swz<RC>(v_tok))) * 16 + (j16 & 1) * 8);
   const unsigned lds_base = lds_at(lds);
 
   const int pt = a.page_tokens, shift = (pt & (pt - 1)) == 0 ? __builtin_ctz(pt) : -1;
@@ -142,32 +194,57 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   const char* v_head = static_cast<const char*>(a.v_pool) + (size_t)it.kvh * pt * (2 * D);
   int id0 = 0;
 
-  // Tile t on its way.  A load's tokens lie in one page (of a multiple of 16 tokens); ids: their pages.
-  auto load_tok = [&](int t, int j) { return t * TOK + (wave + j * HP_NW) * LOAD_TOK; };
-  auto issue_whole = [&](int t, const int (&id)[HP_CPT]) {
-    char* dst = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + wave * 1024;
-    size_t at[HP_CPT];
+  // Where a load is: its tokens lie in one page (pages are a multiple of 16 tokens), ONE: those of all loads of a tile do.  Walked from tile to tile
+  // without divisions.
+  constexpr int CURS = ONE ? 1 : HP_CPT;
+  auto load_tok = [&](int t, int j) { return t * TOK + (ONE ? 0 : (wave + j * HP_NW) * LOAD_TOK); };
+  struct Cursor {
+    int page, off;
+  };
+  Cursor cur[CURS];
+  const int step_pages = TOK / pt, step_off = TOK % pt;
+  auto seek = [&](int t) {
 #pragma unroll
-    for (int j = 0; j < HP_CPT; ++j) {
+    for (int j = 0; j < CURS; ++j) {
       const int tok = load_tok(t, j);
-      at[j] = (size_t)(unsigned)max(__builtin_amdgcn_readfirstlane(id[j]), 0) * page_bytes + (size_t)(tok - page_of(tok) * pt) * (2 * D);
+      cur[j].page = page_of(tok);
+      cur[j].off = tok - cur[j].page * pt;
     }
+  };
+  auto advance = [&]() {
+#pragma unroll
+    for (int j = 0; j < CURS; ++j) {
+      cur[j].page += step_pages;
+      cur[j].off += step_off;
+      if (cur[j].off >= pt) {
+        cur[j].off -= pt;
+        ++cur[j].page;
+      }
+    }
+  };
+  // Tile t on its way, all of its tokens exist; id: its loads' pages, where the cursors are.
+  auto issue_whole = [&](int t, const int (&id)[CURS]) {
+    char* dst = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + wave * 1024;
+    size_t at[CURS];
+#pragma unroll
+    for (int j = 0; j < CURS; ++j) at[j] = (unsigned)max(__builtin_amdgcn_readfirstlane(id[j]), 0) * page_bytes + (size_t)(unsigned)cur[j].off * (2 * D);
 #pragma unroll
     for (int j = 0; j < HP_CPT; ++j)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k_head + at[j] + ld_at[j]),
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k_head + at[j % CURS] + ld_at[j]),
                                        (__attribute__((address_space(3))) void*)(dst + j * HP_NW * 1024), 16, 0, 0);
 #pragma unroll
     for (int j = 0; j < HP_CPT; ++j)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v_head + at[j] + ld_at[j]),
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v_head + at[j % CURS] + ld_at[j]),
                                        (__attribute__((address_space(3))) void*)(dst + HP_TILE + j * HP_NW * 1024), 16, 0, 0);
   };
   // Tokens past the end repeat the last one, those of missing pages are page 0's; they are masked, and their values zeroed.
   auto issue = [&](int t) {
     if ((t + 1) * TOK <= keys) {
-      int id[HP_CPT];
+      int id[CURS];
 #pragma unroll
-      for (int j = 0; j < HP_CPT; ++j) id[j] = lds_read_page(ids + (page_of(load_tok(t, j)) - id0));
+      for (int j = 0; j < CURS; ++j) id[j] = lds_read_page(ids + (cur[j].page - id0));
       issue_whole(t, id);
+      advance();
       return;
     }
     char* dst = lds + (t % HP_NSTAGE) * (2 * HP_TILE) + wave * 1024;
@@ -184,10 +261,8 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   };
   // The tile t is there, its own loads of the next two tiles may be on their way.
   auto arrived = [&](int t, int c1) {
-    if (t + 2 < c1)
-      loads_wait<2 * 2 * HP_CPT>();
-    else if (t + 1 < c1)
-      loads_wait<2 * HP_CPT>();
+    if (t + HP_NSTAGE - 2 < c1)
+      loads_wait<(HP_NSTAGE - 2) * 2 * HP_CPT>();
     else
       loads_wait<0>();
   };
@@ -210,6 +285,9 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   int seen[QB];
 #pragma unroll
   for (int r = 0; r < QB; ++r) {
+    const bf16_t* src = static_cast<const bf16_t*>(a.q) + out_row(min(row_w + 16 * r + j16, it.rows - 1)) * D + 8 * q4;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[r][ks] = *reinterpret_cast<const bf16x8*>(src + 32 * ks);
     m[r] = -INFINITY;
     l[r] = 0.f;
     seen[r] = 0;
@@ -217,18 +295,30 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   out_keep();
   static_for<QB * DB>([&](auto ic) { out_write<decltype(ic)::value>(f32x4{0.f, 0.f, 0.f, 0.f}); });
 
-  // ---- one tile.  CUT: some of its tokens are not seen by some rows; there: its blocks of 16 tokens that have a page ----
-  auto tile_body = [&](int t, int there, auto cut_tag) {
-    constexpr bool CUT = decltype(cut_tag)::value;
+  // The rare step: a score above the reference by more than LAZY.  top: largest score of this lane, in powers of two.
+  auto raise = [&](auto rc, float top) {
+    constexpr int r = decltype(rc)::value;
+    top = fmaxf(top, lane_xor<16>(top, lane));
+    top = fmaxf(top, lane_xor<32>(top, lane));
+    const float m_new = fmaxf(m[r], top);
+    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[r] - m_new);
+    l[r] *= alpha;
+    m[r] = m_new;
+    out_settle_result();
+    static_for<DB>([&](auto dc) { out_scale<r * DB + decltype(dc)::value>(alpha); });
+  };
+
+  // ---- a tile that some rows do not see whole; there: its blocks of 16 tokens that have a page ----
+  auto cut_tile = [&](int t, int there) {
     const int tok0 = t * TOK;
-    const unsigned base = lds_base + (unsigned)((t % HP_NSTAGE) * (2 * HP_TILE));
+    const unsigned base = lds_base + (unsigned)((t % HP_NSTAGE) * (2 * HP_TILE)), kb = base + k_at, vb = base + v_at;
     f32x4 s[QB][TB];
     {
       constexpr int N = KS * TB, AHEAD = D == 128 ? 8 : 4;
       bf16x8 kf[AHEAD];
       static_for<AHEAD>([&](auto ic) {
         constexpr int x = decltype(ic)::value;
-        lds_read_b128<(x % TB) * (16 * RC * 16)>(kf[x], base + k_at[x / TB]);
+        lds_read_b128<(x % TB) * (16 * RC * 16)>(kf[x], kb ^ ((x / TB) << 6));
       });
       static_for<N>([&](auto ic) {
         constexpr int x = decltype(ic)::value, ks = x / TB, n = x % TB;
@@ -240,18 +330,16 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
           else
             score_more(s[r][n], kf[x % AHEAD], q[r][ks]);
         }
-        if constexpr (x + AHEAD < N) lds_read_b128<((x + AHEAD) % TB) * (16 * RC * 16)>(kf[x % AHEAD], base + k_at[(x + AHEAD) / TB]);
+        if constexpr (x + AHEAD < N) lds_read_b128<((x + AHEAD) % TB) * (16 * RC * 16)>(kf[x % AHEAD], kb ^ (((x + AHEAD) / TB) << 6));
       });
     }
-    // the first values start now, so that their way from LDS passes under the softmax
     constexpr int NV = DB * (TB / 2), VA = 4;
     u32x2 lo[VA], hi[VA];
     auto value = [&](auto yc) {
       constexpr int y = decltype(yc)::value;
-      lds_read_tr_b64<(y / DB) * (32 * RC * 16)>(lo[y % VA], base + v_at[y % DB]);
-      lds_read_tr_b64<(y / DB) * (32 * RC * 16) + 16 * RC * 16>(hi[y % VA], base + v_at[y % DB]);
+      lds_read_tr_b64<(y / DB) * (32 * RC * 16)>(lo[y % VA], vb ^ ((y % DB) << 5));
+      lds_read_tr_b64<(y / DB) * (32 * RC * 16) + 16 * RC * 16>(hi[y % VA], vb ^ ((y % DB) << 5));
     };
-    if constexpr (!CUT) static_for<VA>([&](auto ic) { value(ic); });
     out_settle_result();
 #pragma unroll
     for (int r = 0; r < QB; ++r)
@@ -261,15 +349,12 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
     bf16x8 p[QB][TB / 2];
     static_for<QB>([&](auto rc) {
       constexpr int r = decltype(rc)::value;
-      if constexpr (CUT) {
 #pragma unroll
-        for (int n = 0; n < TB; ++n)
+      for (int n = 0; n < TB; ++n) {
+        const int left = ((there >> n) & 1) ? sees[r] - tok0 - 16 * n - 4 * q4 : 0;
+        seen[r] |= left > 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool vis = ((there >> n) & 1) && tok0 + 16 * n + 4 * q4 + i < sees[r];
-            seen[r] |= vis;
-            if (!vis) s[r][n][i] = -INFINITY;
-          }
+        for (int i = 0; i < 4; ++i) s[r][n][i] = i < left ? s[r][n][i] : -INFINITY;
       }
       float top = s[r][0][0];
 #pragma unroll
@@ -277,16 +362,7 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][n][i]);
       top *= a.scale_log2;
-      if (__any(top > m[r] + LAZY)) {
-        top = fmaxf(top, lane_xor<16>(top, lane));
-        top = fmaxf(top, lane_xor<32>(top, lane));
-        const float m_new = fmaxf(m[r], top);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[r] - m_new);
-        l[r] *= alpha;
-        m[r] = m_new;
-        out_settle_result();
-        static_for<DB>([&](auto dc) { out_scale<r * DB + decltype(dc)::value>(alpha); });
-      }
+      if (__any(top > m[r] + LAZY)) raise(rc, top);
       const float ref = m[r] == -INFINITY ? 0.f : m[r];
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -304,10 +380,9 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
     for (int r = 0; r < QB; ++r)
 #pragma unroll
       for (int h = 0; h < TB / 2; ++h) settle_weights(p[r][h]);
-    bool odd = false;
-    if constexpr (CUT) odd = __builtin_amdgcn_readfirstlane(lds_read_page(odd_tile + t % HP_NSTAGE)) == t + 1;
+    const bool odd = __builtin_amdgcn_readfirstlane(lds_read_page(odd_tile + t % HP_NSTAGE)) == t + 1;
     if (!odd) {
-      if constexpr (CUT) static_for<VA>([&](auto ic) { value(ic); });
+      static_for<VA>([&](auto ic) { value(ic); });
       static_for<NV>([&](auto ic) {
         constexpr int x = decltype(ic)::value, d = x % DB, h = x / DB, ahead = NV - 1 - x < VA - 1 ? NV - 1 - x : VA - 1;
         lds_wait<2 * ahead>(lo[x % VA], hi[x % VA]);
@@ -326,8 +401,8 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
         static_for<DB>([&](auto dc) {
           constexpr int d = decltype(dc)::value;
           u32x2 vlo, vhi;
-          lds_read_tr_b64<0>(vlo, base + v_at[d] + h * (32 * RC * 16));
-          lds_read_tr_b64<16 * RC * 16>(vhi, base + v_at[d] + h * (32 * RC * 16));
+          lds_read_tr_b64<0>(vlo, (vb ^ (d << 5)) + h * (32 * RC * 16));
+          lds_read_tr_b64<16 * RC * 16>(vhi, (vb ^ (d << 5)) + h * (32 * RC * 16));
           lds_wait<0>(vlo, vhi);
           bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{vlo[0], vlo[1], vhi[0], vhi[1]} & keep);
           settle_weights(v);
@@ -352,44 +427,114 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
     }
   };
 
+  // ---- a tile that all rows of the workgroup see ----
+  auto plain_tile = [&](int t) {
+    constexpr int NS = KS * TB, NV = DB * (TB / 2), VA = 4;
+    const unsigned base = lds_base + (unsigned)((t % HP_NSTAGE) * (2 * HP_TILE)), kb = base + k_at, vb = base + v_at;
+    f32x4 s[QB][TB];
+    bf16x8 kf[NS], p[QB][TB / 2];
+    u32x2 lo[VA], hi[VA];
+    static_for<NS>([&](auto ic) {
+      constexpr int x = decltype(ic)::value;
+      lds_read_b128<(x % TB) * (16 * RC * 16)>(kf[x], kb ^ ((x / TB) << 6));
+    });
+    static_for<NS>([&](auto ic) {
+      constexpr int x = decltype(ic)::value, ks = x / TB, n = x % TB;
+      lds_wait<NS - 1 - x>(kf[x]);
+#pragma unroll
+      for (int r = 0; r < QB; ++r) {
+        if constexpr (ks == 0)
+          score_first(s[r][n], kf[x], q[r][ks]);
+        else
+          score_more(s[r][n], kf[x], q[r][ks]);
+      }
+    });
+    // the first values start now, so that their way from LDS passes under the softmax
+    auto value = [&](auto yc) {
+      constexpr int y = decltype(yc)::value;
+      lds_read_tr_b64<(y / DB) * (32 * RC * 16)>(lo[y % VA], vb ^ ((y % DB) << 5));
+      lds_read_tr_b64<(y / DB) * (32 * RC * 16) + 16 * RC * 16>(hi[y % VA], vb ^ ((y % DB) << 5));
+    };
+    static_for<VA>([&](auto ic) { value(ic); });
+    out_settle_write();
+    out_settle_write();
+#pragma unroll
+    for (int r = 0; r < QB; ++r)
+#pragma unroll
+      for (int n = 0; n < TB; ++n) settle_scores(s[r][n]);
+    static_for<QB>([&](auto rc) {
+      constexpr int r = decltype(rc)::value;
+      float top = s[r][0][0];
+#pragma unroll
+      for (int n = 0; n < TB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][n][i]);
+      top *= a.scale_log2;
+      if (__any(top > m[r] + LAZY)) raise(rc, top);
+      const float ref = m[r] == -INFINITY ? 0.f : m[r];
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int n = 0; n < TB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[r][n][i], a.scale_log2, -ref));
+          sum[i] += e;
+          p[r][n / 2][4 * (n & 1) + i] = (bf16_t)e;
+        }
+      l[r] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    });
+#pragma unroll
+    for (int r = 0; r < QB; ++r)
+#pragma unroll
+      for (int h = 0; h < TB / 2; ++h) settle_weights(p[r][h]);
+    static_for<NV>([&](auto ic) {
+      constexpr int x = decltype(ic)::value, d = x % DB, h = x / DB, ahead = NV - 1 - x < VA - 1 ? NV - 1 - x : VA - 1;
+      lds_wait<2 * ahead>(lo[x % VA], hi[x % VA]);
+      const u32x4 v = {lo[x % VA][0], lo[x % VA][1], hi[x % VA][0], hi[x % VA][1]};
+      static_for<QB>([&](auto rc) { out_product<decltype(rc)::value * DB + d>(v, p[decltype(rc)::value][h]); });
+      if constexpr (x + VA < NV) value(std::integral_constant<int, x + VA>{});
+    });
+  };
+
   const int t0 = u.k0 / TOK, t1 = (u.k1 + TOK - 1) / TOK;
   const int id_tiles = (int)min(max((long long)(HP_IDS - 1) * pt / TOK, 1ll), 1ll << 26);           // tiles whose pages fit in ids, wherever in a page they begin
   for (int c0 = t0; c0 < t1; c0 += id_tiles) {
     const int c1 = min(t1, c0 + id_tiles);
-    __syncthreads();
+    if (c0 > t0) __syncthreads();                      // the ids and tiles before are read
     id0 = page_of(c0 * TOK);
-    if (tid == 0) *first_hole = 0x7fffffff;
-    __syncthreads();
+    int missing = 0x7fffffff;
     for (int x = tid; x < HP_IDS; x += HP_NW * 64) {
       const int p = id0 + x;
       if (p < a.max_pages && (long long)p * pt < (long long)min(keys, c1 * TOK)) {
         const int id = table[p];
         ids[x] = id;
-        if (id < 0) atomicMin(first_hole, p);
+        if (id < 0) missing = min(missing, p);
       }
     }
+    if (__any(missing != 0x7fffffff))
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) missing = min(missing, __shfl_xor(missing, d));
+    if (lane == 0) first_hole[wave] = missing;
     __syncthreads();
     // tiles that exist whole and that every row of the workgroup sees
-    const int hole = __builtin_amdgcn_readfirstlane(*first_hole), plain = hole == 0x7fffffff ? least : min(least, hole * pt);
+    int hole = first_hole[0];
+#pragma unroll
+    for (int w = 1; w < HP_NW; ++w) hole = min(hole, first_hole[w]);
+    hole = __builtin_amdgcn_readfirstlane(hole);
+    const int plain = hole == 0x7fffffff ? least : min(least, hole * pt);
     const int whole = min(c1, max(c0, plain / TOK));
+    seek(c0);
     for (int t = c0; t < min(c1, c0 + HP_NSTAGE - 1); ++t) issue(t);
-    if (c0 == t0) {
 #pragma unroll
-      for (int r = 0; r < QB; ++r)
+    for (int r = 0; r < QB; ++r)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          q[r][ks] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.q) + out_row(min(row_w + 16 * r + j16, it.rows - 1)) * D + 32 * ks + 8 * q4);
-#pragma unroll
-      for (int r = 0; r < QB; ++r)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[r][ks]));       // complete before the loop
-    }
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[r][ks]));         // complete before the loop (and on every path to it: a wait within would be for the tiles)
     int t = c0;
     // the page ids of the tile that is requested next, read a tile ahead
     const int last_id = page_of(max(min(keys, c1 * TOK) - 1, 0)) - id0;
-    int id[HP_CPT];
+    int id[CURS];
 #pragma unroll
-    for (int j = 0; j < HP_CPT; ++j) id[j] = lds_read_page(ids + min(page_of(load_tok(t + HP_NSTAGE - 1, j)) - id0, last_id));
+    for (int j = 0; j < CURS; ++j) id[j] = lds_read_page(ids + min(cur[j].page - id0, last_id));
     for (; t < whole; ++t) {
       out_keep();
       arrived(t, c1);
@@ -397,18 +542,20 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
       asm volatile("" ::: "memory");
       const int next = t + HP_NSTAGE - 1;
       if (next < c1) {
-        if ((next + 1) * TOK <= keys)
+        if ((next + 1) * TOK <= keys) {
           issue_whole(next, id);
-        else
+          advance();
+        } else {
           issue(next);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < HP_CPT; ++j) lds_request_page(id[j], ids + min(page_of(load_tok(next + 1, j)) - id0, last_id));
-      if (alive) tile_body(t, 0, std::false_type{});
+      for (int j = 0; j < CURS; ++j) lds_request_page(id[j], ids + min(cur[j].page - id0, last_id));
+      plain_tile(t);
 #pragma unroll
-      for (int j = 0; j < HP_CPT; ++j) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(id[j]) : : "memory");      // (long there)
+      for (int j = 0; j < CURS; ++j) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(id[j]) : : "memory");      // (long there)
     }
-    if (whole > t0) seen[0] = seen[1] = 1;
+    if (t > c0) seen[0] = seen[1] = 1;
     for (; t < c1; ++t) {
       out_keep();
       arrived(t, c1);
@@ -435,7 +582,7 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
       asm volatile("" ::: "memory");
       if (t + HP_NSTAGE - 1 < c1) issue(t + HP_NSTAGE - 1);
       if (tok0 >= most) continue;                      // (the wave's rows see none of it; the barriers above are still reached)
-      tile_body(t, there, std::true_type{});
+      cut_tile(t, there);
     }
   }
   if (!alive) return;
@@ -478,7 +625,7 @@ template <int D>
 __global__ void __launch_bounds__(256) heads_prompts_merge_kernel(HeadsArgs a) {
   constexpr int LPR = D / 4, AT_ONCE = 256 / LPR;
   PromptUnit u;
-  if (!prompt_unit<true>(a, blockIdx.x, true, u) || u.parts == 1) return;
+  if (!prompt_unit<true, true>(a, blockIdx.x, u) || u.parts == 1) return;
   const int r = blockIdx.y * AT_ONCE + threadIdx.x / LPR, c = 4 * (threadIdx.x % LPR), row = u.it.row0 + r;
   if (row >= u.it.rows) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
@@ -507,24 +654,29 @@ HeadsPlan heads_prompts_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
   p.rows = HP_ROWS;
   p.items = prompts_items(sh, T);
   p.tiles = (int)(p.items / sh.H_kv);
-  p.n_wg = 2 * device_cu_count();                      // workgroups that the chip holds
+  p.n_wg = HP_PER_CU * device_cu_count();                      // workgroups that the chip holds
   // Split where the items do not fill it twice and there are tokens to split.
   p.n_splits = p.items < 2 * p.n_wg && (int64_t)max_pages * sh.page_tokens > HP_CHUNK_MIN ? 2 : 1;
-  p.slots = p.n_splits > 1 ? p.items + p.n_wg : 0;     // (the parts of an item: what it reads over the chunk's length, rounded up)
-  p.workspace = (size_t)p.slots * p.rows * (sh.d_v + 2) * sizeof(float);
+  p.slots = p.n_splits > 1 ? (p.items <= p.n_wg ? 1 : 2) * (int64_t)p.n_wg : 0;        // (see prompt_chunk)
+  p.workspace = p.slots > 0 ? (size_t)p.slots * p.rows * (sh.d_v + 2) * sizeof(float) + 16 : 0;
   return p;
 }
 
 size_t heads_prompts_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages) {
   if ((int64_t)max_pages * sh.page_tokens <= HP_CHUNK_MIN) return 0;
-  const int64_t n_wg = 2 * device_cu_count();
-  return (size_t)(std::min(prompts_items(sh, T), 2 * n_wg) + n_wg) * HP_ROWS * (sh.d_v + 2) * sizeof(float);
+  const int64_t n_wg = HP_PER_CU * device_cu_count();
+  return (size_t)((prompts_items(sh, T) <= n_wg ? 1 : 2) * n_wg) * HP_ROWS * (sh.d_v + 2) * sizeof(float) + 16;
+}
+
+template <int D>
+static auto prompts_kernel_of(bool parts, bool one) -> void (*)(HeadsArgs) {
+  return parts ? (one ? heads_prompts_kernel<D, true, true> : heads_prompts_kernel<D, true, false>)
+               : (one ? heads_prompts_kernel<D, false, true> : heads_prompts_kernel<D, false, false>);
 }
 
 int launch_heads_prompts(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st) {
-  const bool parts = p.n_splits > 1;
-  void (*fn)(HeadsArgs) = a.d_k == 128 ? (parts ? heads_prompts_kernel<128, true> : heads_prompts_kernel<128, false>)
-                                       : (parts ? heads_prompts_kernel<64, true> : heads_prompts_kernel<64, false>);
+  const bool parts = p.n_splits > 1, one = a.page_tokens % (HP_TILE / (2 * a.d_k)) == 0;
+  void (*fn)(HeadsArgs) = a.d_k == 128 ? prompts_kernel_of<128>(parts, one) : prompts_kernel_of<64>(parts, one);
   int rc = allow_lds(reinterpret_cast<const void*>(fn), HP_LDS, "heads_prompts_kernel");
   if (rc) return rc;
   hipLaunchKernelGGL(fn, dim3((unsigned)(parts ? p.slots : p.items)), dim3(HP_NW * 64), HP_LDS, st, a);

@@ -32,20 +32,21 @@ __device__ __forceinline__ void lds_request_page(int& id, const int* at) {
 }
 
 // ---- output accumulators in registers of our choice ----
-// Quad N is a[4 N : 4 N + 3].  Left to the compiler the accumulators exist twice: a branch may rescale them, and it copies them for every tile so
-// that the branch finds them in other registers (16384 tokens, 64 of them: 2870 us).  So the output product and what else touches them are
-// written out, with the wait states that the compiler then does not insert: 2 between an ordinary write and a matrix instruction that reads
-// it, 11 (here 18) between a matrix instruction and an ordinary one that touches its result.  out_keep() stands at every step of a loop: nothing
-// of the compiler's may live in these registers across it.
+// Quad N is v[192 + 4 N : 195 + 4 N], N < 16: the top of the 256 that two waves per SIMD leave each.  Left to the compiler the accumulators exist twice: a
+// branch may rescale them, and it copies them for every tile so that the branch finds them in other registers (16384 tokens, 64 of them: 2870 us).
+// So the products and what else touches them are written out, with the wait states that the compiler then does not insert: 2 between an ordinary
+// write and a matrix instruction that reads it, 11 (here 18) between a matrix instruction and an ordinary one that touches its result.  (Not
+// accumulation registers: a kernel that names those gets half of its registers of that kind, and spills.)  out_keep() stands at every step of a loop:
+// nothing of the compiler's may live in these registers across it.
+constexpr int OUT0 = 192;
 __device__ __forceinline__ void out_keep() {
 #ifdef __HIP_DEVICE_COMPILE__                         // (the host's compiler does not know the names)
-  asm volatile("" : : : "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", "a10", "a11", "a12", "a13", "a14", "a15", "a16", "a17", "a18", "a19", "a20",
-               "a21", "a22", "a23", "a24", "a25", "a26", "a27", "a28", "a29", "a30", "a31", "a32", "a33", "a34", "a35", "a36", "a37", "a38", "a39", "a40", "a41",
-               "a42", "a43", "a44", "a45", "a46", "a47", "a48", "a49", "a50", "a51", "a52", "a53", "a54", "a55", "a56", "a57", "a58", "a59", "a60", "a61", "a62",
-               "a63");
+  asm volatile("" : : : "v192", "v193", "v194", "v195", "v196", "v197", "v198", "v199", "v200", "v201", "v202", "v203", "v204", "v205", "v206", "v207", "v208", "v209",
+               "v210", "v211", "v212", "v213", "v214", "v215", "v216", "v217", "v218", "v219", "v220", "v221", "v222", "v223", "v224", "v225", "v226", "v227",
+               "v228", "v229", "v230", "v231", "v232", "v233", "v234", "v235", "v236", "v237", "v238", "v239", "v240", "v241", "v242", "v243", "v244", "v245",
+               "v246", "v247", "v248", "v249", "v250", "v251", "v252", "v253", "v254", "v255");
 #endif
 }
-// The scores' products too: the compiler would take accumulation registers for their results, these among them.
 __device__ __forceinline__ void score_first(f32x4& s, const bf16x8& k, const bf16x8& q) {
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
 }
@@ -54,7 +55,7 @@ __device__ __forceinline__ void score_more(f32x4& s, const bf16x8& k, const bf16
 }
 template <int N>
 __device__ __forceinline__ void out_product(const u32x4& v, const bf16x8& p) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 a[%2:%3], %0, %1, a[%2:%3]" : : "v"(v), "v"(p), "n"(4 * N), "n"(4 * N + 3));
+  asm volatile("v_mfma_f32_16x16x32_bf16 v[%2:%3], %0, %1, v[%2:%3]" : : "v"(v), "v"(p), "n"(OUT0 + 4 * N), "n"(OUT0 + 4 * N + 3));
 }
 // The weights are in place: what follows multiplies with them.
 __device__ __forceinline__ void settle_weights(bf16x8& p) { asm volatile("s_nop 1" : "+v"(p) : : "memory"); }
@@ -64,7 +65,7 @@ __device__ __forceinline__ void out_settle_result() { asm volatile("s_nop 15\n\t
 template <int A>
 __device__ __forceinline__ float out_read_one() {
   float x;
-  asm volatile("v_accvgpr_read_b32 %0, a[%1]" : "=v"(x) : "n"(A));
+  asm volatile("v_mov_b32 %0, v[%1]" : "=v"(x) : "n"(OUT0 + A));
   return x;
 }
 template <int N>
@@ -74,20 +75,15 @@ __device__ __forceinline__ f32x4 out_read() {
 }
 template <int N>
 __device__ __forceinline__ void out_write(f32x4 x) {
-  asm volatile("v_accvgpr_write_b32 a[%4], %0\n\tv_accvgpr_write_b32 a[%5], %1\n\tv_accvgpr_write_b32 a[%6], %2\n\tv_accvgpr_write_b32 a[%7], %3"
-               : : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "n"(4 * N), "n"(4 * N + 1), "n"(4 * N + 2), "n"(4 * N + 3));
-}
-template <int A>
-__device__ __forceinline__ void out_scale_one(float by) {
-  float t;
-  asm volatile("v_accvgpr_read_b32 %0, a[%2]\n\tv_mul_f32 %0, %0, %1\n\tv_accvgpr_write_b32 a[%2], %0" : "=&v"(t) : "v"(by), "n"(A));
+  constexpr int A = OUT0 + 4 * N;
+  asm volatile("v_mov_b32 v[%4], %0\n\tv_mov_b32 v[%5], %1\n\tv_mov_b32 v[%6], %2\n\tv_mov_b32 v[%7], %3"
+               : : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "n"(A), "n"(A + 1), "n"(A + 2), "n"(A + 3));
 }
 template <int N>
 __device__ __forceinline__ void out_scale(float by) {
-  out_scale_one<4 * N>(by);
-  out_scale_one<4 * N + 1>(by);
-  out_scale_one<4 * N + 2>(by);
-  out_scale_one<4 * N + 3>(by);
+  constexpr int A = OUT0 + 4 * N;
+  asm volatile("v_mul_f32 v[%1], v[%1], %0\n\tv_mul_f32 v[%2], v[%2], %0\n\tv_mul_f32 v[%3], v[%3], %0\n\tv_mul_f32 v[%4], v[%4], %0"
+               : : "v"(by), "n"(A), "n"(A + 1), "n"(A + 2), "n"(A + 3));
 }
 
 // Whether two bfloat16 hold an infinity or a NaN.

@@ -8,7 +8,7 @@ import test_isa_tree_results as results
 from paper_2508_15881_amd import build as b
 from test_isa_tree_waits import parse, touched_too_early
 
-INSTANCES = {"heads_ranges": 6, "heads_prompts": 4}
+INSTANCES = {"heads_ranges": 6, "heads_prompts": 8}
 
 
 @pytest.fixture(scope="module")
@@ -34,11 +34,12 @@ def test_matrix_instructions_have_their_wait_states(assembly):
 
 
 def test_the_accumulation_registers_are_the_kernels_own(assembly):
-    """No instruction of the compiler's touches a0 to a63."""
-    mine = {("a", k) for k in range(64)}
+    """No instruction of the compiler's touches v192 to v255, and there are no accumulation registers."""
+    mine = {("v", k) for k in range(192, 256)}
     for name, (insts, _) in parse(assembly["heads_prompts"], "heads_prompts_kernel").items():
         theirs = [t for t, in_asm in insts if not in_asm and results.registers(t) & mine]
         assert not theirs, (name, theirs[0])
+        assert not any(kind == "a" for t, _ in insts for kind, _ in results.registers(t)), name
 
 
 def test_nothing_of_the_prompt_kernels_is_kept_in_scratch_memory(assembly):
