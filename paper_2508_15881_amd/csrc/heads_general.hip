@@ -11,6 +11,7 @@
 namespace tpla {
 
 constexpr int HG_JOIN_TOK = 64, HG_ROWS_TOK = 32;      // tokens staged at once
+constexpr int HG_SPLIT = 512;                           // tokens of a block-table row from which on it pays to split them
 
 // JOIN: the four waves have the same 16 rows and a quarter of the staged tokens each, and join at the end: few rows.  Otherwise 16 rows each.
 template <int NB, bool JOIN>
@@ -19,7 +20,9 @@ struct GeneralTile {
   static constexpr int TOK = JOIN ? HG_JOIN_TOK : HG_ROWS_TOK;
   static constexpr int ROWS = JOIN ? 16 : 64;
   static constexpr int BLOCKS = JOIN ? 1 : TOK / 16;   // of 16 tokens per wave
-  static constexpr int LDS = (2 * TOK * PITCH + TOK + 4) * 4;
+  static constexpr int PIECES = TOK * (W / 8);         // of 8 columns, of keys and of values
+  static constexpr int PER_THREAD = (PIECES + 255) / 256;
+  static constexpr int LDS = 2 * TOK * PITCH * 4 + 2 * TOK * 8 + 16;
   static_assert(!JOIN || 4 * 16 * (W + 4) <= 2 * TOK * PITCH, "the join uses the staged rows' place");
 };
 
@@ -30,8 +33,8 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
   extern __shared__ __align__(16) float sm[];
   float* const sk = sm;
   float* const sv = sm + TOK * PITCH;
-  int* const there = reinterpret_cast<int*>(sv + TOK * PITCH);      // whether a staged token exists
-  volatile int* const odd = there + TOK;                            // whether some staged value is not finite
+  long long* const rows_at = reinterpret_cast<long long*>(sv + TOK * PITCH);      // [2][TOK]: row of the pools that a token is, -1: none
+  volatile int* const odd = reinterpret_cast<int*>(rows_at + 2 * TOK);            // whether some staged value is not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j16 = lane & 15, q4 = lane >> 4;
   HeadsItem it;
   if (!heads_item<Tile::ROWS>(a, blockIdx.x, it)) return;
@@ -60,36 +63,51 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
   float m = -INFINITY, l = 0.f;
   bool seen = false;
   const int32_t* table = a.table + (size_t)it.b * a.max_pages;
-  const size_t head_at = (size_t)it.kvh * a.page_tokens;
+  // Where the tokens of a tile are is found a tile ahead: one round trip to memory per tile and not two.
+  auto find_rows = [&](int t0, int which) {
+    if (tid >= TOK) return;
+    const int t = t0 + tid, page = t < k1 ? table[t / a.page_tokens] : -1;
+    rows_at[which * TOK + tid] = page < 0 ? -1 : ((long long)page * a.H_kv + it.kvh) * a.page_tokens + t % a.page_tokens;
+  };
+  if (tid == 0) *odd = 0;
+  find_rows(k0, 0);
+  __syncthreads();
 
-  for (int t0 = k0; t0 < k1; t0 += TOK) {
-    if (tid == 0) *odd = 0;
-    __syncthreads();                                   // the tile before is read
-    if (tid < TOK) there[tid] = t0 + tid < k1 && table[(t0 + tid) / a.page_tokens] >= 0;
+  for (int t0 = k0, which = 0; t0 < k1; t0 += TOK, which ^= 1) {
     const bool some_masked = t0 + TOK > least;
-    for (int part = 0; part < 2; ++part) {
-      const int d = part ? a.d_v : a.d_k;
-      const T* pool = static_cast<const T*>(part ? a.v_pool : a.k_pool);
-      float* dst = part ? sv : sk;
-      for (int x = tid; x < TOK * (Tile::W / 8); x += 256) {
-        const int tok = x / (Tile::W / 8), c = 8 * (x % (Tile::W / 8)), t = t0 + tok;
-        Vec8 r;
+    const long long* const at = rows_at + which * TOK;
+    // (columns from d on are zeros, and so are tokens that are none)
+    Vec8 x[2][Tile::PER_THREAD];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r.v[e] = 0.f;
-        if (c < d && t < k1) {
-          const int page = table[t / a.page_tokens];
-          if (page >= 0) r = load8_cached(pool + (((size_t)page * a.H_kv * a.page_tokens + head_at) + t % a.page_tokens) * d + c);
+    for (int part = 0; part < 2; ++part)
+#pragma unroll
+      for (int k = 0; k < Tile::PER_THREAD; ++k) {
+        const int p = tid + 256 * k, tok = p / (Tile::W / 8), c = 8 * (p % (Tile::W / 8)), d = part ? a.d_v : a.d_k;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[part][k].v[e] = 0.f;
+        if (p < Tile::PIECES && c < d) {
+          const long long row = at[tok];
+          if (row >= 0) x[part][k] = load8_cached(static_cast<const T*>(part ? a.v_pool : a.k_pool) + row * d + c);
         }
+      }
+    find_rows(t0 + TOK, which ^ 1);
+#pragma unroll
+    for (int part = 0; part < 2; ++part)
+#pragma unroll
+      for (int k = 0; k < Tile::PER_THREAD; ++k) {
+        const int p = tid + 256 * k, tok = p / (Tile::W / 8), c = 8 * (p % (Tile::W / 8));
+        if (p >= Tile::PIECES) continue;
+        const Vec8& r = x[part][k];
         if (part && some_masked) {
           bool fine = true;
 #pragma unroll
           for (int e = 0; e < 8; ++e) fine = fine && __builtin_isfinite(r.v[e]);
           if (!fine) *odd = 1;
         }
-        *reinterpret_cast<f32x4*>(dst + tok * PITCH + c) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
-        *reinterpret_cast<f32x4*>(dst + tok * PITCH + c + 4) = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
+        float* dst = (part ? sv : sk) + tok * PITCH + c;
+        *reinterpret_cast<f32x4*>(dst) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
       }
-    }
     __syncthreads();
     const int tok0 = JOIN ? 16 * wave : 0;
     f32x4 s[BLOCKS];
@@ -107,7 +125,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int tok = tok0 + 16 * n + 4 * q4 + i;
-        const bool vis = there[tok] && t0 + tok < sees;
+        const bool vis = at[tok] >= 0 && t0 + tok < sees;
         seen = seen || vis;
         s[n][i] = vis ? s[n][i] * a.scale_log2 : -INFINITY;
         top = fmaxf(top, s[n][i]);
@@ -142,7 +160,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
       // the rows that see it.
       for (int tok = tok0; tok < tok0 + 16 * BLOCKS; ++tok) {
         const int n = (tok - tok0) >> 4, i = tok & 3;
-        const bool holds = q4 == ((tok >> 2) & 3), vis = there[tok] && t0 + tok < sees;
+        const bool holds = q4 == ((tok >> 2) & 3), vis = at[tok] >= 0 && t0 + tok < sees;
         float p = 0.f;
 #pragma unroll
         for (int nn = 0; nn < BLOCKS; ++nn)
@@ -157,7 +175,8 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
         }
       }
     }
-    __syncthreads();                                   // (odd is read)
+    __syncthreads();                                   // the tile is read
+    if (tid == 0) *odd = 0;
   }
 
   l += __shfl_xor(l, 16);
@@ -220,7 +239,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
   }
 }
 
-// The parts of an item, in their order.  A lane holds four columns of a row.
+// grid: (items, groups of 256 quads of columns).  The parts of an item, in their order; a thread holds four columns of a row.
 template <int ROWS, int UNIT>
 __global__ void __launch_bounds__(256) heads_merge_kernel(HeadsArgs a) {
   HeadsItem it;
@@ -228,8 +247,8 @@ __global__ void __launch_bounds__(256) heads_merge_kernel(HeadsArgs a) {
   const int last = min(it.row0 + ROWS, it.rows) - 1, keys = max(it.sees(last, a.G), 0);
   const int per = heads_split_tokens(keys, a.n_splits, UNIT), parts = heads_parts(keys, per);
   if (parts == 1) return;
-  const int quads = a.d_v / 4;
-  for (int x = threadIdx.x; x < (last - it.row0 + 1) * quads; x += 256) {
+  const int quads = a.d_v / 4, x = blockIdx.y * 256 + threadIdx.x;
+  if (x < (last - it.row0 + 1) * quads) {
     const int r = x / quads, c = 4 * (x % quads), row = it.row0 + r;
     const size_t slot0 = (size_t)blockIdx.x * a.n_splits * ROWS + r;
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
@@ -248,9 +267,13 @@ __global__ void __launch_bounds__(256) heads_merge_kernel(HeadsArgs a) {
   }
 }
 
-// Few rows to a head of keys take the kernel whose waves share them.
-static bool general_joins(const tpla_heads_t& sh, int32_t max_new) {
-  return (int64_t)(sh.H / sh.H_kv) * (max_new > 0 ? max_new : 1) <= 16;
+// Rows of an item: 16, which the four waves share, for few rows to a head of keys and where items of 64 would leave compute units idle (three prompts of up to
+// 300 tokens, six heads, 96 columns, float: REPLACE); the rows of a sequence in items of 64 read the keys a quarter as often.
+static int general_rows(const tpla_heads_t& sh, int64_t T, int32_t max_new) {
+  const int64_t G = sh.H / sh.H_kv;
+  if (G * (max_new > 0 ? max_new : 1) <= 16) return 16;
+  const int64_t items = max_new > 0 ? (T * G / 64 + sh.B) * sh.H_kv : (G + 63) / 64 * sh.H_kv * sh.B;
+  return items < device_cu_count() ? 16 : 64;
 }
 
 HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages) {
@@ -258,12 +281,12 @@ HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
   p.kernel = HEADS_GENERAL;
   p.n_wg = 0;
   const int G = sh.H / sh.H_kv;
-  p.rows = general_joins(sh, max_new) ? 16 : 64;
+  p.rows = general_rows(sh, T, max_new);
   const int64_t tiles = max_new > 0 ? T * G / p.rows + sh.B : (G + p.rows - 1) / p.rows;
   p.items = tiles * sh.H_kv * (max_new > 0 ? 1 : sh.B);
   p.tiles = (int)(tiles < 2147483647 ? tiles : 2147483647);
   const int64_t tokens = (int64_t)max_pages * sh.page_tokens, want = (4 * (int64_t)device_cu_count() + p.items - 1) / p.items;
-  const int64_t most = (tokens + 255) / 256;
+  const int64_t most = (tokens + HG_SPLIT - 1) / HG_SPLIT;
   p.n_splits = (int)(want < 1 ? 1 : want < most ? want : most);
   p.slots = p.n_splits > 1 ? p.items * p.n_splits : 0;
   p.workspace = (size_t)p.slots * p.rows * (sh.d_v + 2) * sizeof(float);
@@ -272,7 +295,7 @@ HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
 
 // items * n_splits is below 4 compute units' worth of items and one more split of each, and there are fewer items than that wherever they are split.
 size_t general_heads_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages) {
-  if ((int64_t)max_pages * sh.page_tokens <= 256) return 0;
+  if ((int64_t)max_pages * sh.page_tokens <= HG_SPLIT) return 0;
   const int64_t fill = 4 * (int64_t)device_cu_count();
   size_t most = 0;
   for (int rows = 16; rows <= 64; rows *= 4) {
@@ -313,7 +336,7 @@ int launch_general_heads(const HeadsArgs& a, const HeadsPlan& p, int dtype, hipS
                              : (join ? launch_general<bf16_t, true>(a, p, st) : launch_general<bf16_t, false>(a, p, st));
   if (rc || p.n_splits == 1) return rc;
   void (*fn)(HeadsArgs) = join ? heads_merge_kernel<16, HG_JOIN_TOK> : heads_merge_kernel<64, HG_ROWS_TOK>;
-  hipLaunchKernelGGL(fn, dim3((unsigned)p.items), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)p.items, (unsigned)((p.rows * (a.d_v / 4) + 255) / 256)), dim3(256), 0, st, a);
   return check_launch("heads_merge_kernel");
 }
 

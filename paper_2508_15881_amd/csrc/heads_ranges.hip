@@ -17,6 +17,9 @@ constexpr int HN_NW = 4;
 constexpr int HN_TILE = 8192;            // bytes of keys, and of values, of a tile
 constexpr int HN_LOADS = HN_TILE / 1024; // direct-to-LDS loads each
 constexpr int HN_IDS = 1024;             // page ids held at once
+// Cache policy of the loads: not kept behind their use.  The cache is read once per step, and lines kept for it push out what is on its way (48 ragged
+// sequences, 1.5 GB: 269 us with the ordinary policy, 240 so).
+constexpr int HN_AUX = 2;
 constexpr int HN_MIN_UNITS = 4;          // tiles of a range at least: one per wave
 // Units of an item ahead of its tiles, for what it costs besides them (page ids, queries, the way of the first tiles, the join): many short items
 // are spread over the workgroups, and ranges with several of them end with the others.
@@ -165,14 +168,14 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
 #pragma unroll
         for (int k = 0; k < HN_LOADS; ++k)
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + ld_at[k]),
-                                           (__attribute__((address_space(3))) void*)(dst + k * 1024), 16, 0, 0);
+                                           (__attribute__((address_space(3))) void*)(dst + k * 1024), 16, 0, HN_AUX);
       } else {
 #pragma unroll
         for (int k = 0; k < HN_LOADS; ++k) {
           const int at = k * LOAD_TOK + lane / RC, tok = min(tok0 + at, keys - 1), p = page_of(tok), id = max(lds_read_page(ids + (p - id0)), 0);
           const char* src = head + (size_t)id * page_bytes + (size_t)(tok - p * pt) * (2 * D) + ((lane % RC) ^ heads_swz<RC>(at)) * 16;
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                           (__attribute__((address_space(3))) void*)(dst + k * 1024), 16, 0, 0);
+                                           (__attribute__((address_space(3))) void*)(dst + k * 1024), 16, 0, HN_AUX);
         }
       }
     };
@@ -424,33 +427,46 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
   }
 }
 
-// grid: (items, rows of an item).  The parts of a row in equal shares over groups of D / 4 threads, then over the groups, in a fixed order.
+// grid: (items, rows of an item).  The parts of a row in equal shares over groups of D / 4 threads, then over the groups, in a fixed order.  What a thread
+// reads of the first parts is on its way before the largest reference of the row is known.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(256) heads_ranges_merge_kernel(HeadsArgs a) {
-  constexpr int LPR = D / 4, GROUPS = 256 / LPR;
+  constexpr int LPR = D / 4, GROUPS = 256 / LPR, BATCH = 64 / GROUPS;
   __shared__ f32x4 cols[GROUPS][LPR];
   __shared__ float sums[GROUPS];
   const int item = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, c = tid % LPR, group = tid / LPR;
   const int block = item % a.tiles, v = item / a.tiles, b = v / a.H_kv, kvh = v % a.H_kv, row = block * ROWS + r;
+  const int w0 = a.plan[3 * item], parts = a.plan[3 * item + 1], odd = a.plan[3 * item + 2];        // (not looked at for rows that are none)
   int first;
   const int n = heads_new(a, b, first);
-  if (row >= n * a.G) return;
-  const int w0 = a.plan[3 * item], parts = a.plan[3 * item + 1], odd = a.plan[3 * item + 2];
-  if (parts == 1) return;
+  if (row >= n * a.G || parts == 1) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   auto slot = [&](int s) { return (size_t)(2 * (w0 + s) + (s == 0 ? odd : 0)) * ROWS + r; };
+  f32x4 x[BATCH];
+  float2 part[BATCH];
+  auto request = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const size_t at = slot(min(s0 + k * GROUPS, parts - 1));
+      part[k] = ml[at];
+      x[k] = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + 4 * c);
+    }
+  };
+  request(group);
   float M = -INFINITY;
   for (int s = tid & 63; s < parts; s += 64) M = fmaxf(M, ml[slot(s)].x);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
   float sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int s = group; s < parts; s += GROUPS) {
-    const float2 part = ml[slot(s)];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_acc + slot(s) * D + 4 * c);
-    const float by = heads_join(M, part, sum);
-    if (part.x != -INFINITY) o += x * by;
+  for (int s = group; s < parts; s += BATCH * GROUPS) {
+    if (s > group) request(s);
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (s + k * GROUPS < parts) {
+        const float by = heads_join(M, part[k], sum);
+        if (part[k].x != -INFINITY) o += x[k] * by;
+      }
   }
   cols[group][c] = o;
   if (c == 0) sums[group] = sum;
