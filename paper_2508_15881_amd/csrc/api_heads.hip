@@ -109,7 +109,7 @@ static int check_attention(const tpla_heads_t* sh, int64_t rows, int32_t* max_ne
   if (rows * sh->H >= (int64_t)1 << 28) return fail(TPLA_ERR_UNSUPPORTED, "rows * H = %lld above 2^28 - 1", (long long)rows * sh->H);
   if (sh->B >= 1 << 22) return fail(TPLA_ERR_UNSUPPORTED, "B=%d above 2^22 - 1", sh->B);
   *p = plan_heads(*sh, rows, *max_new, max_pages);
-  if (p->kernel == HEADS_RANGES && (double)p->items * (((double)max_pages * sh->page_tokens + 31) / 32 + 8) >= 2147483647.0)
+  if (p->kernel == HEADS_RANGES && p->n_wg > 0 && (double)p->items * (((double)max_pages * sh->page_tokens + 31) / 32 + 8) >= 2147483647.0)
     return fail(TPLA_ERR_UNSUPPORTED, "sequences * heads of keys * max_pages_per_seq too large");
   if (p->items >= (int64_t)1 << 23) return fail(TPLA_ERR_UNSUPPORTED, "%lld work items are more than a launch has", (long long)p->items);
   return TPLA_OK;

@@ -29,14 +29,14 @@ struct HeadsArgs {
   int T, max_new, n_splits;
   int tiles;                             // of rows: decode per (sequence, head of keys), prefill an upper bound for all sequences, per head of keys
   int32_t* plan;                         // ranges: where the merge finds an item's parts, three ints per item
-  int n_wg;                              // ranges: workgroups
+  int n_wg;                              // ranges: workgroups, each with a range (0: a workgroup per item); prompts: what the chip holds
   float scale_log2;
 };
 
 enum HeadsKernel { HEADS_GENERAL, HEADS_RANGES, HEADS_PROMPTS };
 struct HeadsPlan {
   HeadsKernel kernel;
-  int n_wg;                    // HEADS_RANGES: workgroups, each with an equal range of all tiles
+  int n_wg;                    // HeadsArgs::n_wg
   int64_t slots;               // partial results, of `rows` rows each
   int rows;                    // rows of an item
   int tiles;                   // HeadsArgs::tiles
@@ -48,7 +48,7 @@ struct HeadsPlan {
 HeadsPlan general_heads_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new, int32_t max_pages);
 size_t general_heads_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages);      // the most that a prefill of up to T tokens needs
 int launch_general_heads(const HeadsArgs& a, const HeadsPlan& p, int dtype, hipStream_t st);
-// bf16, d_k = d_v of 64 or 128, pages of a multiple of 16 tokens, at most 64 rows per head of keys: see heads_ranges.hip
+// bf16, d_k = d_v of 64 or 128, pages of a multiple of 16 tokens, at most 32 rows per head of keys: see heads_ranges.hip
 bool heads_mfma_supported(const tpla_heads_t& sh);
 bool heads_ranges_fit(const tpla_heads_t& sh, int32_t max_new);
 HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages);

@@ -16,6 +16,9 @@ namespace tpla {
 constexpr int HN_NW = 4;
 constexpr int HN_TILE = 8192;            // bytes of keys, and of values, of a tile
 constexpr int HN_LOADS = HN_TILE / 1024; // direct-to-LDS loads each
+// Rows per head of keys at most: more fill the tiles of heads_prompts.hip (4000 tokens: 2 sequences, 32 rows 15.4 us here, 29.8 there; 8 sequences of 8 heads of
+// keys, 20 rows 38.4 and 39.7, 48 rows 138 and 41).
+constexpr int HN_MOST = 32;
 constexpr int HN_IDS = 1024;             // page ids held at once
 // Cache policy of the loads: not kept behind their use.  The cache is read once per step, and lines kept for it push out what is on its way (48 ragged
 // sequences, 1.5 GB: 269 us with the ordinary policy, 240 so).
@@ -59,6 +62,23 @@ struct HeadsWalk {
     return u;
   }
   __device__ __forceinline__ int count(const HeadsArgs& a, const Units& u) const { return u.blocks * (u.tiles + HN_START) * a.H_kv; }
+  // One workgroup per item.
+  __device__ __forceinline__ bool take_item(const HeadsArgs& a) {
+    item = blockIdx.x;
+    const int block = item % a.tiles, v = item / a.tiles;
+    it.b = v / a.H_kv;
+    it.kvh = v % a.H_kv;
+    it.row0 = block * ROWS;
+    const int n = heads_new(a, it.b, it.first);
+    it.rows = n * a.G;
+    if (it.row0 >= it.rows) return false;
+    heads_lens(a, it.b, n, it);
+    t0 = 0;
+    t1 = tiles = max((it.keys + TOK - 1) / TOK, 1);
+    whole = true;
+    pos = end = 0;
+    return true;
+  }
   __device__ __forceinline__ bool begin(const HeadsArgs& a) {
     const int lane = threadIdx.x & 63;
     front = units_of(a, lane);
@@ -133,7 +153,8 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
   char* const vbuf = kbuf + HN_TILE;
 
   HeadsWalk<TOK, ROWS> walk;
-  if (!walk.begin(a)) return;
+  const bool items = a.n_wg == 0;                      // short contexts: a workgroup per item
+  if (!(items ? walk.take_item(a) : walk.begin(a) && walk.find(a))) return;
 
   unsigned ld_at[HN_LOADS], k_at[KS], v_at[DB];
 #pragma unroll
@@ -151,7 +172,7 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
   const bool one_page = pt % TOK == 0;                 // a tile never crosses a page
   const size_t page_bytes = (size_t)a.H_kv * pt * (2 * D);
 
-  while (walk.find(a)) {
+  do {
     const HeadsItem it = walk.it;
     const int keys = it.keys;
     const int32_t* table = a.table + (size_t)it.b * a.max_pages;
@@ -369,7 +390,7 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
         if (more) issue(v_head, vbuf, t + HN_NW);
       }
     }
-    walk.note(a);
+    if (!items) walk.note(a);
 
     // ---- the four waves' references, sums and columns, joined through their places ----
     float2* ml = reinterpret_cast<float2*>(ids);
@@ -424,7 +445,7 @@ __global__ void __launch_bounds__(HN_NW * 64, RB == 1 ? 2 : 1) heads_ranges_kern
         }
       }
     }
-  }
+  } while (!items && walk.find(a));
 }
 
 // grid: (items, rows of an item).  The parts of a row in equal shares over groups of D / 4 threads, then over the groups, in a fixed order.  What a thread
@@ -486,13 +507,17 @@ bool heads_mfma_supported(const tpla_heads_t& sh) {
   return sh.dtype == TPLA_BF16 && sh.d_k == sh.d_v && (sh.d_k == 64 || sh.d_k == 128) && sh.page_tokens % 16 == 0;
 }
 bool heads_ranges_fit(const tpla_heads_t& sh, int32_t max_new) {
-  return max_new == 0 || (int64_t)(sh.H / sh.H_kv) * max_new <= 64;
+  return (int64_t)(sh.H / sh.H_kv) * (max_new > 0 ? max_new : 1) <= HN_MOST;
 }
 
 static int ranges_blocks(const tpla_heads_t& sh, int32_t max_new) {        // of 16 rows
   const int64_t rows = (int64_t)(sh.H / sh.H_kv) * (max_new > 0 ? max_new : 1);
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return rows <= 16 ? 1 : 2;
 }
+
+// A workgroup per item, nothing to merge: short contexts, by the width of the block table, and longer ones whose items fill the chip.  32 heads on 8, 128 columns: one
+// sequence of 100 tokens 10.2 us in ranges, 7.6 so, of 1000 12.4 and 16.0; 32 of 500 21.9 and 14.8, of 2000 50.8 and 44.5; 8 of 1000 (64 items) 16.2 and 16.6.
+static bool items_alone(int64_t tokens, int64_t items) { return tokens <= 512 || (tokens <= 2048 && items >= device_cu_count()); }
 
 HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages) {
   HeadsPlan p;
@@ -503,6 +528,12 @@ HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
   p.items = (int64_t)sh.B * sh.H_kv * p.tiles;
   p.n_splits = 1;
+  if (items_alone((int64_t)max_pages * sh.page_tokens, p.items)) {
+    p.n_wg = 0;
+    p.slots = 0;
+    p.workspace = 0;
+    return p;
+  }
   const int tok = HN_TILE / (2 * sh.d_k);
   const double tiles = (double)p.items * (((double)max_pages * sh.page_tokens + tok - 1) / tok + HN_START);
   const int most = device_cu_count() * (rb == 1 ? 2 : 1);
@@ -522,17 +553,17 @@ int launch_heads_ranges(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st) 
   void (*fn)(HeadsArgs);
   void (*merge)(HeadsArgs);
   if (a.d_k == 128) {
-    fn = p.rows == 16 ? heads_ranges_kernel<128, 1> : p.rows == 32 ? heads_ranges_kernel<128, 2> : heads_ranges_kernel<128, 4>;
-    merge = p.rows == 16 ? heads_ranges_merge_kernel<128, 16> : p.rows == 32 ? heads_ranges_merge_kernel<128, 32> : heads_ranges_merge_kernel<128, 64>;
+    fn = p.rows == 16 ? heads_ranges_kernel<128, 1> : heads_ranges_kernel<128, 2>;
+    merge = p.rows == 16 ? heads_ranges_merge_kernel<128, 16> : heads_ranges_merge_kernel<128, 32>;
   } else {
-    fn = p.rows == 16 ? heads_ranges_kernel<64, 1> : p.rows == 32 ? heads_ranges_kernel<64, 2> : heads_ranges_kernel<64, 4>;
-    merge = p.rows == 16 ? heads_ranges_merge_kernel<64, 16> : p.rows == 32 ? heads_ranges_merge_kernel<64, 32> : heads_ranges_merge_kernel<64, 64>;
+    fn = p.rows == 16 ? heads_ranges_kernel<64, 1> : heads_ranges_kernel<64, 2>;
+    merge = p.rows == 16 ? heads_ranges_merge_kernel<64, 16> : heads_ranges_merge_kernel<64, 32>;
   }
   int rc = allow_lds(reinterpret_cast<const void*>(fn), HN_LDS, "heads_ranges_kernel");
   if (rc) return rc;
-  hipLaunchKernelGGL(fn, dim3(p.n_wg), dim3(HN_NW * 64), HN_LDS, st, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)(p.n_wg > 0 ? p.n_wg : p.items)), dim3(HN_NW * 64), HN_LDS, st, a);
   if ((rc = check_launch("heads_ranges_kernel"))) return rc;
-  if (p.n_wg == 1) return TPLA_OK;
+  if (p.n_wg <= 1) return TPLA_OK;
   const int rows = a.G * (a.cu ? a.max_new : 1);
   hipLaunchKernelGGL(merge, dim3((unsigned)p.items, (unsigned)(rows < p.rows ? rows : p.rows)), dim3(256), 0, st, a);
   return check_launch("heads_ranges_merge_kernel");

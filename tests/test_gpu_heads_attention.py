@@ -9,7 +9,7 @@ from heads_common import CODE, DTYPE, Cached, check, decode_parity, prefill_pari
 pytestmark = pytest.mark.gpu
 
 # H, H_kv, d_k, d_v, page, dtype
-SHAPES = [(8, 2, 128, 128, 64, "bf16"), (4, 4, 64, 64, 16, "bf16"), (16, 1, 128, 128, 32, "bf16"), (5, 1, 64, 64, 64, "bf16"), (40, 2, 128, 128, 128, "bf16"),
+SHAPES = [(8, 2, 128, 128, 64, "bf16"), (48, 1, 128, 128, 64, "bf16"), (130, 1, 64, 64, 32, "bf16"), (4, 4, 64, 64, 16, "bf16"), (16, 1, 128, 128, 32, "bf16"), (5, 1, 64, 64, 64, "bf16"), (40, 2, 128, 128, 128, "bf16"),
           (35, 1, 64, 64, 48, "bf16"), (6, 2, 96, 96, 16, "bf16"), (4, 2, 128, 64, 64, "bf16"), (4, 2, 128, 128, 24, "bf16"), (3, 1, 256, 256, 64, "bf16"),
           (6, 2, 96, 96, 16, "f32"), (4, 1, 64, 64, 64, "f32"), (2, 2, 24, 8, 7, "f32"), (12, 1, 128, 128, 64, "f32"), (2, 1, 256, 200, 64, "f32"), (1, 1, 8, 32, 5, "f32")]
 IDS = ["-".join(map(str, s)) for s in SHAPES]
@@ -22,6 +22,27 @@ def test_decode_lengths(H, H_kv, d_k, d_v, page, dtype):
     c.queries(len(lens))
     decode_parity(c, lens)
     decode_parity(c, lens, "f32")
+
+
+@pytest.mark.parametrize("H,H_kv,d_k,d_v,page,dtype", SHAPES, ids=IDS)
+@pytest.mark.parametrize("B", [5, 150])
+def test_decode_short_sequences_in_narrow_and_wide_tables(H, H_kv, d_k, d_v, page, dtype, B):
+    """How the work is cut follows from the width of the block table and the number of items, which the lengths do not tell."""
+    lens = [(37 * b) % 301 for b in range(B)]
+    for width in (-(-301 // page), -(-1500 // page), -(-20000 // page)):
+        c = Cached(lens, H, H_kv, d_k, d_v, page, dtype, max_pages=width, seed=width)
+        c.queries(B)
+        decode_parity(c, lens)
+
+
+@pytest.mark.parametrize("H,H_kv,d_k,d_v,page,dtype", SHAPES, ids=IDS)
+@pytest.mark.parametrize("new", [1, 3, 12, 40])
+def test_a_few_new_tokens_in_narrow_and_wide_tables(H, H_kv, d_k, d_v, page, dtype, new):
+    news, lens = [new, 1, new, new - 1, new], [0, 130, 255, 17, 300]
+    for width in (-(-400 // page), -(-5000 // page)):
+        c = Cached([a + b for a, b in zip(news, lens)], H, H_kv, d_k, d_v, page, dtype, max_pages=width, seed=width)
+        c.queries(sum(news))
+        prefill_parity(c, news, lens)
 
 
 @pytest.mark.parametrize("H,H_kv,d_k,d_v,page,dtype", SHAPES, ids=IDS)

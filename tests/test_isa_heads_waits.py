@@ -8,7 +8,7 @@ import test_isa_tree_results as results
 from paper_2508_15881_amd import build as b
 from test_isa_tree_waits import parse, touched_too_early
 
-INSTANCES = {"heads_ranges": 6, "heads_prompts": 8}
+INSTANCES = {"heads_ranges": 4, "heads_prompts": 8}
 
 
 @pytest.fixture(scope="module")
