@@ -47,39 +47,70 @@ __device__ __forceinline__ PromptSeq prompt_seq(const HeadsArgs& a, int b) {
   s.tiles = (s.it.rows + HP_ROWS - 1) / HP_ROWS;
   return s;
 }
-__device__ __forceinline__ int wave_total(int v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return __builtin_amdgcn_readfirstlane(v);
+__device__ __forceinline__ float wave_total(float v) {
+  const int lane = threadIdx.x & 63;
+  v += lane_xor<1>(v, lane);
+  v += lane_xor<2>(v, lane);
+  v += lane_xor<4>(v, lane);
+  v += lane_xor<8>(v, lane);
+  v += lane_xor<16>(v, lane);
+  return v + lane_xor<32>(v, lane);
 }
-// Tokens of a part, so that the parts of all items are one round of the workgroups that the chip holds, or two where there are more items than that.
-// (A few more than a round would take as long as two: two sequences, 536 parts of 4352 tokens for 512 workgroups, 217 us; 480 of 5120 REPLACE.)
+__device__ __forceinline__ float wave_most(float v) {
+  const int lane = threadIdx.x & 63;
+  v = fmaxf(v, lane_xor<1>(v, lane));
+  v = fmaxf(v, lane_xor<2>(v, lane));
+  v = fmaxf(v, lane_xor<4>(v, lane));
+  v = fmaxf(v, lane_xor<8>(v, lane));
+  v = fmaxf(v, lane_xor<16>(v, lane));
+  return fmaxf(v, lane_xor<32>(v, lane));
+}
+// Tokens of a part: of a few lengths, the one that ends first by an estimate in tokens (floats: every workgroup comes to the same).  S: workgroups at once.
+//   - no split: the longest item, or where there is more than a round of them, the mean of a round's workgroups and half an item;
+//   - parts of c tokens: c if they are one round, otherwise the mean and half of a part; and HP_MERGE for the partial results.
+// A few parts more than a round take as long as two: two sequences, 16 and 7 tiles of 8512 and 20211 tokens, 8 heads of keys: 536 parts of 4352 tokens 217 us, 480 of
+// 5120 195.  One prompt of 2000 tokens, 504 items, 32 heads on 8: unsplit 87 us, in parts of 1024 79; of 4000, 1000 items: stays unsplit.
+constexpr float HP_MERGE = 384.f;
 __device__ __forceinline__ int prompt_chunk(const HeadsArgs& a, const PromptSeq& front) {
   const int lane = threadIdx.x & 63;
-  double work = (double)front.tiles * front.it.keys;
-  int tiles = front.tiles;
+  const float S = (float)a.n_wg, per_token = (float)a.G * (1.f / HP_ROWS);      // tiles per new token
+  // of one sequence: tokens that all its tiles read (tile i sees some L + (i + 1) / per_token)
+  auto reads = [&](const PromptSeq& s) { return s.tiles * ((float)min(s.it.L, s.it.keys) + 0.5f * (float)(s.it.keys - min(s.it.L, s.it.keys))); };
+  float work = reads(front), items = (float)front.tiles, longest = front.tiles > 0 ? (float)front.it.keys : 0.f;
   for (int b0 = 64; b0 < a.B; b0 += 64) {
     const PromptSeq s = prompt_seq(a, b0 + lane);
-    work += (double)s.tiles * s.it.keys;
-    tiles += s.tiles;
+    work += reads(s);
+    items += (float)s.tiles;
+    longest = fmaxf(longest, s.tiles > 0 ? (float)s.it.keys : 0.f);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
-  tiles = wave_total(tiles);
-  const int room = tiles * a.H_kv <= a.n_wg ? a.n_wg : 2 * a.n_wg;
-  const double per = work * a.H_kv / room;
-  if (per >= 1073741824.0) return 0x7fffffff;
-  int chunk = max(((int)per + 63) / 64 * 64, HP_CHUNK_MIN);
-  for (int k = 0; k < 32; ++k) {
-    int units = front.tiles * heads_parts(front.it.keys, chunk);
-    for (int b0 = 64; b0 < a.B; b0 += 64) {
-      const PromptSeq s = prompt_seq(a, b0 + lane);
-      units += s.tiles * heads_parts(s.it.keys, chunk);
+  const float mean = wave_total(work) * (float)a.H_kv / S;
+  items = wave_total(items) * (float)a.H_kv;
+  longest = wave_most(longest);
+  if (!(mean < 1073741824.f) || items == 0.f) return 0x7fffffff;
+  float best = items <= S ? longest : fmaxf(longest, mean + 0.5f * mean * S / items);
+  int chunk = 0x7fffffff;
+#pragma unroll 1
+  for (int k = 0; k < 3; ++k) {
+    const int c = max(((int)(mean * (1.f + 0.19f * k)) + 63) / 64 * 64, HP_CHUNK_MIN);
+    float parts = 0.f, room = 0.f;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      const PromptSeq s = b0 == 0 ? front : prompt_seq(a, b0 + lane);
+      // the tiles that see more than p c tokens, over p
+      const int all = heads_parts(s.it.keys, c);
+      const float first = fminf(floorf((float)s.it.L / (float)c) + 1.f, (float)all);      // parts 0 .. first - 1 are every tile's
+      const float n = (float)all - first, gone = n * ((float)c * 0.5f * ((float)all - 1.f + first) - (float)s.it.L) * per_token;
+      parts += s.tiles > 0 ? fmaxf((float)s.tiles * (float)all - gone, (float)s.tiles) : 0.f;
+      room += (float)s.tiles * (float)all;
     }
-    if (wave_total(units) * a.H_kv <= room) return __builtin_amdgcn_readfirstlane(chunk);
-    chunk += max(chunk / 32 / 64 * 64, 64);
+    parts = wave_total(parts) * (float)a.H_kv;
+    if (wave_total(room) * (float)a.H_kv > (float)a.n_splits * S) continue;      // (below 2^24: exact)
+    const float ends = (parts <= S ? (float)c : mean + 0.5f * mean * S / parts) + HP_MERGE;
+    if (ends < best) {
+      best = ends;
+      chunk = c;
+    }
   }
-  return 0x7fffffff;
+  return __builtin_amdgcn_readfirstlane(chunk);
 }
 
 // Lane k gets what the sequence with the k-th largest key has in this lane (ties by index): `from` its lane.  Bit by bit from the top: the sequences that
@@ -102,9 +133,9 @@ __device__ __forceinline__ int longest_first(int key, int& from) {
   return rank;
 }
 
-// Heads of keys are the fastest index: workgroups go to the XCDs in turn, so each XCD's L2 holds the keys and values of few heads.  PARTS: the work
-// of an item is split; then tiles follow, then parts.  Otherwise whole sequences follow, longest first (in groups of 64), and the tiles of a
-// sequence from its last (most keys) to its first: the grid ends on short items.
+// Heads of keys are the fastest index: workgroups go to the XCDs in turn, so each XCD's L2 holds the keys and values of few heads.  Whole sequences follow,
+// longest first (in groups of 64), PARTS: the parts of all tiles one after the other, and the tiles of a sequence from its last (most keys) to its
+// first: the grid ends on short items.  (From the first tile to the last, one prompt of 4000 tokens, 32 heads on 8: 202 us; so 176.)
 // ITEMS: the unit is an item's part 0 and idx counts items alone (the merge, which finds the chunk in a.plan).
 template <bool PARTS, bool ITEMS>
 __device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, PromptUnit& u) {
@@ -116,13 +147,13 @@ __device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, PromptU
   if (PARTS && !ITEMS && blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = chunk;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     const PromptSeq s = b0 == 0 ? front : prompt_seq(a, b0 + lane);
-    const int parts = PARTS ? heads_parts(s.it.keys, chunk) : 1;
-    int units = s.tiles * parts, count = ITEMS ? s.tiles : units, from = lane;
-    if (!PARTS && a.B > 1) {
+    int tiles = s.tiles, units = s.tiles * (PARTS ? heads_parts(s.it.keys, chunk) : 1), from = lane;
+    if (a.B > 1) {
       longest_first((s.it.keys >> 5) + (s.tiles > 0 ? 1 : 0), from);
-      units = count = __shfl(count, from);
+      tiles = __shfl(tiles, from);
+      units = __shfl(units, from);
     }
-    const int incl = wave_prefix(units), count_incl = ITEMS ? wave_prefix(count) : incl;
+    const int count = ITEMS ? tiles : units, incl = wave_prefix(units), count_incl = ITEMS ? wave_prefix(count) : incl;
     const unsigned long long past = __ballot(count_incl > at);
     if (past == 0) {
       at -= __builtin_amdgcn_readlane(count_incl, 63);
@@ -132,18 +163,18 @@ __device__ __forceinline__ bool prompt_unit(const HeadsArgs& a, int idx, PromptU
     const int place = __builtin_ctzll(past), src = __builtin_amdgcn_readlane(from, place);
     at -= __builtin_amdgcn_readlane(count_incl - count, place);
     before += __builtin_amdgcn_readlane(incl - units, place);
-    const int tiles = __builtin_amdgcn_readlane(s.tiles, src);
+    tiles = __builtin_amdgcn_readlane(tiles, place);
     u.it.b = b0 + src;
     u.it.kvh = kvh;
     u.it.first = __builtin_amdgcn_readlane(s.it.first, src);
     u.it.rows = __builtin_amdgcn_readlane(s.it.rows, src);
     u.it.L = __builtin_amdgcn_readlane(s.it.L, src);
     u.it.keys = __builtin_amdgcn_readlane(s.it.keys, src);
-    const int part = PARTS ? at / tiles : 0, tile = PARTS ? at - part * tiles : tiles - 1 - at;
-    u.it.row0 = tile * HP_ROWS;
+    const int part = PARTS ? at / tiles : 0, nth = PARTS ? at - part * tiles : at;
+    u.it.row0 = (tiles - 1 - nth) * HP_ROWS;
     const int keys = max(u.it.sees(min(u.it.row0 + HP_ROWS, u.it.rows) - 1, a.G), 0);
     u.parts = PARTS ? heads_parts(keys, chunk) : 1;
-    u.slot = (before + tile) * a.H_kv + kvh;
+    u.slot = (before + nth) * a.H_kv + kvh;
     u.step = tiles * a.H_kv;
     if (part >= u.parts) return false;
     u.k0 = PARTS ? part * chunk : 0;                   // (part < parts: below keys)
@@ -620,30 +651,34 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   });
 }
 
-// grid: (items, groups of 256 / (D / 4) rows).  The parts of a row in their order, a thread for four columns.
+// grid: (items, HP_MERGE_Y): the rows of an item dealt over workgroups.  The parts of a row in their order, a thread for four columns.
+constexpr int HP_MERGE_Y = 4;
 template <int D>
 __global__ void __launch_bounds__(256) heads_prompts_merge_kernel(HeadsArgs a) {
   constexpr int LPR = D / 4, AT_ONCE = 256 / LPR;
+  if (a.plan[0] == 0x7fffffff) return;                 // nothing was split
   PromptUnit u;
   if (!prompt_unit<true, true>(a, blockIdx.x, u) || u.parts == 1) return;
-  const int r = blockIdx.y * AT_ONCE + threadIdx.x / LPR, c = 4 * (threadIdx.x % LPR), row = u.it.row0 + r;
-  if (row >= u.it.rows) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
-  auto at = [&](int p) { return (size_t)(u.slot + p * u.step) * HP_ROWS + r; };
-  float M = -INFINITY, sum = 0.f;
-  for (int p = 0; p < u.parts; ++p) M = fmaxf(M, ml[at(p)].x);
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const int c = 4 * (threadIdx.x % LPR);
+  for (int r = blockIdx.y * AT_ONCE + threadIdx.x / LPR; r < HP_ROWS && u.it.row0 + r < u.it.rows; r += HP_MERGE_Y * AT_ONCE) {
+    auto at = [&](int p) { return (size_t)(u.slot + p * u.step) * HP_ROWS + r; };
+    float M = -INFINITY, sum = 0.f;
+    for (int p = 0; p < u.parts; ++p) M = fmaxf(M, ml[at(p)].x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int p = 0; p < u.parts; ++p) {
-    const float2 part = ml[at(p)];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_acc + at(p) * D + c);
-    const float by = heads_join(M, part, sum);
-    if (part.x != -INFINITY) o += x * by;
+    for (int p = 0; p < u.parts; ++p) {
+      const float2 part = ml[at(p)];
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_acc + at(p) * D + c);
+      const float by = heads_join(M, part, sum);
+      if (part.x != -INFINITY) o += x * by;
+    }
+    const int row = u.it.row0 + r;
+    const size_t out = (size_t)(u.it.first + row / a.G) * a.H + u.it.kvh * a.G + row % a.G;
+    const float inv = heads_inverse(sum);
+    store4(a.o, out * D + c, a.o_dtype, sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * inv);
+    if (a.lse && c == 0) a.lse[out] = heads_lse(M, sum);
   }
-  const size_t out = (size_t)(u.it.first + row / a.G) * a.H + u.it.kvh * a.G + row % a.G;
-  const float inv = heads_inverse(sum);
-  store4(a.o, out * D + c, a.o_dtype, sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * inv);
-  if (a.lse && c == 0) a.lse[out] = heads_lse(M, sum);
 }
 
 static int64_t prompts_items(const tpla_heads_t& sh, int64_t T) { return (T * (sh.H / sh.H_kv) / HP_ROWS + sh.B) * sh.H_kv; }
@@ -655,9 +690,10 @@ HeadsPlan heads_prompts_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
   p.items = prompts_items(sh, T);
   p.tiles = (int)(p.items / sh.H_kv);
   p.n_wg = HP_PER_CU * device_cu_count();                      // workgroups that the chip holds
-  // Split where the items do not fill it twice and there are tokens to split.
-  p.n_splits = p.items < 2 * p.n_wg && (int64_t)max_pages * sh.page_tokens > HP_CHUNK_MIN ? 2 : 1;
-  p.slots = p.n_splits > 1 ? (p.items <= p.n_wg ? 1 : 2) * (int64_t)p.n_wg : 0;        // (see prompt_chunk)
+  // Split where the items do not fill it twice and there are tokens to split; n_splits: rounds of partial results that there is room for.
+  const bool split = p.items < 2 * p.n_wg && (int64_t)max_pages * sh.page_tokens > HP_CHUNK_MIN;
+  p.n_splits = split ? (int)(p.items / p.n_wg) + 2 : 1;
+  p.slots = split ? p.n_splits * (int64_t)p.n_wg : 0;
   p.workspace = p.slots > 0 ? (size_t)p.slots * p.rows * (sh.d_v + 2) * sizeof(float) + 16 : 0;
   return p;
 }
@@ -665,7 +701,7 @@ HeadsPlan heads_prompts_plan(const tpla_heads_t& sh, int64_t T, int32_t max_new,
 size_t heads_prompts_room(const tpla_heads_t& sh, int64_t T, int32_t max_pages) {
   if ((int64_t)max_pages * sh.page_tokens <= HP_CHUNK_MIN) return 0;
   const int64_t n_wg = HP_PER_CU * device_cu_count();
-  return (size_t)((prompts_items(sh, T) <= n_wg ? 1 : 2) * n_wg) * HP_ROWS * (sh.d_v + 2) * sizeof(float) + 16;
+  return (size_t)((std::min(prompts_items(sh, T), 2 * n_wg - 1) / n_wg + 2) * n_wg) * HP_ROWS * (sh.d_v + 2) * sizeof(float) + 16;
 }
 
 template <int D>
@@ -681,9 +717,7 @@ int launch_heads_prompts(const HeadsArgs& a, const HeadsPlan& p, hipStream_t st)
   if (rc) return rc;
   hipLaunchKernelGGL(fn, dim3((unsigned)(parts ? p.slots : p.items)), dim3(HP_NW * 64), HP_LDS, st, a);
   if ((rc = check_launch("heads_prompts_kernel")) || !parts) return rc;
-  const int rows = 256 / (a.d_k / 4);
-  hipLaunchKernelGGL(a.d_k == 128 ? heads_prompts_merge_kernel<128> : heads_prompts_merge_kernel<64>, dim3((unsigned)p.items, HP_ROWS / rows), dim3(256), 0,
-                     st, a);
+  hipLaunchKernelGGL(a.d_k == 128 ? heads_prompts_merge_kernel<128> : heads_prompts_merge_kernel<64>, dim3((unsigned)p.items, HP_MERGE_Y), dim3(256), 0, st, a);
   return check_launch("heads_prompts_merge_kernel");
 }
 
