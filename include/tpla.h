@@ -537,7 +537,7 @@ int tpla_commit_drafts(const tpla_shape_t* shape, int32_t T, const int32_t* acce
  */
 typedef struct tpla_heads {
   int32_t B;           /* sequences                                                  */
-  int32_t H;           /* query heads, a multiple of H_kv                            */
+  int32_t H;           /* query heads, a multiple of H_kv, at most 65535             */
   int32_t H_kv;        /* heads of keys and values                                   */
   int32_t d_k;         /* width of a query and a key, a multiple of 8, at most 256   */
   int32_t d_v;         /* width of a value, likewise                                 */

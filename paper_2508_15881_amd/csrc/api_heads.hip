@@ -14,6 +14,7 @@ static int check_heads(const tpla_heads_t* sh) {
   if (sh->d_k % 8 || sh->d_v % 8) return fail(TPLA_ERR_SHAPE, "d_k=%d and d_v=%d must be multiples of 8 (16-byte row pieces)", sh->d_k, sh->d_v);
   if (!(sh->sm_scale > 0.0f) || !isfinite(sh->sm_scale)) return fail(TPLA_ERR_SHAPE, "sm_scale must be positive and finite");
   if (sh->d_k > 256 || sh->d_v > 256) return fail(TPLA_ERR_UNSUPPORTED, "d_k=%d d_v=%d above 256", sh->d_k, sh->d_v);
+  if (sh->H > 65535) return fail(TPLA_ERR_UNSUPPORTED, "H=%d above 65535", sh->H);
   if ((int64_t)sh->H_kv * sh->page_tokens > (int64_t)2147483647) return fail(TPLA_ERR_UNSUPPORTED, "H_kv * page_tokens too large");
   return TPLA_OK;
 }

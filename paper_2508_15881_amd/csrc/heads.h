@@ -24,11 +24,11 @@ struct HeadsArgs {
   const void *q, *k_pool, *v_pool;
   const int32_t *table, *lens, *cu;      // cu nullptr: decode, one row of q per sequence, lens count it; lens nullptr: 0
   void* o;
-  float *lse, *part_acc, *part_ml;       // partial results: [item][split][rows of an item], of d_v columns and of (reference, sum)
+  float *lse, *part_acc, *part_ml;       // partial results: [slot][rows of an item], of d_v columns and of (reference, sum)
   int B, H, H_kv, G, d_k, d_v, page_tokens, max_pages, o_dtype;
   int T, max_new, n_splits;
   int tiles;                             // of rows: decode per (sequence, head of keys), prefill an upper bound for all sequences, per head of keys
-  int32_t* plan;                         // ranges: where the merge finds an item's parts, three ints per item
+  int32_t* plan;                         // ranges: where the merge finds an item's parts, three ints per item; prompts: tokens of a part
   int n_wg;                              // ranges: workgroups, each with a range (0: a workgroup per item); prompts: what the chip holds
   float scale_log2;
 };
@@ -40,8 +40,8 @@ struct HeadsPlan {
   int64_t slots;               // partial results, of `rows` rows each
   int rows;                    // rows of an item
   int tiles;                   // HeadsArgs::tiles
-  int64_t items;               // work items (upper bound), each of n_splits parts of its tokens
-  int n_splits;
+  int64_t items;               // work items (upper bound)
+  int n_splits;                // general: parts of an item; prompts: 1, or rounds of parts that there are slots for
   size_t workspace;            // bytes
 };
 // max_new = 0: decode
@@ -64,7 +64,8 @@ struct HeadsItem {
   int b, kvh, row0, rows;      // rows of the sequence in all; row0 < rows
   int first;                   // row of q and o of its first new token
   int L, keys;                 // tokens before the new ones, tokens that exist
-  __device__ __forceinline__ int sees(int r, int G) const { return min(L + r / G + 1, keys); }     // tokens that row r sees (negative pages apart)
+  // Tokens that row r sees (negative pages apart): L + r / G + 1 of those that exist.
+  __device__ __forceinline__ int sees(int r, int G) const { return r / G + 1 < keys - L ? L + r / G + 1 : keys; }
 };
 
 __device__ __forceinline__ int wave_prefix(int v) {      // inclusive sum over the wave

@@ -516,7 +516,8 @@ static int ranges_blocks(const tpla_heads_t& sh, int32_t max_new) {        // of
 }
 
 // A workgroup per item, nothing to merge: short contexts, by the width of the block table, and longer ones whose items fill the chip.  32 heads on 8, 128 columns: one
-// sequence of 100 tokens 10.2 us in ranges, 7.6 so, of 1000 12.4 and 16.0; 32 of 500 21.9 and 14.8, of 2000 50.8 and 44.5; 8 of 1000 (64 items) 16.2 and 16.6.
+// sequence of 100 tokens 10.2 us in ranges, 7.6 so, of 1000 12.4 and 16.0; 32 of 500 21.9 and 14.8, of 2000 50.8 and 44.5; 8 of 1000 (64 items) 16.2 and 16.6.  (Wider tables may hold one
+// long sequence among short ones, which only ranges divide.)
 static bool items_alone(int64_t tokens, int64_t items) { return tokens <= 512 || (tokens <= 2048 && items >= device_cu_count()); }
 
 HeadsPlan heads_ranges_plan(const tpla_heads_t& sh, int32_t max_new, int32_t max_pages) {

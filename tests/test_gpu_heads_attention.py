@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2508_15881_amd as tp
-from heads_common import CODE, DTYPE, Cached, check, decode_parity, prefill_parity, run_decode, run_prefill
+from heads_common import CODE, DTYPE, HALF_STEP, Cached, check, decode_parity, prefill_parity, run_decode, run_prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -84,6 +84,52 @@ def test_prefill_long_prompt(dtype):
     c = Cached([1500], 4, 1, 128, dtype=dtype, sharp=1.5)
     c.queries(1500)
     prefill_parity(c, [1500], [0], "f32", rows=[0, 1, 31, 32, 63, 64, 127, 128, 500, 511, 512, 1000, 1498, 1499])
+
+
+@pytest.mark.parametrize("H,H_kv,d,page,dtype", [(4, 2, 128, 64, "bf16"), (6, 1, 64, 16, "bf16"), (2, 1, 32, 16, "f32")])
+def test_prefill_many_sequences(H, H_kv, d, page, dtype):
+    news, lens = [(7 * b) % 23 for b in range(150)], [(b * b) % 61 for b in range(150)]
+    c = Cached([a + b for a, b in zip(news, lens)], H, H_kv, d, page=page, dtype=dtype)
+    c.queries(sum(news))
+    prefill_parity(c, news, lens)
+
+
+def wanted(q, k_pool, v_pool, ids, seen, G, scale):
+    """o of one row of q [H, d] over the first `seen` tokens of pages `ids`, and the sum of weight |value|, in 64 bits on the GPU."""
+    d = q.shape[1]
+    K, V = (p[ids].double().transpose(0, 1).reshape(p.shape[1], -1, d)[:, :seen] for p in (k_pool, v_pool))
+    s = (K @ q.double().reshape(-1, G, d).transpose(1, 2)).transpose(1, 2) * scale
+    p = torch.softmax(s, -1)
+    return (p @ V).reshape(-1, d), (p @ V.abs()).reshape(-1, d)
+
+
+def test_more_pages_than_are_held_at_once():
+    """Tokens of more than a thousand small pages in one workgroup: a long prompt that is not split, and ranges of many long sequences."""
+    d, page, n = 64, 16, 17003
+    pages = -(-n // page)
+    pools = [torch.randn((pages, 4, page, d), device="cuda").to(torch.bfloat16) for _ in range(2)]
+    table = torch.randperm(pages, device="cuda").to(torch.int32)[None].contiguous()
+    shape = tp.TplaHeads(1, 8, 4, d, d, page, tp.TPLA_BF16, d ** -0.5)
+    q = (4 * torch.randn((n, 8, d), device="cuda")).to(torch.bfloat16)            # few tokens weigh: a lost one is seen
+    o = torch.empty((n, 8, d), device="cuda")
+    size = tp.tpla_workspace_bytes_prefill_heads(shape, n, n, pages)
+    ws, cu = torch.empty(max(16, size), dtype=torch.uint8, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    tp.tpla_prefill_heads(shape, q, *pools, table, pages, None, cu, n, n, ws, size, o, tp.TPLA_F32, None)
+    for row in (0, 5000, 16300, 16367, 16368, 16400, 17002):
+        want, span = wanted(q[row], *pools, table[0].long(), row + 1, 2, d ** -0.5)
+        assert ((o[row].double() - want).abs() <= (2 * HALF_STEP["bf16"] + 2.0 ** -11) * span).all(), row       # the weights' roundings (see check), floats
+    B, n, G = 520, 16700, 2
+    pages = -(-n // page)
+    pools = [torch.randn((4000, 1, page, d), device="cuda").to(torch.bfloat16) for _ in range(2)]          # sequences share pages: legal for reading
+    table = torch.randint(0, 4000, (B, pages), device="cuda").to(torch.int32)
+    shape = tp.TplaHeads(B, G, 1, d, d, page, tp.TPLA_BF16, d ** -0.5)
+    q, o = (4 * torch.randn((B, G, d), device="cuda")).to(torch.bfloat16), torch.empty((B, G, d), device="cuda")
+    size = tp.tpla_workspace_bytes_heads(shape, pages)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    tp.tpla_decode_heads(shape, q, *pools, table, pages, torch.full((B,), n, dtype=torch.int32, device="cuda"), ws, size, o, tp.TPLA_F32, None)
+    for b in (0, 1, 259, 518, 519):
+        want, span = wanted(q[b], *pools, table[b].long(), n, G, d ** -0.5)
+        assert ((o[b].double() - want).abs() <= (2 * HALF_STEP["bf16"] + 2.0 ** -11) * span).all(), b
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -37,7 +37,8 @@ def close(dtype, got, want, size):
 
 CASES = [(1, 32, 8, 128, 128, "half", "bf16"), (7, 5, 1, 64, 64, "interleaved", "bf16"), (300, 6, 2, 96, 48, "half", "bf16"), (33, 4, 4, 128, 64, "interleaved", "f32"),
          (65, 3, 1, 64, 60, "half", "bf16"), (9, 3, 3, 40, 26, "half", "f32"), (5, 2, 1, 256, 256, "half", "bf16"), (12, 2, 2, 8, 8, "half", "f32"), (700, 17, 1, 24, 0, "half", "bf16"),
-         (1100, 8, 2, 32, 32, "half", "bf16"), (3, 200, 100, 128, 128, "half", "bf16"), (4, 6, 2, 200, 200, "half", "f32")]
+         (1100, 8, 2, 32, 32, "half", "bf16"), (3, 200, 100, 128, 128, "half", "bf16"), (4, 6, 2, 200, 200, "half", "f32"),
+         (31, 5, 5, 64, 36, "interleaved", "bf16"), (2100, 24, 3, 64, 64, "half", "bf16"), (2049, 3, 1, 32, 20, "interleaved", "f32")]
 
 
 def problem(T, H, H_kv, d, rot, layout, dtype, seed=3, d_v=None):
@@ -118,6 +119,27 @@ def test_values_that_are_not_finite_stay_in_their_row():
     want = torch.zeros((T, H), dtype=torch.bool, device="cuda")
     want[2, 1] = want[3, 0] = True
     assert torch.equal(odd, want) and (q_out[4, 2] == 0).all()
+
+
+def test_more_tokens_than_a_launch_has():
+    """Tokens around the borders of the parts that a long call goes in, on other rows than theirs if a stride were lost."""
+    T, H, d = (1 << 20) * 2 + 77, 2, 8
+    shape = shape_of(1, H, 1, d)
+    x = torch.randn((T, H + 1, d), device="cuda").to(torch.bfloat16)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") % 5000
+    freq = torch.from_numpy(tp.tpla_rotary_frequencies(d, 10000.0)).cuda()
+    q_out, k_out = torch.empty((T, H, d), dtype=torch.bfloat16, device="cuda"), torch.empty((T, 1, d), dtype=torch.bfloat16, device="cuda")
+    tp.tpla_norm_rotary_heads(shape, tp.TPLA_ROTARY_HALF, d, freq, 1.0, None, None, EPS, pos, T, x[:, :H], q_out, x[:, H:], k_out)
+    page, slots = 64, torch.arange(T, dtype=torch.int32, device="cuda")
+    pools = [torch.zeros((T // page + 1, 1, page, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q2 = torch.empty_like(q_out)
+    tp.tpla_append_heads(shape, tp.TPLA_ROTARY_HALF, d, freq, 1.0, None, None, EPS, pos, T, x[:, :H], q2, x[:, H:], x[:, H:], slots, *pools)
+    at = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, (1 << 21) - 1, 1 << 21, T - 1], device="cuda")
+    rows = x[at].double().cpu().numpy()
+    want, size = turned(rows, None, np.float64(np.float32(EPS)), d, tp.TPLA_ROTARY_HALF, freq.cpu().numpy(), pos[at].cpu().numpy(), 1.0)
+    close("bf16", q_out[at], want[:, :H], size[:, :H])
+    close("bf16", k_out[at], want[:, H:], size[:, H:])
+    assert torch.equal(q_out, q2) and torch.equal(pools[0].reshape(-1, d)[:T], k_out[:, 0]) and torch.equal(pools[1].reshape(-1, d)[:T], x[:, H])
 
 
 def test_pools_beyond_32_bit_offsets():

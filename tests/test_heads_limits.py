@@ -39,7 +39,7 @@ def prefill(s=None, q=A, kp=A, vp=A, table=A, pages=4, lens=A, cu=A, T=9, most=9
 
 
 BAD_SHAPES = [(dict(dtype=7), -5), (dict(B=0), -2), (dict(H=9), -2), (dict(H_kv=0), -2), (dict(d_k=100), -2), (dict(d_v=60), -2), (dict(page_tokens=0), -2),
-              (dict(sm_scale=0.0), -2), (dict(sm_scale=float("nan")), -2), (dict(d_k=264), -7), (dict(d_v=512), -7), (dict(H=1 << 20, H_kv=1 << 20, page_tokens=1 << 12), -7)]
+              (dict(sm_scale=0.0), -2), (dict(sm_scale=float("nan")), -2), (dict(d_k=264), -7), (dict(d_v=512), -7), (dict(H=1 << 17, H_kv=1 << 17), -7), (dict(H=1 << 15, H_kv=1 << 15, page_tokens=1 << 17), -7)]
 
 
 @pytest.mark.parametrize("kw,want", BAD_SHAPES)
