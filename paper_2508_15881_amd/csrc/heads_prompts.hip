@@ -459,15 +459,21 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
   };
 
   // ---- a tile that all rows of the workgroup see ----
-  auto plain_tile = [&](int t) {
-    constexpr int NS = KS * TB, NV = DB * (TB / 2), VA = 4;
-    const unsigned base = lds_base + (unsigned)((t % HP_NSTAGE) * (2 * HP_TILE)), kb = base + k_at, vb = base + v_at;
+  static_assert(HP_NSTAGE * 2 * HP_TILE <= 65536, "places within the offset of an LDS read");
+  unsigned k_reg[KS], v_reg[DB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) k_reg[ks] = lds_base + (k_at ^ (ks << 6));
+#pragma unroll
+  for (int d = 0; d < DB; ++d) v_reg[d] = lds_base + (v_at ^ (d << 5));
+  // PLACE: t % HP_NSTAGE, so that the places are offsets of the reads and not addresses to be added.
+  auto plain_tile = [&](auto place) {
+    constexpr int NS = KS * TB, NV = DB * (TB / 2), VA = 4, AT = decltype(place)::value * 2 * HP_TILE;
     f32x4 s[QB][TB];
     bf16x8 kf[NS], p[QB][TB / 2];
     u32x2 lo[VA], hi[VA];
     static_for<NS>([&](auto ic) {
       constexpr int x = decltype(ic)::value;
-      lds_read_b128<(x % TB) * (16 * RC * 16)>(kf[x], kb ^ ((x / TB) << 6));
+      lds_read_b128<AT + (x % TB) * (16 * RC * 16)>(kf[x], k_reg[x / TB]);
     });
     static_for<NS>([&](auto ic) {
       constexpr int x = decltype(ic)::value, ks = x / TB, n = x % TB;
@@ -483,8 +489,8 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
     // the first values start now, so that their way from LDS passes under the softmax
     auto value = [&](auto yc) {
       constexpr int y = decltype(yc)::value;
-      lds_read_tr_b64<(y / DB) * (32 * RC * 16)>(lo[y % VA], vb ^ ((y % DB) << 5));
-      lds_read_tr_b64<(y / DB) * (32 * RC * 16) + 16 * RC * 16>(hi[y % VA], vb ^ ((y % DB) << 5));
+      lds_read_tr_b64<AT + (y / DB) * (32 * RC * 16)>(lo[y % VA], v_reg[y % DB]);
+      lds_read_tr_b64<AT + (y / DB) * (32 * RC * 16) + 16 * RC * 16>(hi[y % VA], v_reg[y % DB]);
     };
     static_for<VA>([&](auto ic) { value(ic); });
     out_settle_write();
@@ -582,7 +588,9 @@ __global__ void __launch_bounds__(HP_NW * 64, 2) heads_prompts_kernel(HeadsArgs 
       }
 #pragma unroll
       for (int j = 0; j < CURS; ++j) lds_request_page(id[j], ids + min(cur[j].page - id0, last_id));
-      plain_tile(t);
+      static_for<HP_NSTAGE>([&](auto place) {
+        if (t % HP_NSTAGE == decltype(place)::value) plain_tile(place);
+      });
 #pragma unroll
       for (int j = 0; j < CURS; ++j) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(id[j]) : : "memory");      // (long there)
     }
