@@ -7,6 +7,8 @@
 // the tiles of an item in turn, each with a place of its own in LDS that direct loads fill: no barrier within an item, the next keys are
 // requested once the scores have read the last ones, the next values after the output product, and eight waves on a compute unit keep some
 // 100 KB on their way.  An item that lies in one range is written at once, the parts of the others are merged by a second kernel.
+// 48 sequences of 500 to 32000 tokens, 32 heads on 8, 128 columns (1.53 GB): 240 us with the merge = 6.4 TB/s, where a pure reader reaches 7.2; one sequence of
+// 9001 tokens 17.5 us: the kernel's 13.5 are lengths, page ids, first tiles, each a round trip, four tiles per wave and the join, then 4 of merge.
 #include "heads_tile.h"
 
 #include <algorithm>
