@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
   float* const sk = sm;
   float* const sv = sm + TOK * PITCH;
   long long* const rows_at = reinterpret_cast<long long*>(sv + TOK * PITCH);      // [2][TOK]: row of the pools that a token is, -1: none
-  volatile int* const odd = reinterpret_cast<int*>(rows_at + 2 * TOK);            // whether some staged value is not finite
+  volatile int* const odd = reinterpret_cast<int*>(rows_at + 2 * TOK);            // [2] whether some staged value is not finite, tile by tile in turn
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j16 = lane & 15, q4 = lane >> 4;
   HeadsItem it;
   if (!heads_item<Tile::ROWS>(a, blockIdx.x, it)) return;
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
     const int t = t0 + tid, page = t < k1 ? table[t / a.page_tokens] : -1;
     rows_at[which * TOK + tid] = page < 0 ? -1 : ((long long)page * a.H_kv + it.kvh) * a.page_tokens + t % a.page_tokens;
   };
-  if (tid == 0) *odd = 0;
+  if (tid < 2) odd[tid] = 0;
   find_rows(k0, 0);
   __syncthreads();
 
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
           bool fine = true;
 #pragma unroll
           for (int e = 0; e < 8; ++e) fine = fine && __builtin_isfinite(r.v[e]);
-          if (!fine) *odd = 1;
+          if (!fine) odd[which] = 1;
         }
         float* dst = (part ? sv : sk) + tok * PITCH + c;
         *reinterpret_cast<f32x4*>(dst) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
       }
 #pragma unroll
     for (int c = 0; c < NB; ++c) acc[c] *= alpha;
-    if (!*odd) {
+    if (!odd[which]) {
 #pragma unroll
       for (int n = 0; n < BLOCKS; ++n)
 #pragma unroll
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(256) heads_general_kernel(HeadsArgs a) {
       }
     }
     __syncthreads();                                   // the tile is read
-    if (tid == 0) *odd = 0;
+    if (tid == 0) odd[which] = 0;                      // (set again two tiles on: the barrier of the next lies between)
   }
 
   l += __shfl_xor(l, 16);
