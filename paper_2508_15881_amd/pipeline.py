@@ -220,6 +220,8 @@ class HeadsStep:
         the cache and attended to.  seq_lens: as for place, before the new tokens; decode: one new token for every sequence, seq_lens with it.
         Returns o [T, H, d_v] in the storage type."""
         T = q.shape[0]
+        if T > self.T or (decode and T != self.shape.B):
+            raise ValueError("%d new tokens, the step has %d sequences and room for %d" % (T, self.shape.B, self.T))
         B.tpla_append_heads(self.shape, self.layout, 2 * self.freq.numel(), self.freq, self.amplitude, q_weight, k_weight, self.norm_eps,
                             self.positions[:T], T, q, self.q[:T], k, v, self.slots[:T], k_pool, v_pool)
         if decode:

@@ -2,9 +2,10 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2508_15881_amd as tp
-from paper_2508_15881_amd import binding
+from paper_2508_15881_amd import binding, pipeline as pl
 
 A, F, H, K = 4096, tp.TPLA_F32, tp.TPLA_ROTARY_HALF, 1 << 40
 
@@ -100,10 +101,19 @@ def test_prefill():
 
 
 def test_binding_checks_views():
-    import torch
     s = shape()
     q = torch.zeros((4, 8, 128), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         tp.tpla_norm_rotary_heads(s, H, 128, A, 1.0, None, None, 1e-6, A, 4, q.transpose(1, 2), q, None, None)
     with pytest.raises(ValueError):
         tp.tpla_norm_rotary_heads(s, H, 128, A, 1.0, None, None, 1e-6, A, 5, q, q, None, None)
+
+
+def test_step_refuses_tokens_that_it_has_no_rows_for():
+    step = pl.HeadsStep(shape(B=3), 4, [1.0] * 64, max_tokens=5, device="cpu")
+    rows = lambda T, h: torch.zeros((T, h, 128), dtype=torch.bfloat16)  # noqa: E731
+    pool = torch.zeros((12, 2, 64, 128), dtype=torch.bfloat16)
+    table, lens = torch.zeros((3, 4), dtype=torch.int32), torch.ones(3, dtype=torch.int32)
+    for T, decode in ((6, False), (2, True), (4, True)):
+        with pytest.raises(ValueError, match="new tokens"):
+            step.run(rows(T, 8), rows(T, 2), rows(T, 2), None, None, pool, pool, table, lens, decode=decode)
