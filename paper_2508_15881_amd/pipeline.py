@@ -187,13 +187,18 @@ class DraftStep:
 
 class HeadsStep:
     """Buffers and call order of layers with grouped heads, for the tokens that a serving step adds to each of B sequences: one (decode) or
-    up to max_new (prompts, or parts of prompts behind cached tokens).  The pages, slots and positions are those of the latent layers."""
+    some (prompts, or parts of prompts behind cached tokens).  The pages, slots and positions are those of the latent layers."""
 
-    def __init__(self, shape, max_pages_per_seq, frequencies, max_tokens=None, max_new=1, layout=B.TPLA_ROTARY_HALF, amplitude=1.0, norm_eps=1e-6,
+    def __init__(self, shape, max_pages_per_seq, frequencies, max_tokens=None, max_new=None, layout=B.TPLA_ROTARY_HALF, amplitude=1.0, norm_eps=1e-6,
                  device="cuda"):
-        """max_tokens: room for new tokens of all sequences together (B of them by default)."""
-        self.shape, self.max_pages, self.max_new = shape, int(max_pages_per_seq), int(max_new)
-        self.T = int(max_tokens or shape.B)
+        """max_tokens: room for new tokens of all sequences together (B of them by default); max_new: the most that place lets one of them
+        have, where it is told their numbers (max_tokens by default)."""
+        self.shape, self.max_pages = shape, int(max_pages_per_seq)
+        self.T = shape.B if max_tokens is None else int(max_tokens)
+        self.max_new = self.T if max_new is None else int(max_new)
+        if self.T < 1 or self.max_new < 1:
+            raise ValueError("room for %d new tokens, %d of a sequence" % (self.T, self.max_new))
+        self.news = None
         self.layout, self.amplitude, self.norm_eps = layout, float(amplitude), float(norm_eps)
         self.freq = torch.as_tensor(frequencies, dtype=torch.float64).to(device)
         self.tables = B.TplaShape(shape.B, 1, 8, 1, 8, 1, 1, shape.page_tokens, shape.dtype, 1.0)      # B and page_tokens are what counts
@@ -206,14 +211,26 @@ class HeadsStep:
         n = B.tpla_workspace_bytes_heads(shape, self.max_pages)
         if n == 0:
             raise B.TplaError(-2, B.tpla_last_error())
-        self.ws_bytes = max(n, B.tpla_workspace_bytes_prefill_heads(shape, self.T, self.max_new, self.max_pages))
+        self.ws_bytes = max(n, B.tpla_workspace_bytes_prefill_heads(shape, self.T, self.T, self.max_pages))
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 
-    def place(self, seq_lens, add_lens, free_pages, n_free, pages_held, block_table):
+    def place(self, seq_lens, add_lens, free_pages, n_free, pages_held, block_table, news=None):
         """Pages, slots and positions of the new tokens, packed (once per step, for all layers).  counts: pages taken, pages that were missing;
-        tokens without a page are neither written nor seen."""
+        tokens without a page are neither written nor seen.  news: add_lens as the host knows them, if it does.  They are held to the step's
+        room, run then takes as many rows and no others, and the prefill runs on the kernels for as few as the longest has.  Without them
+        (where a captured step is replayed with other numbers) a sequence may have all of run's rows, and rows that no token owns become NaN
+        here, for all layers."""
+        self.news = None
+        if news is not None:
+            news = [int(n) for n in news]
+            if len(news) != self.shape.B or min(news) < 0 or max(news) > self.max_new or sum(news) > self.T:
+                raise ValueError("new tokens %r of %d sequences, the step has room for %d, %d of a sequence" % (news, self.shape.B, self.T, self.max_new))
+        else:
+            self.o.fill_(math.nan)
+            self.lse.fill_(math.nan)
         B.tpla_extend_sequences(self.tables, seq_lens, add_lens, 0, None, free_pages, n_free, pages_held, pages_held, block_table, self.max_pages,
                                 self.cu, self.slots, self.positions, self.T, self.counts)
+        self.news = news
 
     def run(self, q, k, v, q_weight, k_weight, k_pool, v_pool, block_table, seq_lens, decode=False):
         """One layer: q [T, H, d_k], k [T, H_kv, d_k], v [T, H_kv, d_v] of the step's T new tokens (views of a projection will do), written to
@@ -222,14 +239,16 @@ class HeadsStep:
         T = q.shape[0]
         if T > self.T or (decode and T != self.shape.B):
             raise ValueError("%d new tokens, the step has %d sequences and room for %d" % (T, self.shape.B, self.T))
+        if self.news is not None and (T != sum(self.news) or (decode and set(self.news) != {1})):
+            raise ValueError("%d new tokens%s, place was told %r" % (T, " to decode" if decode else "", self.news))
         B.tpla_append_heads(self.shape, self.layout, 2 * self.freq.numel(), self.freq, self.amplitude, q_weight, k_weight, self.norm_eps,
                             self.positions[:T], T, q, self.q[:T], k, v, self.slots[:T], k_pool, v_pool)
         if decode:
             B.tpla_decode_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.workspace, self.ws_bytes,
                                 self.o[:T], self.shape.dtype, self.lse[:T])
         else:
-            B.tpla_prefill_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.cu, T, min(self.max_new, T),
-                                 self.workspace, self.ws_bytes, self.o[:T], self.shape.dtype, self.lse[:T])
+            B.tpla_prefill_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.cu, T,
+                                 T if self.news is None else max(self.news), self.workspace, self.ws_bytes, self.o[:T], self.shape.dtype, self.lse[:T])
         return self.o[:T]
 
 
