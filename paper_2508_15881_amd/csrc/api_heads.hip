@@ -46,8 +46,8 @@ static int check_rows(int64_t T, int esz, const RowsOf* rows, int n) {
     if (*r.ts < 0 || *r.hs < 0) return fail(TPLA_ERR_SHAPE, "a stride of %s is negative", r.name);
     if (*r.ts * esz % 16 || *r.hs * esz % 16) return fail(TPLA_ERR_ALIGN, "strides of %s must be whole 16 bytes", r.name);
     if (!aligned16(r.p)) return fail(TPLA_ERR_ALIGN, "%s is not 16-byte aligned", r.name);
-    // an output whose rows lie closer than they are wide would be written twice
-    if (r.written && ((T > 1 && *r.ts < r.width) || (r.heads > 1 && *r.hs < r.width))) return fail(TPLA_ERR_SHAPE, "rows of %s overlap", r.name);
+    // an output whose rows share memory would be written twice
+    if (r.written && rows_share(T, *r.ts, r.heads, *r.hs, r.width)) return fail(TPLA_ERR_SHAPE, "rows of %s overlap", r.name);
   }
   return TPLA_OK;
 }

@@ -284,6 +284,29 @@ int check_dtype(const tpla_shape_t* sh);
 int check_shape(const tpla_shape_t* sh);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Whether two rows of `width` elements share some, of n x m rows that begin at i a + j b (strides a, b >= 0).
+inline bool rows_share(int64_t n, int64_t a, int64_t m, int64_t b, int64_t width) {
+  if ((n > 1 && a < width) || (m > 1 && b < width)) return true;
+  if (n <= 1 || m <= 1) return false;
+  if (b <= (a - width) / (m - 1) || a <= (b - width) / (n - 1)) return false;      // all rows of one dimension lie within a step of the other
+  // otherwise some multiple of one stride lies less than a row from one of the other's: the shorter dimension's multiples, and their neighbours
+  if (n > m) {
+    int64_t t = n;
+    n = m;
+    m = t;
+    t = a;
+    a = b;
+    b = t;
+  }
+  for (int64_t i = 1; i < n; ++i) {
+    const __int128 at = (__int128)i * a, j = at / b;
+    if (j >= m) return false;
+    if (j > 0 && at - j * b < width) return true;
+    if (j + 1 < m && (j + 1) * b - at < width) return true;
+  }
+  return false;
+}
+
 // Pages, slots and positions of new tokens; accepted drafts: see token_tables.hip.
 struct ExtendArgs {
   const int32_t* seq_lens;
