@@ -205,8 +205,8 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
     if (s < 0) return fail(TPLA_ERR_SHAPE, "a stride is negative");
     if (s * esz % 16) return fail(TPLA_ERR_ALIGN, "strides must be whole 16 bytes");
   }
-  // an output whose rows lie closer than they are wide would be written twice
-  if (q && ((T > 1 && q_out_token_stride < shape->d_r) || (shape->H > 1 && q_out_head_stride < shape->d_r)))
+  // an output whose rows share memory would be written twice
+  if (q && rows_share(T, q_out_token_stride, shape->H, q_out_head_stride, shape->d_r))
     return fail(TPLA_ERR_SHAPE, "rows of q_out overlap");
   if (k && T > 1 && k_out_token_stride < shape->d_r) return fail(TPLA_ERR_SHAPE, "rows of k_out overlap");
   if ((q && q == q_out && (q_token_stride != q_out_token_stride || q_head_stride != q_out_head_stride)) ||
