@@ -44,7 +44,8 @@ static int check_rows(int64_t T, int esz, const RowsOf* rows, int n) {
     if (!r.p || r.heads == 1) *r.hs = 0;
     if (!r.p) continue;
     if (*r.ts < 0 || *r.hs < 0) return fail(TPLA_ERR_SHAPE, "a stride of %s is negative", r.name);
-    if (*r.ts * esz % 16 || *r.hs * esz % 16) return fail(TPLA_ERR_ALIGN, "strides of %s must be whole 16 bytes", r.name);
+    if (*r.ts % (16 / esz) || *r.hs % (16 / esz)) return fail(TPLA_ERR_ALIGN, "strides of %s must be whole 16 bytes", r.name);
+    if (rows_beyond_memory(T, *r.ts, r.heads, *r.hs, esz)) return fail(TPLA_ERR_SHAPE, "strides of %s reach beyond any memory", r.name);
     if (!aligned16(r.p)) return fail(TPLA_ERR_ALIGN, "%s is not 16-byte aligned", r.name);
     // an output whose rows share memory would be written twice
     if (r.written && rows_share(T, *r.ts, r.heads, *r.hs, r.width)) return fail(TPLA_ERR_SHAPE, "rows of %s overlap", r.name);

@@ -284,6 +284,11 @@ int check_dtype(const tpla_shape_t* sh);
 int check_shape(const tpla_shape_t* sh);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Whether rows at i a + j b elements of esz bytes (i < n, j < m) lie further apart than addresses do; offsets of rows that do not fit 64 bits otherwise.
+inline bool rows_beyond_memory(int64_t n, int64_t a, int64_t m, int64_t b, int esz) {
+  return ((__int128)(n - 1) * a + (__int128)(m - 1) * b) * esz >= (__int128)1 << 62;
+}
+
 // Whether two rows of `width` elements share some, of n x m rows that begin at i a + j b (strides a, b >= 0).
 inline bool rows_share(int64_t n, int64_t a, int64_t m, int64_t b, int64_t width) {
   if ((n > 1 && a < width) || (m > 1 && b < width)) return true;
