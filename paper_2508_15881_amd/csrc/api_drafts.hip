@@ -203,8 +203,11 @@ int tpla_apply_rotary(const tpla_shape_t* shape, int32_t layout, int32_t inverse
   const int64_t strides[] = {q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, k_token_stride, k_out_token_stride};
   for (int64_t s : strides) {
     if (s < 0) return fail(TPLA_ERR_SHAPE, "a stride is negative");
-    if (s * esz % 16) return fail(TPLA_ERR_ALIGN, "strides must be whole 16 bytes");
+    if (s % (16 / esz)) return fail(TPLA_ERR_ALIGN, "strides must be whole 16 bytes");
   }
+  if (rows_beyond_memory(T, q_token_stride, shape->H, q_head_stride, esz) || rows_beyond_memory(T, q_out_token_stride, shape->H, q_out_head_stride, esz) ||
+      rows_beyond_memory(T, k_token_stride, 1, 0, esz) || rows_beyond_memory(T, k_out_token_stride, 1, 0, esz))
+    return fail(TPLA_ERR_SHAPE, "strides reach beyond any memory");
   // an output whose rows share memory would be written twice
   if (q && rows_share(T, q_out_token_stride, shape->H, q_out_head_stride, shape->d_r))
     return fail(TPLA_ERR_SHAPE, "rows of q_out overlap");
