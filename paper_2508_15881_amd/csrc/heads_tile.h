@@ -26,7 +26,7 @@ __device__ __forceinline__ void loads_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-// A page id on its way: wait with lds_wait_id before it is used.
+// A page id on its way: all LDS reads are waited for (lgkmcnt 0), with the id as an operand, before it is used.
 __device__ __forceinline__ void lds_request_page(int& id, const int* at) {
   asm volatile("ds_read_b32 %0, %1" : "=v"(id) : "v"(lds_at(reinterpret_cast<const char*>(at))) : "memory");
 }
