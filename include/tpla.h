@@ -554,7 +554,8 @@ typedef struct tpla_heads {
  * in shape->dtype with strides in elements (innermost dense): they may be columns of a wider projection; pointers and strides in whole
  * 16 bytes (TPLA_ERR_ALIGN; the stride of a single token or head means nothing).  q_weight and k_weight [d_k] in shape->dtype or NULL for
  * all ones.  An output may be its input, with the same strides; no other overlap.  q with q_out, or k with k_out, may be NULL; T = 0 does
- * nothing.  Mean, norm, angles' sines and products in float (angles in double), one rounding on the way out.
+ * nothing.  Mean, norm, angles' sines and products in float (angles in double), one rounding on the way out: a row whose squares or
+ * their mean leave the normal range of a float (columns beyond some 1e19, or below 1e-19 with norm_eps = 0) is not normed to length.
  */
 int tpla_norm_rotary_heads(const tpla_heads_t* shape, int32_t layout, int32_t rot_dim, const double* freq, float amplitude,
                            const void* q_weight, const void* k_weight, float norm_eps, const int32_t* positions, int64_t T,

@@ -9,9 +9,9 @@
 // exchanges between lanes, and the weights stay in the registers that the scores came in.  Tiles that every row of the workgroup sees whole run
 // in a loop of their own, without masks and without a look at the block table.
 //
-// Bound by the issue of vector instructions and by the power limit: of a 16384-token prompt (32 heads on 8, 128 columns, 2.2 TFLOP) 1970 - 2060 us = 1.07 - 1.12 PFLOP/s
-// at 2.2 GHz, the matrix cores are busy 46 % of the time and the vector units 57 %.  Weights in bf16 for the second product, their sum in float from
-// the unrounded ones (the log-sum-exp is a float's).
+// Bound by vector and matrix instructions that hardly pass at the same time: of a 16384-token prompt (32 heads on 8, 128 columns, 2.2 TFLOP) 1970 - 2060 us =
+// 1.07 - 1.12 PFLOP/s, the matrix cores are busy 48 % of the time and the vector units 56 %; the socket draws 1375 W of its 1400, the clock is at 2.23 of 2.4 GHz.
+// Weights in bf16 for the second product, as in heads_ranges.hip; their sum in float from the unrounded ones (the log-sum-exp is a float's).
 // Measured and not kept: exponentials of one block of rows between the matrix instructions of the other, the next tile's keys read ahead (2095 us; with the
 // values read once per block 2240, against 2080 in this order at the time); workgroups of 256 rows (2092, 13 packed prompts 148 -> 162 us); fewer instructions
 // for the maximum and the reference (1990 -> 2030: the clock falls).
@@ -76,8 +76,8 @@ __device__ __forceinline__ float wave_most(float v) {
 // Tokens of a part: of a few lengths, the one that ends first by an estimate in tokens (floats: every workgroup comes to the same).  S: workgroups at once.
 //   - no split: the longest item, or where there is more than a round of them, the mean of a round's workgroups and half an item;
 //   - parts of c tokens: c if they are one round, otherwise the mean and half of a part; and HP_MERGE for the partial results.
-// A few parts more than a round take as long as two: two sequences, 16 and 7 tiles of 8512 and 20211 tokens, 8 heads of keys: 536 parts of 4352 tokens 217 us, 480 of
-// 5120 195.  One prompt of 2000 tokens, 504 items, 32 heads on 8: unsplit 87 us, in parts of 1024 79; of 4000, 1000 items: stays unsplit.
+// A few parts more than a round take as long as two: two sequences, 16 and 7 tiles of 8512 and 20211 tokens, 8 heads of keys: 536 parts of 4288 tokens 237 us, 480 of
+// 5120 200.  One prompt of 2000 tokens, 504 items, 32 heads on 8: unsplit 87 us, in parts of 1024 79; of 4000, 1000 items: stays unsplit.
 constexpr float HP_MERGE = 384.f;
 __device__ __forceinline__ int prompt_chunk(const HeadsArgs& a, const PromptSeq& front) {
   const int lane = threadIdx.x & 63;

@@ -8,7 +8,11 @@
 // requested once the scores have read the last ones, the next values after the output product, and eight waves on a compute unit keep some
 // 100 KB on their way.  An item that lies in one range is written at once, the parts of the others are merged by a second kernel.
 // 48 sequences of 500 to 32000 tokens, 32 heads on 8, 128 columns (1.53 GB): 240 us with the merge = 6.4 TB/s, where a pure reader reaches 7.2; one sequence of
-// 9001 tokens 17.5 us: the kernel's 13.5 are lengths, page ids, first tiles, each a round trip, four tiles per wave and the join, then 4 of merge.
+// 9001 tokens 17.5 us: under the profiler the kernel's 14.5 (lengths, page ids, first tiles, each a round trip, four tiles per wave and the join) and 4 of merge.
+//
+// The weights are rounded to bf16 for the second product, as in the latent decode: its instruction takes both operands in one type, and a second one with what
+// the rounding left would double that product.  References, sums and the log-sum-exp are floats of unrounded weights.  Against 64 bits, in norms, outputs in bf16
+// are off by 0.0018 to 0.0023, where float weights (the plain form) leave 0.0016, the rounding of the output.
 #include "heads_tile.h"
 
 #include <algorithm>
