@@ -14,7 +14,7 @@
 // Weights in bf16 for the second product, as in heads_ranges.hip; their sum in float from the unrounded ones (the log-sum-exp is a float's).
 // Measured and not kept: exponentials of one block of rows between the matrix instructions of the other, the next tile's keys read ahead (2095 us; with the
 // values read once per block 2240, against 2080 in this order at the time); workgroups of 256 rows (2092, 13 packed prompts 148 -> 162 us); fewer instructions
-// for the maximum and the reference (1990 -> 2030: the clock falls).
+// for the maximum and the reference (1990 -> 2030).
 #include "heads_tile.h"
 
 #include <algorithm>

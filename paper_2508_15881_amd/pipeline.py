@@ -218,16 +218,13 @@ class HeadsStep:
         """Pages, slots and positions of the new tokens, packed (once per step, for all layers).  counts: pages taken, pages that were missing;
         tokens without a page are neither written nor seen.  news: add_lens as the host knows them, if it does.  They are held to the step's
         room, run then takes as many rows and no others, and the prefill runs on the kernels for as few as the longest has.  Without them
-        (where a captured step is replayed with other numbers) a sequence may have all of run's rows, and rows that no token owns become NaN
-        here, for all layers."""
+        (where a captured step is replayed with other numbers) run takes at least as many rows as there are new tokens, a sequence may have
+        all of them, and rows that no token owns come back as NaN."""
         self.news = None
         if news is not None:
             news = [int(n) for n in news]
             if len(news) != self.shape.B or min(news) < 0 or max(news) > self.max_new or sum(news) > self.T:
                 raise ValueError("new tokens %r of %d sequences, the step has room for %d, %d of a sequence" % (news, self.shape.B, self.T, self.max_new))
-        else:
-            self.o.fill_(math.nan)
-            self.lse.fill_(math.nan)
         B.tpla_extend_sequences(self.tables, seq_lens, add_lens, 0, None, free_pages, n_free, pages_held, pages_held, block_table, self.max_pages,
                                 self.cu, self.slots, self.positions, self.T, self.counts)
         self.news = news
@@ -247,6 +244,9 @@ class HeadsStep:
             B.tpla_decode_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.workspace, self.ws_bytes,
                                 self.o[:T], self.shape.dtype, self.lse[:T])
         else:
+            if self.news is None:
+                self.o[:T].fill_(math.nan)
+                self.lse[:T].fill_(math.nan)
             B.tpla_prefill_heads(self.shape, self.q[:T], k_pool, v_pool, block_table, self.max_pages, seq_lens, self.cu, T,
                                  T if self.news is None else max(self.news), self.workspace, self.ws_bytes, self.o[:T], self.shape.dtype, self.lse[:T])
         return self.o[:T]

@@ -90,6 +90,7 @@ def test_rows_that_no_token_owns_are_no_numbers_of_an_earlier_step(calls):
     s.o.fill_(3.0)
     s.lse.fill_(3.0)
     place(s)
+    assert (s.o == 3.0).all() and (s.lse == 3.0).all()       # the last layer's output stays until the next one's
     assert torch.isnan(run(s, 20)).all() and torch.isnan(s.lse).all()          # (nothing was computed here)
 
 
