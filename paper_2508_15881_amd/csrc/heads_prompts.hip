@@ -9,8 +9,8 @@
 // exchanges between lanes, and the weights stay in the registers that the scores came in.  Tiles that every row of the workgroup sees whole run
 // in a loop of their own, without masks and without a look at the block table.
 //
-// Bound by vector and matrix instructions that hardly pass at the same time: of a 16384-token prompt (32 heads on 8, 128 columns, 2.2 TFLOP) 1970 - 2060 us =
-// 1.07 - 1.12 PFLOP/s, the matrix cores are busy 48 % of the time and the vector units 56 %; the socket draws 1375 W of its 1400, the clock is at 2.23 of 2.4 GHz.
+// Bound by vector and matrix instructions that hardly pass at the same time: of a 16384-token prompt (32 heads on 8, 128 columns, 2.2 TFLOP) 1970 - 2210 us on
+// different boxes = 1.0 - 1.12 PFLOP/s, the matrix cores are busy 48 % of the time and the vector units 56 %; the socket draws 1375 W of its 1400, the clock is at 2.23 of 2.4 GHz.
 // Weights in bf16 for the second product, as in heads_ranges.hip; their sum in float from the unrounded ones (the log-sum-exp is a float's).
 // Measured and not kept: exponentials of one block of rows between the matrix instructions of the other, the next tile's keys read ahead (2095 us; with the
 // values read once per block 2240, against 2080 in this order at the time); workgroups of 256 rows (2092, 13 packed prompts 148 -> 162 us); fewer instructions
